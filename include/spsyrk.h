@@ -17,6 +17,14 @@
  *   spsyrk_offdiag : C   = A_i A_j^T         (full rectangular block, no prune)
  *   spsyrk_mirror  : C   = C_L + C_L^T - D   (symmetric completion of C_L)
  *
+ * Beside them stand the operators of a model whose inputs and targets are
+ * sparse rows (rows of A, rows of C, tokens), between them and dense rows:
+ *   spsyrk_embed, spsyrk_embed_grad             : table lookup, its gradient
+ *   spsyrk_layer_norm, spsyrk_layer_norm_grad   : layer norm, its gradient
+ *   spsyrk_distill, spsyrk_distill_grad         : loss against a teacher's
+ *                                                 stored entries, with gradient
+ * They have conventions of their own, given with them.
+ *
  * Reproducibility: structure and the count semirings are the same bit for
  * bit on every run; plus-times values of rows with many products (the
  * dense-tile accumulator) are summed in an order that may change from run to
@@ -312,6 +320,128 @@ spsyrk_status spsyrk_symm(const spsyrk_csr* C_lower, spsyrk_semiring sr, int64_t
 #define SPSYRK_NOALLOC_SCRATCH_BYTES (128ull << 20)
 spsyrk_status spsyrk_symm_noalloc(const spsyrk_csr* C_lower, spsyrk_semiring sr, int64_t k, const void* X,
                                   int64_t ldx, void* Y, int64_t ldy, void* hip_stream);
+
+/*
+ * Operators between sparse rows and dense rows
+ * --------------------------------------------
+ * Dense rows (spsyrk_dense) are row-major, nrows x ncols with a stride of
+ * ld >= ncols elements from row to row, of 32-bit floats, IEEE 16-bit floats
+ * or bfloat16; any address and stride that is a multiple of the element is
+ * taken.  Sparse rows (spsyrk_entries) are CSR, or rectangular: row r's
+ * entries are col_idx[r * idx_stride + k] and values[r * val_stride + k],
+ * k < per_row.  Their columns need not ascend; one outside [0, ncols) is
+ * padding and takes no part.
+ * - Sums, statistics and products are formed in 32-bit floats; every output
+ *   element is rounded to its type once.
+ * - Outputs are the caller's arrays and must not overlap the inputs.  Every
+ *   result is the same bit for bit on every run (but for the last bits of a
+ *   gradient of spsyrk_distill_grad at a column that one row of the teacher
+ *   lists three times or more).
+ * - Work is ordered on hip_stream; the calls never wait for the device, and
+ *   can be captured into a graph if the allocator can serve memory then.
+ *   The contents of device arrays are therefore not checked on the host: a
+ *   row_ptr that is not canonical gives meaningless values, never an access
+ *   outside the arrays described.
+ * - Workspace comes from the allocator (hipMallocAsync / hipFreeAsync on the
+ *   stream when it is NULL) and is released before the call returns
+ *   (stream-ordered).
+ * Errors: INVALID_ARG (null arrays, negative or contradicting sizes, unknown
+ * types, ld < ncols, misaligned pointers), SHAPE (a dimension or the number
+ * of entries is 2^31 or more), OOM, HIP.
+ */
+typedef enum spsyrk_dtype {
+    SPSYRK_FLOAT32 = 0,
+    SPSYRK_FLOAT16 = 1,
+    SPSYRK_BFLOAT16 = 2
+} spsyrk_dtype;
+
+typedef struct spsyrk_dense {
+    int64_t nrows;
+    int64_t ncols;
+    int64_t ld;
+    int32_t dtype;          /* spsyrk_dtype */
+    void* data;             /* device array; only read where it is an input */
+} spsyrk_dense;
+
+typedef struct spsyrk_entries {
+    int64_t nrows;
+    int64_t ncols;
+    int64_t nnz;            /* CSR: entries; rectangular: ignored */
+    const int64_t* row_ptr; /* [nrows + 1], or NULL for rectangular rows */
+    int64_t per_row;        /* rectangular: entries per row */
+    int64_t idx_stride;     /* rectangular: elements of col_idx from row to row */
+    int64_t val_stride;     /* rectangular: elements of values from row to row */
+    const void* col_idx;
+    int32_t idx_bytes;      /* 4 (int32) or 8 (int64) */
+    int32_t val_dtype;      /* spsyrk_dtype of values */
+    const void* values;     /* may be NULL where a call says so */
+} spsyrk_entries;
+
+/*
+ * Y = scale A W: the lookup of rows of the table W by the columns of A.
+ * A: m x v; rectangular rows hold one entry each and no values (tokens: Y's
+ * row is scale times W's row, or zero for padding), CSR rows any number of
+ * entries, weighted by their values (NULL: 1), summed in their order (rows of
+ * many entries in a fixed order of partial sums).  W: v x d, Y: m x d, of one type.
+ */
+spsyrk_status spsyrk_embed(const spsyrk_entries* A, const spsyrk_dense* W, float scale,
+                           const spsyrk_allocator* al, void* hip_stream, const spsyrk_dense* Y);
+
+/*
+ * dW = scale A^T G: the gradient of the table for the gradient G of Y, every
+ * row of dW written (zero where no entry names it).  The entries are sorted by
+ * column, stably, so that a column's are summed in their order in A.
+ * A as for spsyrk_embed; G: m x d, dW: v x d, of one type.
+ */
+spsyrk_status spsyrk_embed_grad(const spsyrk_entries* A, const spsyrk_dense* G, float scale,
+                                const spsyrk_allocator* al, void* hip_stream, const spsyrk_dense* dW);
+
+/*
+ * Layer norm of every row of X (m x d, d >= 1): y = (x - mean) rstd gamma +
+ * beta with rstd = 1 / sqrt(var + eps), var the mean square of x - mean.
+ * gamma, beta: d elements of param_dtype (SPSYRK_FLOAT32 or X's type), NULL for
+ * ones and zeros.  Y: m x d of X's type.  mean, rstd: m floats each, kept for
+ * the gradient.  eps >= 0.
+ */
+spsyrk_status spsyrk_layer_norm(const spsyrk_dense* X, const void* gamma, const void* beta, int param_dtype,
+                                float eps, void* hip_stream, const spsyrk_dense* Y, float* mean, float* rstd);
+
+/*
+ * The gradient of spsyrk_layer_norm: for the gradient G of Y, with X, mean and
+ * rstd of the forward call and its gamma (NULL: ones): dX (m x d of X's type),
+ * and the parameters' gradients summed over the rows, dgamma and dbeta (d
+ * elements of param_dtype; either may be NULL and is then left out).
+ */
+spsyrk_status spsyrk_layer_norm_grad(const spsyrk_dense* G, const spsyrk_dense* X, const float* mean,
+                                     const float* rstd, const void* gamma, int param_dtype,
+                                     const spsyrk_allocator* al, void* hip_stream, const spsyrk_dense* dX,
+                                     void* dgamma, void* dbeta);
+
+/*
+ * Distillation of the teacher's stored entries (m x v, for example the top
+ * logits of a larger model, or rows of similarities) into the logits S
+ * (m x v): with z = S / T, q = softmax(z) over all columns and p = the softmax
+ * of values / T over a row's entries,
+ *     loss[r] = T^2 sum over the row's entries of p (log p - log q),
+ * T^2 times the divergence of p from q on the entries' columns.  T =
+ * temperature, finite and positive.  Logits of -inf have q = 0; a row without
+ * entries, one whose teacher values are all -inf and one whose logits are all
+ * -inf have loss 0.  NaN or +inf in a row's logits or teacher values make its
+ * loss NaN.  loss: m floats.
+ */
+spsyrk_status spsyrk_distill(const spsyrk_dense* S, const spsyrk_entries* teacher, float temperature,
+                             const spsyrk_allocator* al, void* hip_stream, float* loss);
+
+/*
+ * The same loss together with the gradient of sum over the rows of
+ * weight[r] loss[r] in the logits: dS = weight T (q - p), of S's type (a
+ * column listed more than once in a row has the sum of its p).  weight: m
+ * floats, NULL for ones; a row of weight 0, and one whose loss is 0 for want
+ * of entries or logits, has a gradient of zeros whatever its logits hold.
+ */
+spsyrk_status spsyrk_distill_grad(const spsyrk_dense* S, const spsyrk_entries* teacher, float temperature,
+                                  const float* weight, const spsyrk_allocator* al, void* hip_stream, float* loss,
+                                  const spsyrk_dense* dS);
 
 /* Static description of a status code. */
 const char* spsyrk_status_string(spsyrk_status s);

@@ -9,6 +9,14 @@ unloadable library raises instead of falling back to anything else.
     A = sp.DeviceCSR.from_host(csr, device="cuda:0")
     C = sp.lower(A, "jaccard")          # tril(A A^T), Jaccard values
     F = sp.mirror(C, "jaccard")         # full symmetric matrix
+
+and of the operators between sparse rows and dense rows (``rows.py``):
+
+    h = sp.embed(A, W)                              # A W: rows of a table, tokens or weighted bags
+    y, mean, rstd = sp.layer_norm(h, gamma, beta)
+    loss, dS = sp.distill_grad(S, F, temperature)   # F's rows as the teacher of the logits S
+    dh, dgamma, dbeta = sp.layer_norm_grad(dy, h, mean, rstd, gamma, beta)
+    dW = sp.embed_grad(A, dh, W.shape[0])
 """
 from __future__ import annotations
 
@@ -70,6 +78,34 @@ class Stats(ctypes.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_}
 
 
+class _Dense(ctypes.Structure):
+    _fields_ = [("nrows", ctypes.c_int64), ("ncols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("data", ctypes.c_void_p)]
+
+
+class _Entries(ctypes.Structure):
+    _fields_ = [("nrows", ctypes.c_int64), ("ncols", ctypes.c_int64), ("nnz", ctypes.c_int64),
+                ("row_ptr", ctypes.c_void_p), ("per_row", ctypes.c_int64), ("idx_stride", ctypes.c_int64),
+                ("val_stride", ctypes.c_int64), ("col_idx", ctypes.c_void_p), ("idx_bytes", ctypes.c_int32),
+                ("val_dtype", ctypes.c_int32), ("values", ctypes.c_void_p)]
+
+
+def _declare_rows(lib):
+    """Signatures of the operators between sparse rows and dense rows."""
+    dense, entries, alloc = ctypes.POINTER(_Dense), ctypes.POINTER(_Entries), ctypes.POINTER(_Allocator)
+    ptr, f32, i32 = ctypes.c_void_p, ctypes.c_float, ctypes.c_int
+    for name, args in (
+            ("spsyrk_embed", [entries, dense, f32, alloc, ptr, dense]),
+            ("spsyrk_embed_grad", [entries, dense, f32, alloc, ptr, dense]),
+            ("spsyrk_layer_norm", [dense, ptr, ptr, i32, f32, ptr, dense, ptr, ptr]),
+            ("spsyrk_layer_norm_grad", [dense, dense, ptr, ptr, ptr, i32, alloc, ptr, dense, ptr, ptr]),
+            ("spsyrk_distill", [dense, entries, f32, alloc, ptr, ptr]),
+            ("spsyrk_distill_grad", [dense, entries, f32, ptr, alloc, ptr, ptr, dense])):
+        fn = getattr(lib, name)
+        fn.restype = i32
+        fn.argtypes = args
+
+
 _lib = None
 _lib_lock = threading.Lock()
 
@@ -119,6 +155,7 @@ def library():
             lib.spsyrk_symm_noalloc.restype = ctypes.c_int
             lib.spsyrk_symm_noalloc.argtypes = [ctypes.POINTER(_Csr), ctypes.c_int, ctypes.c_int64, ctypes.c_void_p,
                                                 ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
+            _declare_rows(lib)
             lib.spsyrk_status_string.argtypes = [ctypes.c_int]
             lib.spsyrk_status_string.restype = ctypes.c_char_p
             lib.spsyrk_last_error_detail.argtypes = []
@@ -142,6 +179,8 @@ def library():
 EXPORTS = ("spsyrk_lower", "spsyrk_lower_plan", "spsyrk_lower_execute", "spsyrk_plan_destroy",
            "spsyrk_lower_accumulate", "spsyrk_offdiag", "spsyrk_offdiag_half", "spsyrk_mirror",
            "spsyrk_symm", "spsyrk_symm_noalloc",
+           "spsyrk_embed", "spsyrk_embed_grad", "spsyrk_layer_norm", "spsyrk_layer_norm_grad",
+           "spsyrk_distill", "spsyrk_distill_grad",
            "spsyrk_status_string",
            "spsyrk_last_error_detail", "spsyrk_last_stats", "spsyrk_abi_version", "spsyrk_timing_begin",
            "spsyrk_timing_begin_phases", "spsyrk_timing_end", "spsyrk_debug_build", "spsyrk_debug_flags")
@@ -486,3 +525,16 @@ def timing_end() -> dict:
     if rc != 0:
         raise SpsyrkError(rc, library().spsyrk_last_error_detail().decode())
     return {name: (t.ms[k], t.launches[k]) for k, name in enumerate(PHASES) if t.launches[k]}
+
+
+_ROWS = ("embed", "embed_grad", "layer_norm", "layer_norm_grad", "distill", "distill_grad")
+
+
+def __getattr__(name):
+    # the operators between sparse rows and dense rows (rows.py), which need
+    # torch at import, while this module leaves it to the first call
+    if name in _ROWS:
+        from . import rows
+        fn = globals()[name] = getattr(rows, name)
+        return fn
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

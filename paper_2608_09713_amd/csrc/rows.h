@@ -1,0 +1,144 @@
+// Dense rows of 16- and 32-bit floats next to sparse rows: element types,
+// 16-byte packs, and the arguments of the lookup, layer norm and distillation
+// kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "common.h"
+
+namespace spsyrk {
+
+// element types (same values as spsyrk_dtype)
+enum Dtype : int { kDtF32 = 0, kDtF16 = 1, kDtBF16 = 2 };
+inline int dtype_bytes(int dt) { return dt == kDtF32 ? 4 : 2; }
+
+// f(element) for an element of the type (the dispatch of every launch below)
+template <typename F>
+inline void by_dtype(int dt, F f) {
+    if (dt == kDtF32)
+        f(float());
+    else if (dt == kDtF16)
+        f(_Float16());
+    else
+        f(__bf16());
+}
+
+// 16 bytes of elements.  The vector type is aligned as one element: gfx950
+// loads and stores 16 bytes at any element's address with one instruction, so
+// rows of odd lengths and strides go through the same code as aligned ones.
+template <typename T>
+struct Pack;
+template <>
+struct Pack<float> {
+    static constexpr int N = 4;
+    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <>
+struct Pack<_Float16> {
+    static constexpr int N = 8;
+    typedef _Float16 V __attribute__((ext_vector_type(8), aligned(2)));
+};
+template <>
+struct Pack<__bf16> {
+    static constexpr int N = 8;
+    typedef __bf16 V __attribute__((ext_vector_type(8), aligned(2)));
+};
+template <typename T>
+using PackV = typename Pack<T>::V;
+
+// The pack at p, of which the first `valid` elements exist (others read as
+// `fill`; nothing past them is touched).
+template <typename T>
+__device__ inline PackV<T> load_pack(const T* p, int64_t valid, float fill = 0.f) {
+    constexpr int N = Pack<T>::N;
+    if (valid >= N) return *reinterpret_cast<const PackV<T>*>(p);
+    PackV<T> v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = i < valid ? p[i] : T(fill);
+    return v;
+}
+
+// the same for data read once (a streamed load)
+template <typename T>
+__device__ inline PackV<T> load_pack_nt(const T* p, int64_t valid, float fill = 0.f) {
+    if (valid >= Pack<T>::N) return __builtin_nontemporal_load(reinterpret_cast<const PackV<T>*>(p));
+    return load_pack(p, valid, fill);
+}
+
+template <typename T>
+__device__ inline void store_pack(T* p, PackV<T> v, int64_t valid) {
+    constexpr int N = Pack<T>::N;
+    if (valid >= N) {
+        *reinterpret_cast<PackV<T>*>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < valid) p[i] = v[i];
+}
+
+template <typename T>
+__device__ inline void store_pack_nt(T* p, PackV<T> v, int64_t valid) {
+    if (valid >= Pack<T>::N)
+        __builtin_nontemporal_store(v, reinterpret_cast<PackV<T>*>(p));
+    else
+        store_pack(p, v, valid);
+}
+
+// one value of a run-time type
+__device__ inline float load_value(const void* p, int dt, int64_t i) {
+    if (dt == kDtF32) return static_cast<const float*>(p)[i];
+    if (dt == kDtF16) return float(static_cast<const _Float16*>(p)[i]);
+    return float(static_cast<const __bf16*>(p)[i]);
+}
+
+// Sparse rows: CSR (rp), or rectangular rows of per_row entries, row r's
+// columns from idx[r * istride] and values from val[r * vstride].  Columns of
+// 4 or 8 bytes (ib); those outside [0, n) are padding.
+struct Entries {
+    int64_t m = 0, n = 0, nnz = 0;
+    const int64_t* rp = nullptr;
+    int64_t per_row = 0, istride = 0, vstride = 0;
+    const void* idx = nullptr;
+    int ib = 4;
+    const void* val = nullptr;  // null: every value is 1
+    int vt = kDtF32;
+};
+
+__device__ inline int64_t load_column(const void* idx, int ib, int64_t i) {
+    return ib == 4 ? int64_t(static_cast<const int32_t*>(idx)[i]) : static_cast<const int64_t*>(idx)[i];
+}
+
+struct DenseRows {
+    int64_t m = 0, n = 0, ld = 0;
+    int dt = kDtF32;
+    void* p = nullptr;
+};
+
+// ---- embed.hip
+// Y = scale A W: one column per row (tokens), or CSR rows.
+void embed_tokens(const Entries& A, const DenseRows& W, float scale, const DenseRows& Y, hipStream_t s);
+size_t embed_csr_tmp_bytes(int64_t nnz, int64_t d);
+void embed_csr(const Entries& A, const DenseRows& W, float scale, const DenseRows& Y, void* tmp, hipStream_t s);
+// dW = scale A^T G, dW of A.n rows.  tmp: embed_grad_tmp_bytes(A, d)
+size_t embed_grad_tmp_bytes(const Entries& A, int64_t d);
+void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRows& dW, void* tmp, hipStream_t s);
+
+// ---- norm.hip
+// Parameters and their gradients are of type pt; null: none.
+void layer_norm(const DenseRows& X, const void* gamma, const void* beta, int pt, float eps, const DenseRows& Y,
+                float* mean, float* rstd, hipStream_t s);
+size_t layer_norm_grad_tmp_bytes(int64_t m, int64_t d, int dt, bool params);
+void layer_norm_grad(const DenseRows& G, const DenseRows& X, const float* mean, const float* rstd, const void* gamma,
+                     int pt, const DenseRows& dX, void* dgamma, void* dbeta, void* tmp, hipStream_t s);
+
+// ---- distill.hip
+// loss of every row; with dS.p its gradient too, times weight (null: 1)
+size_t distill_tmp_bytes(int64_t m, int64_t v, int dt, bool grad);
+void distill(const DenseRows& S, const Entries& teacher, float temperature, const float* weight, float* loss,
+             const DenseRows& dS, void* tmp, hipStream_t s);
+
+}  // namespace spsyrk

@@ -1,0 +1,258 @@
+"""Operators of a model whose inputs and targets are sparse rows: table lookup,
+layer norm and distillation, forward and backward (C-ABI in
+``include/spsyrk.h``).
+
+Dense arguments are torch tensors of one GPU, float32, float16 or bfloat16,
+whose last dimension is contiguous; rows may be strided (a slice of columns).
+Leading dimensions count as rows where they can be walked with one stride.
+Work is enqueued on the current stream of the tensors' device and nothing waits
+for it.  Autograd does not record these calls: every gradient is a call of its
+own.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+import paper_2608_09713_amd as _sp
+
+_DTYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_byref = ctypes.byref
+
+
+def _rows(t, name):
+    """(_Dense of the tensor's rows, number of rows); the last dimension is the columns."""
+    dt = _DTYPE.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, not {t.dtype}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dim() < 1:
+        raise ValueError(f"{name} must have at least one dimension")
+    cols = t.shape[-1]
+    if t.is_contiguous():
+        rows = t.numel() // cols if cols else t.shape[:-1].numel()
+        return _sp._Dense(rows, cols, cols, dt, t.data_ptr())
+    try:
+        v = t.view(-1, cols) if t.dim() != 2 else t
+    except RuntimeError:
+        v = None
+    if v is None or v.stride(1) != 1 or (v.shape[0] > 1 and v.stride(0) < cols):
+        raise ValueError(f"{name} must have rows of contiguous elements at one stride")
+    return _sp._Dense(v.shape[0], cols, max(v.stride(0), cols), dt, v.data_ptr())
+
+
+def _vector(t, name, n, dtypes, device):
+    """Address of a contiguous vector of n elements (None: null)."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, not {t.dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, of {n} elements")
+    _same_device(device, t, name)
+    return t.data_ptr()
+
+
+def _same_device(device, t, name):
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+
+
+def _entries_csr(A, values, name):
+    """_Entries of a DeviceCSR."""
+    for t, want in ((A.row_ptr, (torch.int64,)), (A.col_idx, (torch.int32, torch.int64))):
+        if t.dtype not in want:
+            raise TypeError(f"{name}: row_ptr must be int64, col_idx int32 or int64")
+        if not t.is_cuda or not t.is_contiguous():
+            raise TypeError(f"{name}: CSR arrays must be contiguous device tensors")
+    if A.row_ptr.numel() != A.nrows + 1 or A.col_idx.numel() < A.nnz:
+        raise ValueError(f"{name}: row_ptr must have nrows + 1 entries and col_idx at least nnz")
+    v, vp, vt = A.values, None, 0
+    if v is not None:
+        vt = _DTYPE.get(v.dtype)
+        if vt is None:
+            raise TypeError(f"{name}: values must be float32, float16 or bfloat16, not {v.dtype}")
+        if v.numel() < A.nnz or not v.is_contiguous():
+            raise ValueError(f"{name}: values must be contiguous, of at least nnz entries")
+        _same_device(A.row_ptr.device, v, f"{name}.values")
+        vp = v.data_ptr()
+    elif values:
+        raise TypeError(f"{name}: values are required")
+    _same_device(A.row_ptr.device, A.col_idx, f"{name}.col_idx")
+    return _sp._Entries(A.nrows, A.ncols, A.nnz, A.row_ptr.data_ptr(), 0, 0, 0, A.col_idx.data_ptr(),
+                        A.col_idx.element_size(), vt, vp)
+
+
+def _tokens(t, ncols, name):
+    """_Entries of a tensor of tokens, one row each."""
+    if t.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"{name} must be a DeviceCSR, or int32 or int64 tokens, not {t.dtype}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    n, stride = t.numel(), 1
+    if not t.is_contiguous():
+        if t.dim() != 1 or t.stride(0) < 0:
+            raise ValueError(f"{name} must be contiguous, or one strided dimension")
+        stride = t.stride(0)
+    return _sp._Entries(n, ncols, 0, None, 1, stride, 0, t.data_ptr(), t.element_size(), 0, None)
+
+
+def _run(fn, device, args, workspace):
+    """Call fn(*args) on the device's current stream; args may hold _STREAM and _ALLOC."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _run(fn, device, args, workspace)
+    arena = _sp._TorchArena(device) if workspace else None
+    stream = torch.cuda.current_stream(device).cuda_stream
+    rc = fn(*[stream if a is _STREAM else (_byref(arena.struct) if arena else None) if a is _ALLOC else a
+              for a in args])
+    if rc != 0:
+        raise _sp.SpsyrkError(rc, _sp.library().spsyrk_last_error_detail().decode())
+    if arena and arena.live:
+        raise RuntimeError("library left allocations unreleased")
+
+
+_STREAM, _ALLOC = object(), object()
+
+
+def embed(rows, weight, scale=1.0):
+    """Rows of the table ``weight`` (v x d): ``scale`` times ``weight[token]`` for
+    a tensor of tokens (shape + (d,); zeros for tokens outside [0, v), which are
+    padding), or ``scale * A @ weight`` for a DeviceCSR (m x d; its values, or
+    ones, weight the entries)  (spsyrk_embed)."""
+    lib = _sp.library()
+    w = _rows(weight, "weight")
+    if weight.dim() != 2:
+        raise ValueError("weight must be v x d")
+    if isinstance(rows, torch.Tensor):
+        a, csr, shape = _tokens(rows, w.nrows, "rows"), False, rows.shape
+        _same_device(weight.device, rows, "rows")
+    else:
+        a, csr, shape = _entries_csr(rows, False, "rows"), True, (rows.nrows,)
+        _same_device(weight.device, rows.row_ptr, "rows")
+    out = torch.empty((*shape, w.ncols), dtype=weight.dtype, device=weight.device)
+    y = _sp._Dense(a.nrows, w.ncols, w.ncols, w.dtype, out.data_ptr())
+    _run(lib.spsyrk_embed, weight.device, (_byref(a), _byref(w), scale, _ALLOC, _STREAM, _byref(y)), csr)
+    return out
+
+
+def embed_grad(rows, grad, v, scale=1.0):
+    """The gradient (v x d) of the table looked up by ``embed(rows, weight,
+    scale)`` for the gradient ``grad`` of its result: ``scale * A.T @ grad``,
+    summed by entries sorted by column (spsyrk_embed_grad)."""
+    lib = _sp.library()
+    g = _rows(grad, "grad")
+    if isinstance(rows, torch.Tensor):
+        a, first = _tokens(rows, v, "rows"), rows
+    else:
+        a, first = _entries_csr(rows, False, "rows"), rows.row_ptr
+    _same_device(grad.device, first, "rows")
+    out = torch.empty((v, g.ncols), dtype=grad.dtype, device=grad.device)
+    w = _sp._Dense(v, g.ncols, g.ncols, g.dtype, out.data_ptr())
+    _run(lib.spsyrk_embed_grad, grad.device, (_byref(a), _byref(g), scale, _ALLOC, _STREAM, _byref(w)), True)
+    return out
+
+
+def _params(x, d, weight, bias, what):
+    """(type code, addresses) of the layer norm's parameters."""
+    first = weight if weight is not None else bias
+    pt = x.dtype if first is None else first.dtype
+    if pt not in (torch.float32, x.dtype):
+        raise TypeError(f"{what}: weight and bias must be float32 or {x.dtype}, not {pt}")
+    return (_DTYPE[pt], _vector(weight, "weight", d, (pt,), x.device), _vector(bias, "bias", d, (pt,), x.device), pt)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """(y, mean, rstd): y = (x - mean) rstd weight + bias over the last dimension,
+    with the rows' mean and 1 / sqrt(var + eps) as float32 (spsyrk_layer_norm).
+    ``weight`` and ``bias``: float32 or x's type, None for ones and zeros."""
+    lib = _sp.library()
+    a = _rows(x, "x")
+    pt, wp, bp, _ = _params(x, a.ncols, weight, bias, "layer_norm")
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    o = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, y.data_ptr())
+    _run(lib.spsyrk_layer_norm, x.device,
+         (_byref(a), wp, bp, pt, eps, _STREAM, _byref(o), mean.data_ptr(), rstd.data_ptr()), False)
+    return y, mean, rstd
+
+
+def layer_norm_grad(grad, x, mean, rstd, weight=None, bias=None):
+    """(dx, dweight, dbias) of ``layer_norm(x, weight, bias)`` for the gradient
+    ``grad`` of y; dweight and dbias have the parameters' type and are None for
+    a parameter that is None (spsyrk_layer_norm_grad)."""
+    lib = _sp.library()
+    g, a = _rows(grad, "grad"), _rows(x, "x")
+    if grad.shape != x.shape:
+        raise ValueError("grad and x must have one shape")
+    _same_device(x.device, grad, "grad")
+    pt, wp, _, pdt = _params(x, a.ncols, weight, bias, "layer_norm_grad")
+    mp = _vector(mean, "mean", a.nrows, (torch.float32,), x.device)
+    rp = _vector(rstd, "rstd", a.nrows, (torch.float32,), x.device)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dw = None if weight is None else torch.empty(weight.shape, dtype=pdt, device=x.device)
+    db = None if bias is None else torch.empty(bias.shape, dtype=pdt, device=x.device)
+    o = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, dx.data_ptr())
+    _run(lib.spsyrk_layer_norm_grad, x.device,
+         (_byref(g), _byref(a), mp, rp, wp, pt, _ALLOC, _STREAM, _byref(o),
+          None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()),
+         dw is not None or db is not None)
+    return dx, dw, db
+
+
+def _teacher(teacher, s, logits):
+    """_Entries of a DeviceCSR, or of a (values, indices) pair with the logits' leading dimensions."""
+    if not isinstance(teacher, tuple):
+        e = _entries_csr(teacher, True, "teacher")
+        _same_device(logits.device, teacher.row_ptr, "teacher")
+        return e
+    values, indices = teacher
+    if values.shape != indices.shape or values.shape[:-1] != logits.shape[:-1]:
+        raise ValueError("the teacher's values and indices must have one shape, and the logits' leading dimensions")
+    if indices.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"the teacher's indices must be int32 or int64, not {indices.dtype}")
+    _same_device(logits.device, values, "teacher values")
+    _same_device(logits.device, indices, "teacher indices")
+    v = _rows(values, "teacher values")
+    k = v.ncols
+    stride = k
+    if not indices.is_contiguous():
+        if indices.dim() != 2 or indices.stride(1) != 1:
+            raise ValueError("the teacher's indices must be contiguous, or strided rows of contiguous elements")
+        stride = indices.stride(0)
+    return _sp._Entries(s.nrows, s.ncols, 0, None, k, stride, v.ld, indices.data_ptr(), indices.element_size(),
+                        v.dtype, values.data_ptr())
+
+
+def distill(logits, teacher, temperature=1.0):
+    """Loss (float32, one per row of ``logits``) of distilling the teacher's
+    stored entries: temperature^2 times the divergence of the logits' softmax
+    from the teacher's softmax over the row's entries (spsyrk_distill).
+    ``teacher``: a DeviceCSR over the logits' columns, or a tuple (values,
+    indices) as torch.topk returns; indices outside the columns are padding."""
+    lib = _sp.library()
+    s = _rows(logits, "logits")
+    t = _teacher(teacher, s, logits)
+    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
+    _run(lib.spsyrk_distill, logits.device,
+         (_byref(s), _byref(t), temperature, _ALLOC, _STREAM, loss.data_ptr()), True)
+    return loss
+
+
+def distill_grad(logits, teacher, temperature=1.0, weight=None):
+    """(loss, gradient): ``distill`` together with the gradient, of the logits'
+    type, of ``(weight * loss).sum()`` (``weight``: float32, one per row; None
+    for ones)  (spsyrk_distill_grad)."""
+    lib = _sp.library()
+    s = _rows(logits, "logits")
+    t = _teacher(teacher, s, logits)
+    wp = _vector(weight, "weight", s.nrows, (torch.float32,), logits.device)
+    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
+    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    g = _sp._Dense(s.nrows, s.ncols, s.ncols, s.dtype, grad.data_ptr())
+    _run(lib.spsyrk_distill_grad, logits.device,
+         (_byref(s), _byref(t), temperature, wp, _ALLOC, _STREAM, loss.data_ptr(), _byref(g)), True)
+    return loss, grad
