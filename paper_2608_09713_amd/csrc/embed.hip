@@ -9,8 +9,8 @@
 // (stable, so a column's entries are added in their order in A and the result
 // is the same on every run).  Sums are held in 32-bit floats and rounded once.
 //
-// A wavefront takes a target's columns 16 bytes a lane, kUnroll packs of a
-// row at once; targets of narrow rows share a wavefront.  A target of more
+// A wavefront takes a target's columns 16 bytes a lane, a few packs of a row
+// at once; targets of narrow rows share a wavefront.  A target of more
 // than a tile of entries (a frequent token) would be walked by one wavefront:
 // such targets are left to a second launch, in which every tile of entries
 // sums its part of the (at most two) long targets that reach into it, and a
@@ -23,7 +23,8 @@
 namespace spsyrk {
 namespace {
 
-constexpr int kUnroll = 4;  // packs of one row per lane
+constexpr int kUnroll = 4;     // packs of one row per lane: tokens
+constexpr int kSumUnroll = 2;  // and sums, which hold several entries' packs
 
 // Lanes per row (a power of two, at most a wavefront) for rows of `packs` packs.
 inline int lane_bits(int64_t packs) {
@@ -42,11 +43,10 @@ __device__ inline int64_t all_waves() { return int64_t(gridDim.x) * kWavesPerBlo
 
 // ---- tokens
 
-template <typename T, int U>
+template <typename T, int N, int U>
 __global__ __launch_bounds__(kBlock) void tokens_kernel(Entries A, const T* __restrict__ W, int64_t ldw, int64_t d,
                                                         float scale, T* __restrict__ Y, int64_t ldy, int lg,
                                                         int64_t chunks, int64_t units) {
-    constexpr int N = Pack<T>::N;
     const int lane = lane_id(), sub = lane >> lg, l = lane & ((1 << lg) - 1);
     const int rows = kWave >> lg;
     for (int64_t u = first_wave(); u < units; u += all_waves()) {
@@ -55,21 +55,23 @@ __global__ __launch_bounds__(kBlock) void tokens_kernel(Entries A, const T* __re
         const int64_t c0 = (u % chunks * (int64_t(U) << lg) + l) * N;
         const int64_t col = load_column(A.idx, A.ib, row * A.istride);
         const bool named = col >= 0 && col < A.n;
-        const T* src = W + (named ? col * ldw : 0);
-        PackV<T> v[U];
+        const T* src = W + col * ldw;
+        Vec<T, N> v[U];
+        Place at[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int64_t c = c0 + (int64_t(k) << lg) * N;
-            v[k] = load_pack(src + c, named ? d - c : 0);
+            at[k] = place<N>(c0 + (int64_t(k) << lg) * N, d);
+            v[k] = Vec<T, N>(T(0.f));
+            if (named) v[k] = load_vec<T, N>(src + at[k].c);
         }
         T* dst = Y + row * ldy;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int64_t c = c0 + (int64_t(k) << lg) * N;
-            PackV<T> o;
+            if (at[k].skip >= N) break;
+            Vec<T, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[i] = T(float(v[k][i]) * scale);
-            store_pack_nt(dst + c, o, d - c);
+            store_vec_nt<T, N>(dst + at[k].c, o);
         }
     }
 }
@@ -87,20 +89,20 @@ struct Targets {
     int ib;
     const void* w;  // weight of every entry (null: 1)
     int wt;
+    const uint32_t* owner;  // target of every entry (null: found by search)
     __device__ inline int64_t at(int64_t t) const {
         const int64_t s = int64_t(start[t]);
         return s < 0 ? 0 : (s > nnz ? nnz : s);
     }
 };
 
-// acc += sum of the entries [a, b) over the lane's packs at c0, c0 + (N << lg), ...
+// acc += sum of the entries [a, b) over the lane's packs.
 // Every group of 1 << lg lanes reads its entries' rows and weights one per
-// lane and takes them from there by lane reads.
-template <typename T, int U, typename P>
+// lane and takes them from there by lane reads; E entries' packs are in
+// flight at once.
+template <typename T, int N, int U, int E, typename P>
 __device__ inline void sum_entries(const Targets<P>& t, int64_t a, int64_t b, const T* __restrict__ src,
-                                   int64_t nsrc, int64_t ld, int64_t d, int64_t c0, int lg,
-                                   float (&acc)[U][Pack<T>::N]) {
-    constexpr int N = Pack<T>::N;
+                                   int64_t nsrc, int64_t ld, const Place (&at)[U], int lg, float (&acc)[U][N]) {
     const int width = 1 << lg, l = lane_id() & (width - 1);
     for (int64_t base = a; base < b; base += width) {
         int64_t row = -1;
@@ -111,52 +113,58 @@ __device__ inline void sum_entries(const Targets<P>& t, int64_t a, int64_t b, co
             if (row < 0 || row >= nsrc) row = -1;
         }
         const int n = int(min(int64_t(width), b - base));
-        for (int j = 0; j < n; ++j) {
-            const int64_t r = __shfl(row, j, width);
-            const float wj = __shfl(w, j, width);
-            if (r < 0) continue;
-            const T* p = src + r * ld;
+        for (int j = 0; j < n; j += E) {
+            Vec<T, N> v[E][U];
+            float wj[E];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int64_t c = c0 + (int64_t(k) << lg) * N;
-                const PackV<T> v = load_pack(p + c, d - c);
+            for (int x = 0; x < E; ++x) {
+                const int y = min(j + x, width - 1);
+                int64_t r = __shfl(row, y, width);
+                wj[x] = __shfl(w, y, width);
+                if (j + x >= n) r = -1;
+                // (nothing is read for padding, which adds zeros)
 #pragma unroll
-                for (int i = 0; i < N; ++i) acc[k][i] = fmaf(wj, float(v[i]), acc[k][i]);
+                for (int k = 0; k < U; ++k) v[x][k] = Vec<T, N>(T(0.f));
+                if (r >= 0) {
+                    const T* p = src + r * ld;
+#pragma unroll
+                    for (int k = 0; k < U; ++k) v[x][k] = load_vec<T, N>(p + at[k].c);
+                }
             }
+#pragma unroll
+            for (int x = 0; x < E; ++x)
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) acc[k][i] = fmaf(wj[x], float(v[x][k][i]), acc[k][i]);
         }
     }
 }
 
-template <typename T, int U, typename P>
-__global__ __launch_bounds__(kBlock) void sum_targets(Targets<P> t, const T* __restrict__ src, int64_t nsrc,
-                                                      int64_t lds, int64_t d, float scale, T* __restrict__ out,
-                                                      int64_t ldo, int lg, int64_t chunks, int64_t units,
-                                                      int64_t tile) {
-    constexpr int N = Pack<T>::N;
-    const int lane = lane_id(), sub = lane >> lg, l = lane & ((1 << lg) - 1);
-    const int rows = kWave >> lg;
-    for (int64_t u = first_wave(); u < units; u += all_waves()) {
-        const int64_t target = u / chunks * rows + sub;
-        if (target >= t.targets) continue;
-        const int64_t a = t.at(target), b = t.at(target + 1);
-        if (b - a > tile) continue;
-        const int64_t c0 = (u % chunks * (int64_t(U) << lg) + l) * N;
-        float acc[U][N] = {};
-        sum_entries<T, U>(t, a, b, src, nsrc, lds, d, c0, lg, acc);
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int64_t c = c0 + (int64_t(k) << lg) * N;
-            PackV<T> o;
-#pragma unroll
-            for (int i = 0; i < N; ++i) o[i] = T(acc[k][i] * scale);
-            store_pack_nt(out + target * ldo + c, o, d - c);
-        }
-    }
-}
+// What one launch of the sums works on.
+template <typename T, typename P>
+struct Sums {
+    Targets<P> t;
+    const T* src;
+    int64_t nsrc, lds, d;
+    float scale;
+    T* out;
+    int64_t ldo;
+    int lg;
+    int64_t chunks;            // wavefronts per target
+    int64_t tile, ntiles;
+    float* part;               // two rows of dp sums per tile
+    int64_t dp;
+    int32_t* long_of;          // the targets that those belong to (-1: none)
+    unsigned tile_blocks;      // workgroups of the tiles, before those of the targets
+    int64_t tile_units, target_units;
+    int per;                   // targets that a group of lanes takes, one after another
+};
 
 // the target that holds entry e: the largest t in [0, targets) with start[t] <= e
 template <typename P>
 __device__ inline int64_t target_of(const Targets<P>& t, int64_t e) {
+    if (t.owner) return t.owner[e];
     int64_t lo = 0, hi = t.targets - 1;
     while (lo < hi) {
         const int64_t mid = (lo + hi + 1) >> 1;
@@ -171,70 +179,131 @@ __device__ inline int64_t target_of(const Targets<P>& t, int64_t e) {
 // Tile q's part of the long targets that hold its first and its last entry,
 // into part[2 q] and part[2 q + 1] (the latter only for a target that starts
 // inside the tile).
-template <typename T, int U, typename P>
-__global__ __launch_bounds__(kBlock) void sum_tiles(Targets<P> t, const T* __restrict__ src, int64_t nsrc,
-                                                    int64_t lds, int64_t d, float* __restrict__ part, int64_t tile,
-                                                    int lg, int64_t chunks, int64_t units, int64_t ntiles) {
-    constexpr int N = Pack<T>::N;
-    const int lane = lane_id(), sub = lane >> lg, l = lane & ((1 << lg) - 1);
-    const int rows = kWave >> lg;
-    const int64_t end = t.at(t.targets);
-    for (int64_t u = first_wave(); u < units; u += all_waves()) {
-        const int64_t q = u / chunks * rows + sub;
-        const int64_t e0 = q * tile, e1 = min(end, e0 + tile);
-        if (q >= ntiles || e0 >= e1) continue;
-        const int64_t c0 = (u % chunks * (int64_t(U) << lg) + l) * N;
-        const int64_t first = target_of(t, e0), last = target_of(t, e1 - 1);
-        for (int k2 = 0; k2 < 2; ++k2) {
-            const int64_t target = k2 ? last : first;
-            if (k2 && last == first) break;
-            const int64_t a = t.at(target), b = t.at(target + 1);
-            if (b - a <= tile) continue;
+template <typename T, int N, int U, typename P>
+__device__ inline void sum_tile(const Sums<T, P>& a, int64_t q, int64_t chunk, int l, int64_t end) {
+    const int64_t e0 = q * a.tile, e1 = min(end, e0 + a.tile);
+    int64_t of[2] = {-1, -1};
+    if (e0 < e1) {
+        of[0] = target_of(a.t, e0);
+        of[1] = target_of(a.t, e1 - 1);
+        if (of[1] == of[0]) of[1] = -1;
+    }
+    Place at[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) at[k] = place<N>((chunk * (int64_t(U) << a.lg) + (int64_t(k) << a.lg) + l) * N, a.d);
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        int64_t x0 = 0, x1 = 0;
+        if (of[z] >= 0) {
+            x0 = a.t.at(of[z]);
+            x1 = a.t.at(of[z] + 1);
+            if (x1 - x0 <= a.tile) of[z] = -1;
+        }
+        if (chunk == 0 && l == 0) a.long_of[2 * q + z] = int32_t(of[z]);
+        if (of[z] < 0) continue;
+        float acc[U][N] = {};
+        sum_entries<T, N, U, 4>(a.t, max(x0, e0), min(x1, e1), a.src, a.nsrc, a.lds, at, a.lg, acc);
+        float* dst = a.part + (2 * q + z) * a.dp;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (at[k].skip >= N) break;
+            Vec<float, N> o;
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = acc[k][i];
+            store_vec<float, N>(dst + at[k].c, o);
+        }
+    }
+}
+
+template <typename T, int N, int U, typename P>
+__global__ __launch_bounds__(kBlock) void sums_kernel(Sums<T, P> a) {
+    const int lane = lane_id(), sub = lane >> a.lg, l = lane & ((1 << a.lg) - 1);
+    const int rows = kWave >> a.lg;
+    const int w = threadIdx.x / kWave;
+    if (blockIdx.x < a.tile_blocks) {
+        const int64_t end = a.t.at(a.t.targets);
+        for (int64_t u = int64_t(blockIdx.x) * kWavesPerBlock + w; u < a.tile_units;
+             u += int64_t(a.tile_blocks) * kWavesPerBlock) {
+            const int64_t q = u / a.chunks * rows + sub;
+            if (q < a.ntiles) sum_tile<T, N, U>(a, q, u % a.chunks, l, end);
+        }
+        return;
+    }
+    for (int64_t u = int64_t(blockIdx.x - a.tile_blocks) * kWavesPerBlock + w; u < a.target_units;
+         u += int64_t(gridDim.x - a.tile_blocks) * kWavesPerBlock) {
+        const int64_t t0 = (u / a.chunks * rows + sub) * a.per;
+        if (t0 >= a.t.targets) continue;
+        Place at[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            at[k] = place<N>((u % a.chunks * (int64_t(U) << a.lg) + (int64_t(k) << a.lg) + l) * N, a.d);
+        // the starts of the group's targets, one per lane (per < 1 << lg, or one target)
+        const int n = int(min(int64_t(a.per), a.t.targets - t0));
+        int64_t s = a.t.at(t0 + min(l, n));
+        int64_t x1 = a.per == 1 ? a.t.at(t0) : __shfl(s, 0, 1 << a.lg);
+        for (int j = 0; j < n; ++j) {
+            const int64_t x0 = x1;
+            x1 = a.per == 1 ? a.t.at(t0 + 1) : __shfl(s, j + 1, 1 << a.lg);
+            if (x1 - x0 > a.tile) continue;
             float acc[U][N] = {};
-            sum_entries<T, U>(t, max(a, e0), min(b, e1), src, nsrc, lds, d, c0, lg, acc);
-            float* dst = part + (2 * q + k2) * d;
+            sum_entries<T, N, U, U == 1 ? 4 : 2>(a.t, x0, x1, a.src, a.nsrc, a.lds, at, a.lg, acc);
+            T* dst = a.out + (t0 + j) * a.ldo;
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-                const int64_t c = c0 + (int64_t(k) << lg) * N;
+                if (at[k].skip >= N) break;
+                Vec<T, N> o;
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (c + i < d) dst[c + i] = acc[k][i];
+                for (int i = 0; i < N; ++i) o[i] = T(acc[k][i] * a.scale);
+                store_vec_nt<T, N>(dst + at[k].c, o);
             }
         }
     }
 }
 
 // The long target that starts in tile q, if any (it holds the tile's last
-// entry): its parts in tile order, 64 columns per workgroup.
+// entry): its parts in tile order within a wavefront, the wavefronts' in
+// theirs; 256 columns at a time.
 template <typename T, typename P>
-__global__ __launch_bounds__(kBlock) void join_tiles(Targets<P> t, const float* __restrict__ part, int64_t d,
-                                                     float scale, T* __restrict__ out, int64_t ldo, int64_t tile,
-                                                     int64_t ntiles) {
-    __shared__ float sum[kWavesPerBlock][kWave];
+__global__ __launch_bounds__(kBlock) void join_tiles(Sums<T, P> a) {
+    __shared__ float4 sum[kWavesPerBlock][kWave];
     const int64_t q = blockIdx.x;
-    const int64_t end = t.at(t.targets);
-    const int64_t e0 = q * tile, e1 = min(end, e0 + tile);
-    if (e0 >= e1) return;
-    const int64_t target = target_of(t, e1 - 1);
-    const int64_t a = t.at(target), b = t.at(target + 1);
-    if (b - a <= tile || a < e0 || a >= e1) return;
-    const int64_t tiles = min((b - 1) / tile, ntiles - 1) - q + 1;
-    // the target's part of its first tile is the second one if another target
-    // holds that tile's first entry
-    const int64_t skip = target_of(t, e0) == target ? 0 : 1;
-    const int w = threadIdx.x / kWave, lane = lane_id();
+    const int z = a.long_of[2 * q + 1] >= 0 ? 1 : 0;
+    const int64_t target = a.long_of[2 * q + z];
+    if (target < 0) return;
+    const int64_t x0 = a.t.at(target), x1 = a.t.at(target + 1);
+    if (x1 <= x0 || x0 / a.tile != q) return;
+    const int64_t tiles = min((x1 - 1) / a.tile, a.ntiles - 1) - q + 1;
+    const int w = threadIdx.x / kWave, l = lane_id();
     const int64_t per = (tiles + kWavesPerBlock - 1) / kWavesPerBlock;
-    for (int64_t c = int64_t(blockIdx.y) * kWave + lane; c - lane < d; c += int64_t(gridDim.y) * kWave) {
-        float s = 0.f;
-        if (c < d)
-            for (int64_t x = w * per; x < min(tiles, (w + 1) * per); ++x)
-                s += part[(2 * (q + x) + (x == 0 ? skip : 0)) * d + c];
-        sum[w][lane] = s;
+    const float* p = a.part + 2 * q * a.dp;
+    for (int64_t c = int64_t(blockIdx.y) * 4 * kWave + 4 * l; c - 4 * l < a.d; c += int64_t(gridDim.y) * 4 * kWave) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < a.d) {
+            const int64_t end = min(tiles, (w + 1) * per);
+#pragma unroll 4
+            for (int64_t x = w * per; x < end; ++x) {
+                const float4 v = *reinterpret_cast<const float4*>(p + (2 * x + (x == 0 ? z : 0)) * a.dp + c);
+                s.x += v.x;
+                s.y += v.y;
+                s.z += v.z;
+                s.w += v.w;
+            }
+        }
+        sum[w][l] = s;
         __syncthreads();
-        if (w == 0 && c < d) {
-            float r = 0.f;
-            for (int i = 0; i < kWavesPerBlock; ++i) r += sum[i][lane];
-            out[target * ldo + c] = T(r * scale);
+        if (w == 0 && c < a.d) {
+#pragma unroll
+            for (int i = 1; i < kWavesPerBlock; ++i) {
+                const float4 v = sum[i][l];
+                s.x += v.x;
+                s.y += v.y;
+                s.z += v.z;
+                s.w += v.w;
+            }
+            const float r[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i < a.d) a.out[target * a.ldo + c + i] = T(r[i] * a.scale);
         }
         __syncthreads();
     }
@@ -243,7 +312,7 @@ __global__ __launch_bounds__(kBlock) void join_tiles(Targets<P> t, const float* 
 // Entries per tile: 64, doubled for every fourfold of 2^16 entries, so that
 // neither a tile nor the parts of one target grow past the square root of
 // the entries by much.
-inline int64_t sum_tile(int64_t nnz) {
+inline int64_t sum_tile_entries(int64_t nnz) {
     int64_t t = 64;
     while (t * t * 16 < nnz) t *= 2;
     return t;
@@ -251,42 +320,57 @@ inline int64_t sum_tile(int64_t nnz) {
 
 inline size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 
+inline int64_t part_columns(int64_t d) { return (d + 3) & ~int64_t(3); }
+
 inline size_t part_bytes(int64_t nnz, int64_t d) {
-    const int64_t tile = sum_tile(nnz);
-    return nnz > tile ? size_t((nnz + tile - 1) / tile) * 2 * size_t(d) * sizeof(float) : 0;
+    const int64_t tile = sum_tile_entries(nnz);
+    if (nnz <= tile) return 0;
+    const size_t rows = size_t((nnz + tile - 1) / tile) * 2;
+    return round256(rows * size_t(part_columns(d)) * sizeof(float)) + round256(rows * sizeof(int32_t));
 }
 
-template <typename T, int U, typename P>
-void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const DenseRows& out, float* part,
+template <typename T, int N, int U, typename P>
+void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const DenseRows& out, void* tmp,
                  int64_t packs, int lg, hipStream_t s) {
-    const int64_t chunks = (packs + (int64_t(U) << lg) - 1) / (int64_t(U) << lg);
-    const int64_t rows = kWave >> lg, d = out.n;
-    const int64_t tile = sum_tile(t.nnz);
-    const int64_t units = (t.targets + rows - 1) / rows * chunks;
-    const T* sp = static_cast<const T*>(src.p);
-    T* op = static_cast<T*>(out.p);
-    sum_targets<T, U, P><<<grid_for(units), kBlock, 0, s>>>(t, sp, src.m, src.ld, d, scale, op, out.ld, lg, chunks,
-                                                            units, tile);
-    if (t.nnz <= tile) return;  // (no target is long)
-    const int64_t ntiles = (t.nnz + tile - 1) / tile;
-    const int64_t tunits = (ntiles + rows - 1) / rows * chunks;
-    sum_tiles<T, U, P><<<grid_for(tunits), kBlock, 0, s>>>(t, sp, src.m, src.ld, d, part, tile, lg, chunks, tunits,
-                                                           ntiles);
-    join_tiles<T, P><<<dim3(unsigned(ntiles), unsigned(std::min<int64_t>((d + kWave - 1) / kWave, 64))), kBlock, 0,
-                       s>>>(t, part, d, scale, op, out.ld, tile, ntiles);
+    Sums<T, P> a;
+    a.t = t;
+    a.src = static_cast<const T*>(src.p);
+    a.nsrc = src.m;
+    a.lds = src.ld;
+    a.d = out.n;
+    a.scale = scale;
+    a.out = static_cast<T*>(out.p);
+    a.ldo = out.ld;
+    a.lg = lg;
+    a.chunks = (packs + (int64_t(U) << lg) - 1) / (int64_t(U) << lg);
+    const int64_t rows = kWave >> lg;
+    a.tile = sum_tile_entries(t.nnz);
+    a.ntiles = t.nnz > a.tile ? (t.nnz + a.tile - 1) / a.tile : 0;  // (no target is long)
+    a.dp = part_columns(a.d);
+    a.part = static_cast<float*>(tmp);
+    a.long_of = reinterpret_cast<int32_t*>(static_cast<char*>(tmp) +
+                                           round256(size_t(a.ntiles) * 2 * size_t(a.dp) * sizeof(float)));
+    a.tile_units = (a.ntiles + rows - 1) / rows * a.chunks;
+    a.tile_blocks = a.ntiles ? grid_for(a.tile_units) : 0;
+    a.per = lg >= 4 && t.targets >= (int64_t(1) << 15) ? 8 : 1;
+    a.target_units = (t.targets + rows * a.per - 1) / (rows * a.per) * a.chunks;
+    sums_kernel<T, N, U, P><<<a.tile_blocks + grid_for(a.target_units), kBlock, 0, s>>>(a);
+    if (a.ntiles)
+        join_tiles<T, P><<<dim3(unsigned(a.ntiles), unsigned(std::min<int64_t>((a.d + 255) / 256, 4))), kBlock, 0,
+                           s>>>(a);
 }
 
 template <typename P>
-void grouped_sums(const Targets<P>& t, const DenseRows& src, float scale, const DenseRows& out, float* part,
+void grouped_sums(const Targets<P>& t, const DenseRows& src, float scale, const DenseRows& out, void* tmp,
                   hipStream_t s) {
-    by_dtype(out.dt, [&](auto e) {
+    by_width(out.dt, out.n, [&](auto e, auto width) {
         using T = decltype(e);
-        const int64_t packs = (out.n + Pack<T>::N - 1) / Pack<T>::N;
+        constexpr int N = decltype(width)::value;
+        const int64_t packs = (out.n + N - 1) / N;
         const int lg = lane_bits(packs);
-        if (packs <= kWave)
-            launch_sums<T, 1, P>(t, src, scale, out, part, packs, lg, s);
-        else
-            launch_sums<T, kUnroll, P>(t, src, scale, out, part, packs, lg, s);
+        if constexpr (N > 1)
+            if (packs > kWave) return launch_sums<T, N, kSumUnroll, P>(t, src, scale, out, tmp, packs, lg, s);
+        launch_sums<T, N, 1, P>(t, src, scale, out, tmp, packs, lg, s);
     });
 }
 
@@ -305,17 +389,39 @@ __device__ inline int64_t row_of(const int64_t* rp, int64_t m, int64_t e) {
     return lo;
 }
 
-// Sort records: the column (n for padding, which sorts past every column),
-// the row and the weight of every entry.
+// Sort records of CSR entries, or of many tokens: the column (n for padding,
+// which sorts past every column), the row and the weight of every entry.  A
+// workgroup takes kRecords entries; the pointers of their rows are searched in
+// LDS where they fit.
+constexpr int kRecords = 2048;
+constexpr int kRecordRows = 2048;
 __global__ __launch_bounds__(kBlock) void sort_records(Entries A, uint32_t* __restrict__ key,
                                                        uint32_t* __restrict__ row, float* __restrict__ w) {
-    const int64_t stride = int64_t(gridDim.x) * kBlock;
-    for (int64_t e = int64_t(blockIdx.x) * kBlock + threadIdx.x; e < A.nnz; e += stride) {
-        const int64_t r = A.rp ? row_of(A.rp, A.m, e) : e;
-        const int64_t c = load_column(A.idx, A.ib, A.rp ? e : e * A.istride);
-        key[e] = uint32_t(c >= 0 && c < A.n ? c : A.n);
-        row[e] = uint32_t(r);
-        if (w) w[e] = load_value(A.val, A.vt, e);
+    __shared__ int64_t range[2];
+    __shared__ int64_t ptr[kRecordRows];
+    for (int64_t e0 = int64_t(blockIdx.x) * kRecords; e0 < A.nnz; e0 += int64_t(gridDim.x) * kRecords) {
+        const int64_t e1 = min(A.nnz, e0 + kRecords);
+        int64_t r0 = 0, n = 0;
+        if (A.rp) {
+            __syncthreads();
+            if (threadIdx.x < 2) range[threadIdx.x] = row_of(A.rp, A.m, threadIdx.x ? e1 - 1 : e0);
+            __syncthreads();
+            r0 = range[0];
+            n = range[1] - r0 + 1;
+            if (n >= 1 && n <= kRecordRows) {
+                for (int i = threadIdx.x; i < n; i += kBlock) ptr[i] = A.rp[r0 + i];
+                __syncthreads();
+            } else {
+                n = 0;
+            }
+        }
+        for (int64_t e = e0 + threadIdx.x; e < e1; e += kBlock) {
+            const int64_t r = !A.rp ? e : n ? r0 + max(upper_bound_lds(ptr, 0, int(n), e) - 1, 0) : row_of(A.rp, A.m, e);
+            const int64_t c = load_column(A.idx, A.ib, A.rp ? e : e * A.istride);
+            key[e] = uint32_t(c >= 0 && c < A.n ? c : A.n);
+            row[e] = uint32_t(r);
+            if (w) w[e] = load_value(A.val, A.vt, e);
+        }
     }
 }
 
@@ -327,6 +433,156 @@ __global__ __launch_bounds__(kBlock) void column_bounds(const uint32_t* __restri
         start[c] = uint32_t(lower_bound_u32(key, 0, nnz, uint64_t(c)));
 }
 
+// Few tokens are sorted in two launches, against three per digit and two more
+// of the radix sort, which for few records is all launches and latency.
+// The columns are dealt to at most kSortGroups groups of consecutive columns.
+// First, tiles of 1024 tokens are split by group (stable, padding left out),
+// with every tile's first record of every group; then one workgroup per group
+// takes its records from the tiles in order and sorts them by column.
+constexpr int kSortBlock = 1024;
+constexpr int kSortWaves = kSortBlock / kWave;
+constexpr int kSortBins = 1024;   // columns per group, at most
+constexpr int kSortGroups = 512;
+constexpr int kSortBatch = 4;     // groups of 64 records read at once
+constexpr int64_t kFewTokens = int64_t(1) << 17;
+
+// Lanes of the wavefront with a lane's value (of `bits` bits), among those of `in`.
+__device__ inline uint64_t lanes_of(uint32_t x, int bits, bool in) {
+    uint64_t same = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+        const bool one = (x >> b) & 1;
+        const uint64_t m = __ballot(one);
+        same &= one ? m : ~m;
+    }
+    return same;
+}
+
+// Turns the counts hist[wavefront][x], x < n <= kSortBlock, into first places
+// from `first` on, by x and then by wavefront; returns x's first place to
+// thread x and the end to all.
+template <int W>
+__device__ inline uint32_t places(uint32_t (*hist)[W], int n, uint32_t first, uint32_t* scratch, uint32_t* end) {
+    uint32_t own = 0, total;
+    const int x = threadIdx.x;
+    if (x < n)
+        for (int i = 0; i < kSortWaves; ++i) own += hist[i][x];
+    const uint32_t at = first + block_exclusive_scan<uint32_t, kSortBlock>(own, scratch, &total);
+    uint32_t next = at;
+    if (x < n)
+        for (int i = 0; i < kSortWaves; ++i) {
+            const uint32_t c = hist[i][x];
+            hist[i][x] = next;
+            next += c;
+        }
+    *end = first + total;
+    __syncthreads();
+    return at;
+}
+
+template <typename I>
+__global__ __launch_bounds__(kSortBlock) void split_tokens(const I* __restrict__ tok, int64_t stride, int64_t n,
+                                                           int64_t v, int lgbins, int groups, int bits,
+                                                           uint2* __restrict__ rec, uint32_t* __restrict__ first) {
+    __shared__ uint32_t hist[kSortWaves][kSortGroups];
+    __shared__ uint32_t scratch[kSortWaves];
+    const int w = threadIdx.x / kWave;
+    for (int i = threadIdx.x; i < kSortWaves * kSortGroups; i += kSortBlock) hist[0][i] = 0;
+    const int64_t e = int64_t(blockIdx.x) * kSortBlock + threadIdx.x;
+    const int64_t t = e < n ? int64_t(tok[e * stride]) : -1;
+    const bool in = t >= 0 && t < v;
+    const uint32_t g = in ? uint32_t(t) >> lgbins : 0;
+    __syncthreads();
+    const uint64_t same = lanes_of(g, bits, in);
+    const uint32_t rank = __popcll(same & lanemask_lt());
+    if (in && rank == 0) hist[w][g] = __popcll(same);
+    __syncthreads();
+    uint32_t end;
+    const uint32_t at = places(hist, groups, 0, scratch, &end);
+    uint32_t* f = first + int64_t(blockIdx.x) * (groups + 1);
+    if (int(threadIdx.x) < groups) f[threadIdx.x] = at;
+    if (threadIdx.x == 0) f[groups] = end;
+    if (in) rec[int64_t(blockIdx.x) * kSortBlock + hist[w][g] + rank] = make_uint2(uint32_t(t), uint32_t(e));
+}
+
+__global__ __launch_bounds__(kSortBlock) void sort_groups(const uint2* __restrict__ rec,
+                                                          const uint32_t* __restrict__ first, int tiles, int groups,
+                                                          int lgbins, int64_t v, uint32_t* __restrict__ start,
+                                                          uint32_t* __restrict__ key, uint32_t* __restrict__ row) {
+    constexpr int kTiles = int(kFewTokens / kSortBlock);
+    __shared__ uint32_t hist[kSortWaves][kSortBins];
+    __shared__ uint32_t scratch[kSortWaves];
+    __shared__ uint32_t upto[kTiles + 1], from[kTiles];  // the group's records before each tile, and in the tile
+    const int g = blockIdx.x, bins = 1 << lgbins;
+    const int w = threadIdx.x / kWave, l = lane_id();
+    for (int i = threadIdx.x; i < kSortWaves * bins; i += kSortBlock) hist[i >> lgbins][i & (bins - 1)] = 0;
+    uint32_t before = 0, count = 0;
+    if (int(threadIdx.x) < tiles) {
+        const uint32_t* f = first + int64_t(threadIdx.x) * (groups + 1) + g;
+        before = f[0];
+        count = f[1] - before;
+        from[threadIdx.x] = threadIdx.x * kSortBlock + before;
+    }
+    uint32_t m, all;
+    const uint32_t mine = block_exclusive_scan<uint32_t, kSortBlock>(count, scratch, &m);
+    (void)block_exclusive_scan<uint32_t, kSortBlock>(before, scratch, &all);
+    if (int(threadIdx.x) <= tiles) upto[threadIdx.x] = int(threadIdx.x) < tiles ? mine : m;
+    __syncthreads();
+    // records of consecutive stretches, whole groups of 64, one stretch per wavefront
+    const uint32_t per = ((m + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
+    const uint32_t i0 = w * per, i1 = min(m, i0 + per);
+    const uint32_t lo = uint32_t(g) << lgbins;
+    uint2 r[kSortBatch];
+    auto load = [&](uint32_t base) {
+#pragma unroll
+        for (int k = 0; k < kSortBatch; ++k) {
+            const uint32_t i = base + k * kWave + l;
+            r[k] = make_uint2(~0u, 0u);
+            if (i < i1) {
+                const int q = upper_bound_lds(upto, 0, tiles, i) - 1;
+                r[k] = rec[from[q] + (i - upto[q])];
+            }
+        }
+    };
+    for (uint32_t i = i0; i < i1; i += kSortBatch * kWave) {
+        load(i);
+#pragma unroll
+        for (int k = 0; k < kSortBatch; ++k)
+            if (r[k].x != ~0u) atomicAdd(&hist[w][r[k].x - lo], 1u);
+    }
+    __syncthreads();
+    uint32_t end;
+    const uint32_t at = places(hist, bins, all, scratch, &end);
+    if (int(threadIdx.x) < bins && int64_t(lo) + threadIdx.x < v) start[lo + threadIdx.x] = at;
+    if (g == groups - 1 && threadIdx.x == 0) start[v] = end;
+    for (uint32_t i = i0; i < i1; i += kSortBatch * kWave) {
+        if (per > kSortBatch * kWave) load(i);  // (else they are still held)
+#pragma unroll
+        for (int k = 0; k < kSortBatch; ++k) {
+            const bool in = r[k].x != ~0u;
+            const uint32_t bin = in ? r[k].x - lo : 0;
+            const uint64_t same = lanes_of(bin, lgbins, in);
+            const uint32_t rank = __popcll(same & lanemask_lt());
+            if (in) {
+                const uint32_t pos = hist[w][bin] + rank;
+                key[pos] = r[k].x;
+                row[pos] = r[k].y;
+            }
+            // (a wavefront's LDS accesses are in order, and only it uses this row)
+            __builtin_amdgcn_wave_barrier();
+            if (in && rank == 0) hist[w][bin] += __popcll(same);
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
+// log2 of the columns per group (-1: the tokens go by the radix sort)
+inline int few_tokens_bins(const Entries& A) {
+    if (A.rp || A.m > kFewTokens || A.n > int64_t(kSortBins) * kSortGroups) return -1;
+    int lg = 0;
+    while ((int64_t(256) << lg) < A.n && (1 << lg) < kSortBins) ++lg;
+    return lg;
+}
+
 inline unsigned thread_grid(int64_t n) {
     return unsigned(std::min<int64_t>((n + kBlock - 1) / kBlock, int64_t(1) << 16));
 }
@@ -334,9 +590,10 @@ inline unsigned thread_grid(int64_t n) {
 }  // namespace
 
 void embed_tokens(const Entries& A, const DenseRows& W, float scale, const DenseRows& Y, hipStream_t s) {
-    by_dtype(Y.dt, [&](auto e) {
+    by_width(Y.dt, Y.n, [&](auto e, auto width) {
         using T = decltype(e);
-        const int64_t packs = (Y.n + Pack<T>::N - 1) / Pack<T>::N;
+        constexpr int N = decltype(width)::value;
+        const int64_t packs = (Y.n + N - 1) / N;
         const int lg = lane_bits(packs);
         const int64_t per = packs <= kWave ? 1 : kUnroll;
         const int64_t chunks = (packs + (per << lg) - 1) / (per << lg);
@@ -344,25 +601,35 @@ void embed_tokens(const Entries& A, const DenseRows& W, float scale, const Dense
         const int64_t units = (A.m + rows - 1) / rows * chunks;
         const T* w = static_cast<const T*>(W.p);
         T* y = static_cast<T*>(Y.p);
-        if (per == 1)
-            tokens_kernel<T, 1><<<grid_for(units), kBlock, 0, s>>>(A, w, W.ld, Y.n, scale, y, Y.ld, lg, chunks, units);
-        else
-            tokens_kernel<T, kUnroll><<<grid_for(units), kBlock, 0, s>>>(A, w, W.ld, Y.n, scale, y, Y.ld, lg, chunks,
-                                                                         units);
+        if constexpr (N > 1)
+            if (per > 1) {
+                tokens_kernel<T, N, kUnroll><<<grid_for(units), kBlock, 0, s>>>(A, w, W.ld, Y.n, scale, y, Y.ld, lg,
+                                                                                chunks, units);
+                return;
+            }
+        tokens_kernel<T, N, 1><<<grid_for(units), kBlock, 0, s>>>(A, w, W.ld, Y.n, scale, y, Y.ld, lg, chunks, units);
     });
 }
 
 size_t embed_csr_tmp_bytes(int64_t nnz, int64_t d) { return part_bytes(nnz, d); }
 
 void embed_csr(const Entries& A, const DenseRows& W, float scale, const DenseRows& Y, void* tmp, hipStream_t s) {
-    Targets<int64_t> t{A.rp, A.m, A.nnz, A.idx, A.ib, A.val, A.vt};
-    grouped_sums(t, W, scale, Y, static_cast<float*>(tmp), s);
+    Targets<int64_t> t{A.rp, A.m, A.nnz, A.idx, A.ib, A.val, A.vt, nullptr};
+    grouped_sums(t, W, scale, Y, tmp, s);
+}
+
+// Scratch of the sort: the radix sort's, or every tile's first records by group.
+static size_t sort_scratch_bytes(const Entries& A) {
+    if (few_tokens_bins(A) < 0) return round256(radix_tmp_bytes(A.nnz));
+    return round256(size_t((A.nnz + kSortBlock - 1) / kSortBlock) * (kSortGroups + 1) * sizeof(uint32_t));
 }
 
 size_t embed_grad_tmp_bytes(const Entries& A, int64_t d) {
-    const size_t words = round256(size_t(A.nnz) * sizeof(uint32_t));
-    return words * (A.val ? 6 : 4) + round256(size_t(A.n + 1) * sizeof(uint32_t)) +
-           round256(radix_tmp_bytes(A.nnz)) + part_bytes(A.nnz, d);
+    // keys and rows, sorted and before; the latter are records of both in the
+    // split, which end at most a tile past the entries
+    const size_t words = round256((size_t(A.nnz) + kSortBlock) * sizeof(uint32_t));
+    return words * (A.val ? 6 : 4) + round256(size_t(A.n + 1) * sizeof(uint32_t)) + sort_scratch_bytes(A) +
+           part_bytes(A.nnz, d);
 }
 
 void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRows& dW, void* tmp, hipStream_t s) {
@@ -372,7 +639,7 @@ void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRo
         at += round256(bytes);
         return p;
     };
-    const size_t words = size_t(A.nnz) * sizeof(uint32_t);
+    const size_t words = (size_t(A.nnz) + kSortBlock) * sizeof(uint32_t);
     uint32_t* start = reinterpret_cast<uint32_t*>(take(size_t(A.n + 1) * sizeof(uint32_t)));
     uint32_t *key[2], *row[2];
     float* w[2] = {nullptr, nullptr};
@@ -381,16 +648,32 @@ void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRo
         row[i] = reinterpret_cast<uint32_t*>(take(words));
         if (A.val) w[i] = reinterpret_cast<float*>(take(words));
     }
-    void* sort_tmp = take(radix_tmp_bytes(A.nnz));
+    void* sort_tmp = take(sort_scratch_bytes(A));
     int which = 0;
-    if (A.nnz > 0) {
-        sort_records<<<thread_grid(A.nnz), kBlock, 0, s>>>(A, key[0], row[0], w[0]);
+    const int lgbins = few_tokens_bins(A);
+    if (lgbins >= 0) {
+        const int groups = int((A.n + (int64_t(1) << lgbins) - 1) >> lgbins);
+        const int tiles = int((A.nnz + kSortBlock - 1) / kSortBlock);
+        uint2* rec = reinterpret_cast<uint2*>(key[1]);   // (nnz records: two of the sort's buffers)
+        uint32_t* first = static_cast<uint32_t*>(sort_tmp);
+        if (tiles > 0) {
+            const int bits = bit_width_u64(uint64_t(groups - 1));
+            if (A.ib == 4)
+                split_tokens<int32_t><<<tiles, kSortBlock, 0, s>>>(static_cast<const int32_t*>(A.idx), A.istride, A.nnz,
+                                                                   A.n, lgbins, groups, bits, rec, first);
+            else
+                split_tokens<int64_t><<<tiles, kSortBlock, 0, s>>>(static_cast<const int64_t*>(A.idx), A.istride, A.nnz,
+                                                                   A.n, lgbins, groups, bits, rec, first);
+        }
+        sort_groups<<<groups, kSortBlock, 0, s>>>(rec, first, tiles, groups, lgbins, A.n, start, key[0], row[0]);
+    } else if (A.nnz > 0) {
+        sort_records<<<unsigned(std::min<int64_t>((A.nnz + kRecords - 1) / kRecords, 1 << 16)), kBlock, 0, s>>>(A, key[0], row[0], w[0]);
         which = radix_sort(key[0], key[1], row[0], row[1], w[0], w[1], A.val ? 4 : 0, A.nnz,
                            bit_width_u64(uint64_t(A.n)), sort_tmp, s);
     }
-    column_bounds<<<thread_grid(A.n + 1), kBlock, 0, s>>>(key[which], A.nnz, A.n, start);
-    Targets<uint32_t> t{start, A.n, A.nnz, row[which], 4, w[which], kDtF32};
-    grouped_sums(t, G, scale, dW, reinterpret_cast<float*>(at), s);
+    if (lgbins < 0) column_bounds<<<thread_grid(A.n + 1), kBlock, 0, s>>>(key[which], A.nnz, A.n, start);
+    Targets<uint32_t> t{start, A.n, A.nnz, row[which], 4, w[which], kDtF32, key[which]};
+    grouped_sums(t, G, scale, dW, at, s);
 }
 
 }  // namespace spsyrk

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "common.h"
 
@@ -86,6 +87,57 @@ __device__ inline void store_pack_nt(T* p, PackV<T> v, int64_t valid) {
         __builtin_nontemporal_store(v, reinterpret_cast<PackV<T>*>(p));
     else
         store_pack(p, v, valid);
+}
+
+// N elements, aligned as one (see above): a whole pack, or one element for
+// rows shorter than a pack.
+template <typename T, int N>
+struct VecOf {
+    typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+template <typename T, int N>
+using Vec = typename VecOf<T, N>::V;
+
+// Where the N elements from column c on are taken in a row of d >= N columns:
+// a pack that would pass the row's end is moved back onto its last N columns.
+// Its first `skip` elements then belong to other packs too (all N if c >= d):
+// maps may write them twice, with one value; sums leave them out.
+struct Place {
+    int c, skip;
+};
+template <int N>
+__device__ inline Place place(int64_t c, int64_t d) {
+    const int64_t at = min(c, d - N);
+    return {int(at), int(min(c - at, int64_t(N)))};
+}
+template <typename T, int N>
+__device__ inline Vec<T, N> load_vec(const T* p) {
+    return *reinterpret_cast<const Vec<T, N>*>(p);
+}
+template <typename T, int N>
+__device__ inline Vec<T, N> load_vec_nt(const T* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const Vec<T, N>*>(p));
+}
+template <typename T, int N>
+__device__ inline void store_vec(T* p, Vec<T, N> v) {
+    *reinterpret_cast<Vec<T, N>*>(p) = v;
+}
+template <typename T, int N>
+__device__ inline void store_vec_nt(T* p, Vec<T, N> v) {
+    __builtin_nontemporal_store(v, reinterpret_cast<Vec<T, N>*>(p));
+}
+
+// f(element, width): the pack width for rows of d columns
+template <typename F>
+inline void by_width(int dt, int64_t d, F f) {
+    by_dtype(dt, [&](auto e) {
+        using T = decltype(e);
+        constexpr int N = 16 / int(sizeof(T));
+        if (d >= N)
+            f(e, std::integral_constant<int, N>());
+        else
+            f(e, std::integral_constant<int, 1>());
+    });
 }
 
 // one value of a run-time type
