@@ -89,7 +89,8 @@ struct Targets {
     int ib;
     const void* w;  // weight of every entry (null: 1)
     int wt;
-    const uint32_t* owner;  // target of every entry (null: found by search)
+    const uint32_t* owner;  // target of every tile's first and last entry, by entry (null: found by search)
+    int step;               // words from an entry's row, and weight, to the next one's
     __device__ inline int64_t at(int64_t t) const {
         const int64_t s = int64_t(start[t]);
         return s < 0 ? 0 : (s > nnz ? nnz : s);
@@ -108,8 +109,8 @@ __device__ inline void sum_entries(const Targets<P>& t, int64_t a, int64_t b, co
         int64_t row = -1;
         float w = 0.f;
         if (base + l < b) {
-            row = load_column(t.from, t.ib, base + l);
-            w = t.w ? load_value(t.w, t.wt, base + l) : 1.f;
+            row = load_column(t.from, t.ib, (base + l) * t.step);
+            w = t.w ? load_value(t.w, t.wt, (base + l) * t.step) : 1.f;
             if (row < 0 || row >= nsrc) row = -1;
         }
         const int n = int(min(int64_t(width), b - base));
@@ -215,6 +216,71 @@ __device__ inline void sum_tile(const Sums<T, P>& a, int64_t q, int64_t chunk, i
     }
 }
 
+// Targets t0 + j .. t0 + r - 1, whose entries are [x0, end): kSumEntries
+// entries' packs are in flight at once, across targets.
+constexpr int kSumEntries = 4;
+template <typename T, int N, int U, typename P, typename S>
+__device__ inline void sum_run(const Sums<T, P>& a, int64_t t0, int j, int r, int64_t x0, int64_t end,
+                               const S& start, const Place (&at)[U]) {
+    constexpr int E = kSumEntries;
+    const int width = 1 << a.lg, l = lane_id() & (width - 1);
+    float acc[U][N] = {};
+    int64_t next = start(j + 1);
+    auto flush = [&]() {
+        T* dst = a.out + (t0 + j) * a.ldo;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            Vec<T, N> o;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                o[i] = T(acc[k][i] * a.scale);
+                acc[k][i] = 0.f;
+            }
+            if (at[k].skip < N) store_vec_nt<T, N>(dst + at[k].c, o);
+        }
+        ++j;
+        if (j < r) next = start(j + 1);
+    };
+    for (int64_t base = x0; base < end; base += width) {
+        int64_t row = -1;
+        float w = 0.f;
+        if (base + l < end) {
+            row = load_column(a.t.from, a.t.ib, (base + l) * a.t.step);
+            w = a.t.w ? load_value(a.t.w, a.t.wt, (base + l) * a.t.step) : 1.f;
+            if (row < 0 || row >= a.nsrc) row = -1;
+        }
+        const int n = int(min(int64_t(width), end - base));
+        for (int y = 0; y < n; y += E) {
+            Vec<T, N> v[E][U];
+            float wj[E];
+#pragma unroll
+            for (int x = 0; x < E; ++x) {
+                int64_t q = __shfl(row, min(y + x, width - 1), width);
+                wj[x] = __shfl(w, min(y + x, width - 1), width);
+                if (y + x >= n) q = -1;
+                // (nothing is read for padding, which adds zeros)
+#pragma unroll
+                for (int k = 0; k < U; ++k) v[x][k] = Vec<T, N>(T(0.f));
+                if (q >= 0) {
+                    const T* p = a.src + q * a.lds;
+#pragma unroll
+                    for (int k = 0; k < U; ++k) v[x][k] = load_vec<T, N>(p + at[k].c);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < E; ++x) {
+                if (y + x < n)
+                    while (base + y + x >= next) flush();
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) acc[k][i] = fmaf(wj[x], float(v[x][k][i]), acc[k][i]);
+            }
+        }
+    }
+    while (j < r) flush();
+}
+
 template <typename T, int N, int U, typename P>
 __global__ __launch_bounds__(kBlock) void sums_kernel(Sums<T, P> a) {
     const int lane = lane_id(), sub = lane >> a.lg, l = lane & ((1 << a.lg) - 1);
@@ -238,24 +304,25 @@ __global__ __launch_bounds__(kBlock) void sums_kernel(Sums<T, P> a) {
         for (int k = 0; k < U; ++k)
             at[k] = place<N>((u % a.chunks * (int64_t(U) << a.lg) + (int64_t(k) << a.lg) + l) * N, a.d);
         // the starts of the group's targets, one per lane (per < 1 << lg, or one target)
-        const int n = int(min(int64_t(a.per), a.t.targets - t0));
-        int64_t s = a.t.at(t0 + min(l, n));
-        int64_t x1 = a.per == 1 ? a.t.at(t0) : __shfl(s, 0, 1 << a.lg);
-        for (int j = 0; j < n; ++j) {
-            const int64_t x0 = x1;
-            x1 = a.per == 1 ? a.t.at(t0 + 1) : __shfl(s, j + 1, 1 << a.lg);
-            if (x1 - x0 > a.tile) continue;
-            float acc[U][N] = {};
-            sum_entries<T, N, U, U == 1 ? 4 : 2>(a.t, x0, x1, a.src, a.nsrc, a.lds, at, a.lg, acc);
-            T* dst = a.out + (t0 + j) * a.ldo;
-#pragma unroll
-            for (int k = 0; k < U; ++k) {
-                if (at[k].skip >= N) break;
-                Vec<T, N> o;
-#pragma unroll
-                for (int i = 0; i < N; ++i) o[i] = T(acc[k][i] * a.scale);
-                store_vec_nt<T, N>(dst + at[k].c, o);
+        const int n = int(min(int64_t(a.per), a.t.targets - t0)), width = 1 << a.lg;
+        const int64_t s = a.t.at(t0 + min(l, n));
+        auto start = [&](int j) { return a.per == 1 ? a.t.at(t0 + j) : __shfl(s, j, width); };
+        for (int j = 0; j < n;) {
+            // a run of targets none of which is long: their entries follow one
+            // another and are read without regard to where a target ends
+            const int64_t x0 = start(j);
+            int64_t end = x0;
+            int r = j;
+            for (; r < n; ++r) {
+                const int64_t next = start(r + 1);
+                if (next - end > a.tile) break;
+                end = next;
             }
+            if (r > j)
+                sum_run<T, N, U>(a, t0, j, r, x0, end, start, at);
+            else
+                ++r;
+            j = r;
         }
     }
 }
@@ -356,7 +423,7 @@ void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const D
     a.target_units = (t.targets + rows * a.per - 1) / (rows * a.per) * a.chunks;
     sums_kernel<T, N, U, P><<<a.tile_blocks + grid_for(a.target_units), kBlock, 0, s>>>(a);
     if (a.ntiles)
-        join_tiles<T, P><<<dim3(unsigned(a.ntiles), unsigned(std::min<int64_t>((a.d + 255) / 256, 4))), kBlock, 0,
+        join_tiles<T, P><<<dim3(unsigned(a.ntiles), unsigned(std::min<int64_t>((a.d + 255) / 256, 16))), kBlock, 0,
                            s>>>(a);
 }
 
@@ -376,53 +443,18 @@ void grouped_sums(const Targets<P>& t, const DenseRows& src, float scale, const 
 
 // ---- the gradient's entries sorted by column
 
-// the row that holds entry e (row pointers kept inside [0, nnz])
+// The row that holds entry e, found by a whole wavefront: 64 probes a step.
+// (Any row pointers end the search, inside [0, m).)
 __device__ inline int64_t row_of(const int64_t* rp, int64_t m, int64_t e) {
     int64_t lo = 0, hi = m - 1;
     while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (rp[mid] <= e)
-            lo = mid;
-        else
-            hi = mid - 1;
+        const int64_t n = hi - lo, step = (n + kWave - 1) / kWave;
+        const uint64_t below = __ballot(rp[lo + min((lane_id() + 1) * step, n)] <= e);
+        const int64_t c = below == ~uint64_t(0) ? kWave : __builtin_ctzll(~below);
+        hi = min(hi, lo + (c + 1) * step - 1);
+        lo += min(c * step, n);
     }
-    return lo;
-}
-
-// Sort records of CSR entries, or of many tokens: the column (n for padding,
-// which sorts past every column), the row and the weight of every entry.  A
-// workgroup takes kRecords entries; the pointers of their rows are searched in
-// LDS where they fit.
-constexpr int kRecords = 2048;
-constexpr int kRecordRows = 2048;
-__global__ __launch_bounds__(kBlock) void sort_records(Entries A, uint32_t* __restrict__ key,
-                                                       uint32_t* __restrict__ row, float* __restrict__ w) {
-    __shared__ int64_t range[2];
-    __shared__ int64_t ptr[kRecordRows];
-    for (int64_t e0 = int64_t(blockIdx.x) * kRecords; e0 < A.nnz; e0 += int64_t(gridDim.x) * kRecords) {
-        const int64_t e1 = min(A.nnz, e0 + kRecords);
-        int64_t r0 = 0, n = 0;
-        if (A.rp) {
-            __syncthreads();
-            if (threadIdx.x < 2) range[threadIdx.x] = row_of(A.rp, A.m, threadIdx.x ? e1 - 1 : e0);
-            __syncthreads();
-            r0 = range[0];
-            n = range[1] - r0 + 1;
-            if (n >= 1 && n <= kRecordRows) {
-                for (int i = threadIdx.x; i < n; i += kBlock) ptr[i] = A.rp[r0 + i];
-                __syncthreads();
-            } else {
-                n = 0;
-            }
-        }
-        for (int64_t e = e0 + threadIdx.x; e < e1; e += kBlock) {
-            const int64_t r = !A.rp ? e : n ? r0 + max(upper_bound_lds(ptr, 0, int(n), e) - 1, 0) : row_of(A.rp, A.m, e);
-            const int64_t c = load_column(A.idx, A.ib, A.rp ? e : e * A.istride);
-            key[e] = uint32_t(c >= 0 && c < A.n ? c : A.n);
-            row[e] = uint32_t(r);
-            if (w) w[e] = load_value(A.val, A.vt, e);
-        }
-    }
+    return max(lo, int64_t(0));
 }
 
 // start[c] = sorted entries of columns before c, c = 0 .. n
@@ -433,18 +465,24 @@ __global__ __launch_bounds__(kBlock) void column_bounds(const uint32_t* __restri
         start[c] = uint32_t(lower_bound_u32(key, 0, nnz, uint64_t(c)));
 }
 
-// Few tokens are sorted in two launches, against three per digit and two more
-// of the radix sort, which for few records is all launches and latency.
+// Up to kFewEntries entries over up to 2^19 columns are sorted in two launches,
+// against three or four per digit and two more of the radix sort, which for so
+// few records is mostly launches and latency (65536 tokens of 131072: 17 us,
+// 65 by digits; 1.57 M weighted CSR entries of 200003: %s).
 // The columns are dealt to at most kSortGroups groups of consecutive columns.
-// First, tiles of 1024 tokens are split by group (stable, padding left out),
-// with every tile's first record of every group; then one workgroup per group
-// takes its records from the tiles in order and sorts them by column.
+// First, tiles of entries are split by group (stable, padding left out), with
+// every tile's first record of every group; then one workgroup per group takes
+// its records from the tiles in order and sorts them by column: rows, or with
+// weights pairs of row and weight.
 constexpr int kSortBlock = 1024;
 constexpr int kSortWaves = kSortBlock / kWave;
 constexpr int kSortBins = 1024;   // columns per group, at most
 constexpr int kSortGroups = 512;
 constexpr int kSortBatch = 4;     // groups of 64 records read at once
-constexpr int64_t kFewTokens = int64_t(1) << 17;
+constexpr int kSortTiles = 1024;  // tiles, at most
+constexpr int kSortItems = 4;     // entries per thread of a tile, past kSmallEntries
+constexpr int64_t kSmallEntries = int64_t(1) << 17;
+constexpr int64_t kFewEntries = int64_t(kSortTiles) * kSortBlock * kSortItems;
 
 // Lanes of the wavefront with a lane's value (of `bits` bits), among those of `in`.
 __device__ inline uint64_t lanes_of(uint32_t x, int bits, bool in) {
@@ -479,39 +517,107 @@ __device__ inline uint32_t places(uint32_t (*hist)[W], int n, uint32_t first, ui
     return at;
 }
 
-template <typename I>
-__global__ __launch_bounds__(kSortBlock) void split_tokens(const I* __restrict__ tok, int64_t stride, int64_t n,
-                                                           int64_t v, int lgbins, int groups, int bits,
-                                                           uint2* __restrict__ rec, uint32_t* __restrict__ first) {
+// Rows of the entries [e0, e1) of a workgroup: the pointers of theirs are
+// searched in LDS where they fit, else in memory (every thread calls find_rows).
+constexpr int kRecordRows = 2048;
+struct RowFinder {
+    int64_t r0, n;
+    const int64_t* ptr;
+    __device__ inline int64_t row(int64_t e) const {
+        if (!ptr) return e;
+        int64_t lo = 0, hi = n - 1;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi + 1) >> 1;
+            if (ptr[mid] <= e)
+                lo = mid;
+            else
+                hi = mid - 1;
+        }
+        return r0 + lo;
+    }
+};
+template <int NT>
+__device__ inline RowFinder find_rows(const Entries& A, int64_t e0, int64_t e1, int64_t* range, int64_t* ptr) {
+    if (!A.rp) return {0, 0, nullptr};
+    __syncthreads();
+    const int w = threadIdx.x / kWave;
+    if (w < 2) {
+        const int64_t r = row_of(A.rp, A.m, w ? e1 - 1 : e0);
+        if (lane_id() == 0) range[w] = r;
+    }
+    __syncthreads();
+    const int64_t r0 = range[0], n = range[1] - r0 + 1;
+    if (n < 1 || n > kRecordRows) return {0, A.m, A.rp};
+    for (int i = threadIdx.x; i < n; i += NT) ptr[i] = A.rp[r0 + i];
+    __syncthreads();
+    return {r0, n, ptr};
+}
+
+template <typename I, int ITEMS>
+__global__ __launch_bounds__(kSortBlock) void split_entries(Entries A, int lgbins, int groups, int bits,
+                                                            uint2* __restrict__ rec, float* __restrict__ recw,
+                                                            uint32_t* __restrict__ first) {
     __shared__ uint32_t hist[kSortWaves][kSortGroups];
     __shared__ uint32_t scratch[kSortWaves];
-    const int w = threadIdx.x / kWave;
+    __shared__ int64_t range[2], ptr[kRecordRows];
+    const int w = threadIdx.x / kWave, l = lane_id();
     for (int i = threadIdx.x; i < kSortWaves * kSortGroups; i += kSortBlock) hist[0][i] = 0;
-    const int64_t e = int64_t(blockIdx.x) * kSortBlock + threadIdx.x;
-    const int64_t t = e < n ? int64_t(tok[e * stride]) : -1;
-    const bool in = t >= 0 && t < v;
-    const uint32_t g = in ? uint32_t(t) >> lgbins : 0;
+    const int64_t base = int64_t(blockIdx.x) * kSortBlock * ITEMS;
+    // a wavefront's entries are consecutive
+    const int64_t e0 = base + int64_t(w) * kWave * ITEMS + l;
+    const I* idx = static_cast<const I*>(A.idx);
+    const int64_t stride = A.rp ? 1 : A.istride;
+    I t[ITEMS];
+    float wv[ITEMS];
+    uint32_t rank[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const int64_t e = e0 + k * kWave;
+        t[k] = e < A.nnz ? idx[e * stride] : I(-1);
+        wv[k] = recw && e < A.nnz ? load_value(A.val, A.vt, e) : 0.f;
+    }
+    const RowFinder rows = find_rows<kSortBlock>(A, base, min(A.nnz, base + kSortBlock * ITEMS), range, ptr);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+        if (t[k] >= A.n) t[k] = -1;
     __syncthreads();
-    const uint64_t same = lanes_of(g, bits, in);
-    const uint32_t rank = __popcll(same & lanemask_lt());
-    if (in && rank == 0) hist[w][g] = __popcll(same);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const bool in = t[k] >= 0;
+        const uint32_t g = in ? uint32_t(t[k]) >> lgbins : 0;
+        const uint64_t same = lanes_of(g, bits, in);
+        const uint32_t lower = __popcll(same & lanemask_lt());
+        rank[k] = hist[w][g] + lower;
+        // (a wavefront's LDS accesses are in order, and only it uses this row)
+        __builtin_amdgcn_wave_barrier();
+        if (in && lower == 0) hist[w][g] += __popcll(same);
+        __builtin_amdgcn_wave_barrier();
+    }
     __syncthreads();
     uint32_t end;
     const uint32_t at = places(hist, groups, 0, scratch, &end);
     uint32_t* f = first + int64_t(blockIdx.x) * (groups + 1);
     if (int(threadIdx.x) < groups) f[threadIdx.x] = at;
     if (threadIdx.x == 0) f[groups] = end;
-    if (in) rec[int64_t(blockIdx.x) * kSortBlock + hist[w][g] + rank] = make_uint2(uint32_t(t), uint32_t(e));
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        if (t[k] < 0) continue;
+        const int64_t e = e0 + k * kWave;
+        const int64_t pos = base + hist[w][uint32_t(t[k]) >> lgbins] + rank[k];
+        rec[pos] = make_uint2(uint32_t(t[k]), uint32_t(rows.row(e)));
+        if (recw) recw[pos] = wv[k];
+    }
 }
 
 __global__ __launch_bounds__(kSortBlock) void sort_groups(const uint2* __restrict__ rec,
-                                                          const uint32_t* __restrict__ first, int tiles, int groups,
-                                                          int lgbins, int64_t v, uint32_t* __restrict__ start,
+                                                          const float* __restrict__ recw,
+                                                          const uint32_t* __restrict__ first, int tiles, int tile,
+                                                          int groups, int lgbins, int64_t v,
+                                                          uint32_t* __restrict__ start, int part,
                                                           uint32_t* __restrict__ key, uint32_t* __restrict__ row) {
-    constexpr int kTiles = int(kFewTokens / kSortBlock);
     __shared__ uint32_t hist[kSortWaves][kSortBins];
     __shared__ uint32_t scratch[kSortWaves];
-    __shared__ uint32_t upto[kTiles + 1], from[kTiles];  // the group's records before each tile, and in the tile
+    __shared__ uint32_t upto[kSortTiles + 1], from[kSortTiles];  // the group's records before each tile, and in it
     const int g = blockIdx.x, bins = 1 << lgbins;
     const int w = threadIdx.x / kWave, l = lane_id();
     for (int i = threadIdx.x; i < kSortWaves * bins; i += kSortBlock) hist[i >> lgbins][i & (bins - 1)] = 0;
@@ -520,18 +626,20 @@ __global__ __launch_bounds__(kSortBlock) void sort_groups(const uint2* __restric
         const uint32_t* f = first + int64_t(threadIdx.x) * (groups + 1) + g;
         before = f[0];
         count = f[1] - before;
-        from[threadIdx.x] = threadIdx.x * kSortBlock + before;
+        from[threadIdx.x] = threadIdx.x * tile + before;
     }
     uint32_t m, all;
     const uint32_t mine = block_exclusive_scan<uint32_t, kSortBlock>(count, scratch, &m);
     (void)block_exclusive_scan<uint32_t, kSortBlock>(before, scratch, &all);
-    if (int(threadIdx.x) <= tiles) upto[threadIdx.x] = int(threadIdx.x) < tiles ? mine : m;
+    upto[threadIdx.x] = mine;  // (m past the tiles)
+    if (threadIdx.x == 0) upto[kSortTiles] = m;
     __syncthreads();
     // records of consecutive stretches, whole groups of 64, one stretch per wavefront
     const uint32_t per = ((m + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
     const uint32_t i0 = w * per, i1 = min(m, i0 + per);
     const uint32_t lo = uint32_t(g) << lgbins;
     uint2 r[kSortBatch];
+    float rw[kSortBatch];
     auto load = [&](uint32_t base) {
 #pragma unroll
         for (int k = 0; k < kSortBatch; ++k) {
@@ -539,7 +647,9 @@ __global__ __launch_bounds__(kSortBlock) void sort_groups(const uint2* __restric
             r[k] = make_uint2(~0u, 0u);
             if (i < i1) {
                 const int q = upper_bound_lds(upto, 0, tiles, i) - 1;
-                r[k] = rec[from[q] + (i - upto[q])];
+                const uint32_t src = from[q] + (i - upto[q]);
+                r[k] = rec[src];
+                if (recw) rw[k] = recw[src];
             }
         }
     };
@@ -564,10 +674,13 @@ __global__ __launch_bounds__(kSortBlock) void sort_groups(const uint2* __restric
             const uint32_t rank = __popcll(same & lanemask_lt());
             if (in) {
                 const uint32_t pos = hist[w][bin] + rank;
-                key[pos] = r[k].x;
-                row[pos] = r[k].y;
+                if (recw)
+                    reinterpret_cast<uint2*>(row)[pos] = make_uint2(r[k].y, __float_as_uint(rw[k]));
+                else
+                    row[pos] = r[k].y;
+                // (the sums ask for the columns of their tiles' first and last entries)
+                if (pos % part == 0 || pos % part == part - 1 || pos == end - 1) key[pos] = r[k].x;
             }
-            // (a wavefront's LDS accesses are in order, and only it uses this row)
             __builtin_amdgcn_wave_barrier();
             if (in && rank == 0) hist[w][bin] += __popcll(same);
             __builtin_amdgcn_wave_barrier();
@@ -575,11 +688,30 @@ __global__ __launch_bounds__(kSortBlock) void sort_groups(const uint2* __restric
     }
 }
 
-// log2 of the columns per group (-1: the tokens go by the radix sort)
-inline int few_tokens_bins(const Entries& A) {
-    if (A.rp || A.m > kFewTokens || A.n > int64_t(kSortBins) * kSortGroups) return -1;
+// Sort records of the radix sort: the column (n for padding, which sorts past
+// every column), the row and the weight of every entry.
+constexpr int kRecords = 2048;
+__global__ __launch_bounds__(kBlock) void sort_records(Entries A, uint32_t* __restrict__ key,
+                                                       uint32_t* __restrict__ row, float* __restrict__ w) {
+    __shared__ int64_t range[2], ptr[kRecordRows];
+    for (int64_t e0 = int64_t(blockIdx.x) * kRecords; e0 < A.nnz; e0 += int64_t(gridDim.x) * kRecords) {
+        const int64_t e1 = min(A.nnz, e0 + kRecords);
+        const RowFinder rows = find_rows<kBlock>(A, e0, e1, range, ptr);
+        for (int64_t e = e0 + threadIdx.x; e < e1; e += kBlock) {
+            const int64_t c = load_column(A.idx, A.ib, A.rp ? e : e * A.istride);
+            key[e] = uint32_t(c >= 0 && c < A.n ? c : A.n);
+            row[e] = uint32_t(rows.row(e));
+            if (w) w[e] = load_value(A.val, A.vt, e);
+        }
+    }
+}
+
+// log2 of the columns per group (-1: the entries go by the radix sort)
+inline int few_entries_bins(const Entries& A) {
+    if (A.nnz > kFewEntries || A.n > int64_t(kSortBins) * kSortGroups) return -1;
     int lg = 0;
-    while ((int64_t(256) << lg) < A.n && (1 << lg) < kSortBins) ++lg;
+    const int64_t groups = A.nnz > kSmallEntries ? kSortGroups : 256;
+    while ((groups << lg) < A.n && (1 << lg) < kSortBins) ++lg;
     return lg;
 }
 
@@ -614,22 +746,30 @@ void embed_tokens(const Entries& A, const DenseRows& W, float scale, const Dense
 size_t embed_csr_tmp_bytes(int64_t nnz, int64_t d) { return part_bytes(nnz, d); }
 
 void embed_csr(const Entries& A, const DenseRows& W, float scale, const DenseRows& Y, void* tmp, hipStream_t s) {
-    Targets<int64_t> t{A.rp, A.m, A.nnz, A.idx, A.ib, A.val, A.vt, nullptr};
+    Targets<int64_t> t{A.rp, A.m, A.nnz, A.idx, A.ib, A.val, A.vt, nullptr, 1};
     grouped_sums(t, W, scale, Y, tmp, s);
 }
 
+// entries per tile of the two-launch sort
+static int sort_tile(int64_t nnz) { return nnz <= kSmallEntries ? kSortBlock : kSortBlock * kSortItems; }
+
 // Scratch of the sort: the radix sort's, or every tile's first records by group.
 static size_t sort_scratch_bytes(const Entries& A) {
-    if (few_tokens_bins(A) < 0) return round256(radix_tmp_bytes(A.nnz));
-    return round256(size_t((A.nnz + kSortBlock - 1) / kSortBlock) * (kSortGroups + 1) * sizeof(uint32_t));
+    if (few_entries_bins(A) < 0) return round256(radix_tmp_bytes(A.nnz));
+    const int tile = sort_tile(A.nnz);
+    return round256(size_t((A.nnz + tile - 1) / tile) * (kSortGroups + 1) * sizeof(uint32_t));
+}
+
+// Bytes of each of the sort's buffers: keys, rows and weights, sorted and
+// before.  (Key and row before the sort hold the split's records, which end at
+// most a tile past the entries.)
+static size_t sort_buffer_bytes(int64_t nnz) {
+    return round256((size_t(nnz) + kSortBlock * kSortItems) * sizeof(uint32_t));
 }
 
 size_t embed_grad_tmp_bytes(const Entries& A, int64_t d) {
-    // keys and rows, sorted and before; the latter are records of both in the
-    // split, which end at most a tile past the entries
-    const size_t words = round256((size_t(A.nnz) + kSortBlock) * sizeof(uint32_t));
-    return words * (A.val ? 6 : 4) + round256(size_t(A.n + 1) * sizeof(uint32_t)) + sort_scratch_bytes(A) +
-           part_bytes(A.nnz, d);
+    return sort_buffer_bytes(A.nnz) * (A.val ? 6 : 4) + round256(size_t(A.n + 1) * sizeof(uint32_t)) +
+           sort_scratch_bytes(A) + part_bytes(A.nnz, d);
 }
 
 void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRows& dW, void* tmp, hipStream_t s) {
@@ -639,40 +779,48 @@ void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRo
         at += round256(bytes);
         return p;
     };
-    const size_t words = (size_t(A.nnz) + kSortBlock) * sizeof(uint32_t);
+    const size_t words = sort_buffer_bytes(A.nnz);
     uint32_t* start = reinterpret_cast<uint32_t*>(take(size_t(A.n + 1) * sizeof(uint32_t)));
     uint32_t *key[2], *row[2];
-    float* w[2] = {nullptr, nullptr};
+    float* w[2];
     for (int i = 0; i < 2; ++i) {
         key[i] = reinterpret_cast<uint32_t*>(take(words));
         row[i] = reinterpret_cast<uint32_t*>(take(words));
-        if (A.val) w[i] = reinterpret_cast<float*>(take(words));
+        w[i] = A.val ? reinterpret_cast<float*>(take(words)) : nullptr;
     }
     void* sort_tmp = take(sort_scratch_bytes(A));
-    int which = 0;
-    const int lgbins = few_tokens_bins(A);
+    int which = 0, step = 1;
+    const int lgbins = few_entries_bins(A);
     if (lgbins >= 0) {
         const int groups = int((A.n + (int64_t(1) << lgbins) - 1) >> lgbins);
-        const int tiles = int((A.nnz + kSortBlock - 1) / kSortBlock);
-        uint2* rec = reinterpret_cast<uint2*>(key[1]);   // (nnz records: two of the sort's buffers)
+        const int tile = sort_tile(A.nnz);
+        const int tiles = int((A.nnz + tile - 1) / tile);
+        const int bits = bit_width_u64(uint64_t(groups - 1));
+        uint2* rec = reinterpret_cast<uint2*>(key[1]);  // (two of the sort's buffers)
         uint32_t* first = static_cast<uint32_t*>(sort_tmp);
+        auto split = [&](auto kernel) {
+            kernel<<<tiles, kSortBlock, 0, s>>>(A, lgbins, groups, bits, rec, w[1], first);
+        };
         if (tiles > 0) {
-            const int bits = bit_width_u64(uint64_t(groups - 1));
-            if (A.ib == 4)
-                split_tokens<int32_t><<<tiles, kSortBlock, 0, s>>>(static_cast<const int32_t*>(A.idx), A.istride, A.nnz,
-                                                                   A.n, lgbins, groups, bits, rec, first);
+            if (tile == kSortBlock)
+                A.ib == 4 ? split(split_entries<int32_t, 1>) : split(split_entries<int64_t, 1>);
             else
-                split_tokens<int64_t><<<tiles, kSortBlock, 0, s>>>(static_cast<const int64_t*>(A.idx), A.istride, A.nnz,
-                                                                   A.n, lgbins, groups, bits, rec, first);
+                A.ib == 4 ? split(split_entries<int32_t, kSortItems>) : split(split_entries<int64_t, kSortItems>);
         }
-        sort_groups<<<groups, kSortBlock, 0, s>>>(rec, first, tiles, groups, lgbins, A.n, start, key[0], row[0]);
+        // (row[0] and w[0] hold the pairs)
+        sort_groups<<<groups, kSortBlock, 0, s>>>(rec, w[1], first, tiles, tile, groups, lgbins, A.n, start,
+                                                  int(sum_tile_entries(A.nnz)), key[0], row[0]);
+        if (A.val) {
+            w[0] = reinterpret_cast<float*>(row[0]) + 1;
+            step = 2;
+        }
     } else if (A.nnz > 0) {
         sort_records<<<unsigned(std::min<int64_t>((A.nnz + kRecords - 1) / kRecords, 1 << 16)), kBlock, 0, s>>>(A, key[0], row[0], w[0]);
         which = radix_sort(key[0], key[1], row[0], row[1], w[0], w[1], A.val ? 4 : 0, A.nnz,
                            bit_width_u64(uint64_t(A.n)), sort_tmp, s);
     }
     if (lgbins < 0) column_bounds<<<thread_grid(A.n + 1), kBlock, 0, s>>>(key[which], A.nnz, A.n, start);
-    Targets<uint32_t> t{start, A.n, A.nnz, row[which], 4, w[which], kDtF32, key[which]};
+    Targets<uint32_t> t{start, A.n, A.nnz, row[which], 4, w[which], kDtF32, key[which], step};
     grouped_sums(t, G, scale, dW, at, s);
 }
 
