@@ -12,7 +12,8 @@
 // 32-bit floats.  The parameters' gradients are summed by the threads that
 // own the columns over the rows of a workgroup, written once per workgroup,
 // and added in the workgroups' order by a second launch, so that results do
-// not depend on timing.  Rows too long for registers are read again instead.
+// not depend on timing; the gradient's workgroups load a row ahead.  Rows too
+// long for registers are read again instead.
 #include <algorithm>
 
 #include "internal.h"
@@ -23,10 +24,10 @@ namespace {
 
 constexpr int kRowBlock = 1024;  // threads per row, at most
 
-// N parameters of type PT at column c (0 where none exist)
-template <typename T, typename PT>
-__device__ inline void load_params(const PT* p, int64_t c, int64_t d, float none, float (&out)[Pack<T>::N]) {
-    constexpr int N = Pack<T>::N, NP = Pack<PT>::N;
+// N parameters of type PT at column c
+template <int N, typename PT>
+__device__ inline void load_params(const PT* p, int c, float none, float (&out)[N]) {
+    constexpr int NP = N * int(sizeof(PT)) > 16 ? 16 / int(sizeof(PT)) : N;
     if (!p) {
 #pragma unroll
         for (int i = 0; i < N; ++i) out[i] = none;
@@ -34,80 +35,85 @@ __device__ inline void load_params(const PT* p, int64_t c, int64_t d, float none
     }
 #pragma unroll
     for (int q = 0; q < N / NP; ++q) {
-        const PackV<PT> v = load_pack(p + c + q * NP, d - c - q * NP);
+        const Vec<PT, NP> v = load_vec<PT, NP>(p + c + q * NP);
 #pragma unroll
         for (int i = 0; i < NP; ++i) out[q * NP + i] = float(v[i]);
     }
 }
 
 // Sum over the TPR threads of a row (a wavefront, or the whole workgroup with
-// buf of TPR / kWave words); every thread gets it.
+// buf of TPR / kWave words, not used again before the next sum's barrier).
 template <int TPR>
 __device__ inline float row_sum(float v, float* buf) {
-    v = wave_reduce_sum(v);
-    if constexpr (TPR == kWave) return v;
-    if (lane_id() == 0) buf[threadIdx.x / kWave] = v;
-    __syncthreads();
-    float s = 0.f;
+    v = wave_total(v);
+    if constexpr (TPR > kWave) {
+        if (lane_id() == 0) buf[threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = 0.f;
 #pragma unroll
-    for (int i = 0; i < TPR / kWave; ++i) s += buf[i];
-    __syncthreads();
-    return s;
+        for (int i = 0; i < TPR / kWave; ++i) v += buf[i];
+    }
+    return v;
 }
 
-template <int TPR>
-constexpr int threads_of() {
-    return TPR == kWave ? kBlock : TPR;
+// The places of a thread's packs.  NP is the row's packs per thread, rounded
+// up, so that only the last one can pass the row's end.
+template <int N, int TPR, int NP>
+__device__ inline void row_places(int l, int64_t d, Place (&at)[NP]) {
+#pragma unroll
+    for (int k = 0; k < NP; ++k) at[k] = place<N>((int64_t(k) * TPR + l) * N, d);
+}
+// whether element i of pack k belongs to this thread alone
+template <int NP>
+__device__ inline bool mine(const Place (&at)[NP], int k, int i) {
+    return k < NP - 1 || i >= at[k].skip;
 }
 
-template <typename T, typename PT, int TPR, int NP>
-__global__ __launch_bounds__(threads_of<TPR>()) void norm_kernel(const T* __restrict__ x, int64_t ldx, int64_t m,
-                                                                 int64_t d, const PT* __restrict__ gamma,
-                                                                 const PT* __restrict__ beta, float eps,
-                                                                 T* __restrict__ y, int64_t ldy,
-                                                                 float* __restrict__ mean, float* __restrict__ rstd) {
-    constexpr int N = Pack<T>::N, ROWS = threads_of<TPR>() / TPR;
-    __shared__ float buf[TPR / kWave];
+template <typename T, typename PT, int N, int TPR, int NP>
+__global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void norm_kernel(
+    const T* __restrict__ x, int64_t ldx, int64_t m, int64_t d, const PT* __restrict__ gamma,
+    const PT* __restrict__ beta, float eps, T* __restrict__ y, int64_t ldy, float* __restrict__ mean,
+    float* __restrict__ rstd) {
+    constexpr int ROWS = TPR < kBlock ? kBlock / TPR : 1;
+    __shared__ float buf[2][2][TPR / kWave];
     const int l = threadIdx.x % TPR;
-    for (int64_t r = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR; r < m; r += int64_t(gridDim.x) * ROWS) {
-        PackV<T> v[NP];
+    int turn = 0;
+    Place at[NP];
+    row_places<N, TPR>(l, d, at);
+    for (int64_t r = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR; r < m;
+         r += int64_t(gridDim.x) * ROWS, turn ^= 1) {
+        Vec<T, N> v[NP];
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            const int64_t c = (int64_t(k) * TPR + l) * N;
-            v[k] = load_pack_nt(x + r * ldx + c, d - c);
-        }
+        for (int k = 0; k < NP; ++k) v[k] = load_vec_nt<T, N>(x + r * ldx + at[k].c);
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < NP; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) s += float(v[k][i]);
-        const float mu = row_sum<TPR>(s, buf) / float(d);
+            for (int i = 0; i < N; ++i) s += mine(at, k, i) ? float(v[k][i]) : 0.f;
+        const float mu = row_sum<TPR>(s, buf[turn][0]) / float(d);
         s = 0.f;
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            const int64_t c = (int64_t(k) * TPR + l) * N;
+        for (int k = 0; k < NP; ++k)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float z = c + i < d ? float(v[k][i]) - mu : 0.f;
+                const float z = mine(at, k, i) ? float(v[k][i]) - mu : 0.f;
                 s = fmaf(z, z, s);
             }
-        }
-        const float rs = 1.f / sqrtf(row_sum<TPR>(s, buf) / float(d) + eps);
+        const float rs = 1.f / sqrtf(row_sum<TPR>(s, buf[turn][1]) / float(d) + eps);
         if (l == 0) {
             mean[r] = mu;
             rstd[r] = rs;
         }
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            const int64_t c = (int64_t(k) * TPR + l) * N;
-            if (c >= d) break;
+            if (at[k].skip >= N) break;
             float g[N], b[N];
-            load_params<T, PT>(gamma, c, d, 1.f, g);
-            load_params<T, PT>(beta, c, d, 0.f, b);
-            PackV<T> o;
+            load_params<N>(gamma, at[k].c, 1.f, g);
+            load_params<N>(beta, at[k].c, 0.f, b);
+            Vec<T, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[i] = T(fmaf((float(v[k][i]) - mu) * rs, g[i], b[i]));
-            store_pack_nt(y + r * ldy + c, o, d - c);
+            store_vec_nt<T, N>(y + r * ldy + at[k].c, o);
         }
     }
 }
@@ -118,128 +124,180 @@ __global__ __launch_bounds__(kRowBlock) void norm_long(const T* __restrict__ x, 
                                                        const PT* __restrict__ gamma, const PT* __restrict__ beta,
                                                        float eps, T* __restrict__ y, int64_t ldy,
                                                        float* __restrict__ mean, float* __restrict__ rstd) {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = 16 / int(sizeof(T));
     constexpr int64_t STEP = int64_t(kRowBlock) * N;
-    __shared__ float buf[kRowBlock / kWave];
-    for (int64_t r = blockIdx.x; r < m; r += gridDim.x) {
+    __shared__ float buf[2][2][kRowBlock / kWave];
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < m; r += gridDim.x, turn ^= 1) {
         const T* xr = x + r * ldx;
         float s = 0.f;
         for (int64_t c = int64_t(threadIdx.x) * N; c < d; c += STEP) {
-            const PackV<T> v = load_pack(xr + c, d - c);
+            const Place at = place<N>(c, d);
+            const Vec<T, N> v = load_vec<T, N>(xr + at.c);
 #pragma unroll
-            for (int i = 0; i < N; ++i) s += float(v[i]);
+            for (int i = 0; i < N; ++i) s += i >= at.skip ? float(v[i]) : 0.f;
         }
-        const float mu = row_sum<kRowBlock>(s, buf) / float(d);
+        const float mu = row_sum<kRowBlock>(s, buf[turn][0]) / float(d);
         s = 0.f;
         for (int64_t c = int64_t(threadIdx.x) * N; c < d; c += STEP) {
-            const PackV<T> v = load_pack(xr + c, d - c);
+            const Place at = place<N>(c, d);
+            const Vec<T, N> v = load_vec<T, N>(xr + at.c);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float z = c + i < d ? float(v[i]) - mu : 0.f;
+                const float z = i >= at.skip ? float(v[i]) - mu : 0.f;
                 s = fmaf(z, z, s);
             }
         }
-        const float rs = 1.f / sqrtf(row_sum<kRowBlock>(s, buf) / float(d) + eps);
+        const float rs = 1.f / sqrtf(row_sum<kRowBlock>(s, buf[turn][1]) / float(d) + eps);
         if (threadIdx.x == 0) {
             mean[r] = mu;
             rstd[r] = rs;
         }
         for (int64_t c = int64_t(threadIdx.x) * N; c < d; c += STEP) {
-            const PackV<T> v = load_pack(xr + c, d - c);
+            const Place at = place<N>(c, d);
+            const Vec<T, N> v = load_vec<T, N>(xr + at.c);
             float g[N], b[N];
-            load_params<T, PT>(gamma, c, d, 1.f, g);
-            load_params<T, PT>(beta, c, d, 0.f, b);
-            PackV<T> o;
+            load_params<N>(gamma, at.c, 1.f, g);
+            load_params<N>(beta, at.c, 0.f, b);
+            Vec<T, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[i] = T(fmaf((float(v[i]) - mu) * rs, g[i], b[i]));
-            store_pack_nt(y + r * ldy + c, o, d - c);
+            store_vec_nt<T, N>(y + r * ldy + at.c, o);
         }
     }
 }
 
 // ---- gradient
 
+// Threads per workgroup: rows of a wavefront share one of eight.
+constexpr int kGradBlock = 512;
+template <int TPR>
+constexpr int grad_threads() {
+    return TPR == kWave ? kGradBlock : TPR;
+}
+
+// a row's packs of x and dy, and its statistics
+template <typename T, int N, int NP>
+struct GradRow {
+    Vec<T, N> x[NP], dy[NP];
+    float mu, rs;
+};
+
 // part: per workgroup the sums of dy h over its rows (d words), then of dy
 // (null: no parameters)
-template <typename T, typename PT, int TPR, int NP>
-__global__ __launch_bounds__(threads_of<TPR>()) void norm_grad_kernel(
+template <typename T, typename PT, int N, int TPR, int NP>
+__global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
     const T* __restrict__ dy, int64_t ldg, const T* __restrict__ x, int64_t ldx, int64_t m, int64_t d,
     const float* __restrict__ mean, const float* __restrict__ rstd, const PT* __restrict__ gamma, T* __restrict__ dx,
     int64_t ldd, float* __restrict__ part) {
-    constexpr int N = Pack<T>::N, ROWS = threads_of<TPR>() / TPR;
-    __shared__ float buf[TPR / kWave];
+    constexpr int ROWS = grad_threads<TPR>() / TPR, WAVES = TPR / kWave;
+    __shared__ float2 buf[2][WAVES];
     const int l = threadIdx.x % TPR;
+    int turn = 0;
+    Place at[NP];
+    row_places<N, TPR>(l, d, at);
     float g[NP][N], dg[NP][N] = {}, db[NP][N] = {};
 #pragma unroll
-    for (int k = 0; k < NP; ++k) load_params<T, PT>(gamma, (int64_t(k) * TPR + l) * N, d, 1.f, g[k]);
-    for (int64_t r = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR; r < m; r += int64_t(gridDim.x) * ROWS) {
-        PackV<T> v[NP], w[NP];
+    for (int k = 0; k < NP; ++k) load_params<N>(gamma, at[k].c, 1.f, g[k]);
+    auto load = [&](int64_t r) {
+        GradRow<T, N, NP> q;
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            const int64_t c = (int64_t(k) * TPR + l) * N;
-            v[k] = load_pack_nt(x + r * ldx + c, d - c);
-            w[k] = load_pack_nt(dy + r * ldg + c, d - c);  // (0 past the row: adds nothing below)
+            q.x[k] = load_vec_nt<T, N>(x + r * ldx + at[k].c);
+            q.dy[k] = load_vec_nt<T, N>(dy + r * ldg + at[k].c);
         }
-        const float mu = mean[r], rs = rstd[r];
+        q.mu = mean[r];
+        q.rs = rstd[r];
+        return q;
+    };
+    const int64_t step = int64_t(gridDim.x) * ROWS;
+    int64_t r = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR;
+    // (a row ahead, but where its registers would spill)
+    constexpr bool AHEAD = TPR < kRowBlock || NP == 1;
+    GradRow<T, N, NP> next;
+    if (AHEAD && r < m) next = load(r);
+    for (; r < m; r += step, turn ^= 1) {
+        const GradRow<T, N, NP> q = AHEAD ? next : load(r);
+        if (AHEAD && r + step < m) next = load(r + step);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int k = 0; k < NP; ++k)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float h = (float(v[k][i]) - mu) * rs, a = float(w[k][i]) * g[k][i];
+                const float w = float(q.dy[k][i]), h = (float(q.x[k][i]) - q.mu) * q.rs;
+                const float a = mine(at, k, i) ? w * g[k][i] : 0.f;
                 s1 += a;
                 s2 = fmaf(a, h, s2);
-                dg[k][i] = fmaf(float(w[k][i]), h, dg[k][i]);
-                db[k][i] += float(w[k][i]);
+                dg[k][i] = fmaf(w, h, dg[k][i]);
+                db[k][i] += w;
             }
-        s1 = row_sum<TPR>(s1, buf) / float(d);
-        s2 = row_sum<TPR>(s2, buf) / float(d);
+        s1 = wave_total(s1);
+        s2 = wave_total(s2);
+        if constexpr (WAVES > 1) {
+            // (two buffers: a wavefront can be one row ahead of another)
+            if (lane_id() == 0) buf[turn][l / kWave] = make_float2(s1, s2);
+            __syncthreads();
+            s1 = s2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                s1 += buf[turn][i].x;
+                s2 += buf[turn][i].y;
+            }
+        }
+        s1 /= float(d);
+        s2 /= float(d);
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            const int64_t c = (int64_t(k) * TPR + l) * N;
-            if (c >= d) break;
-            PackV<T> o;
+            if (at[k].skip >= N) break;
+            Vec<T, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float h = (float(v[k][i]) - mu) * rs;
-                o[i] = T(rs * (float(w[k][i]) * g[k][i] - s1 - h * s2));
+                const float h = (float(q.x[k][i]) - q.mu) * q.rs;
+                o[i] = T(q.rs * (float(q.dy[k][i]) * g[k][i] - s1 - h * s2));
             }
-            store_pack_nt(dx + r * ldd + c, o, d - c);
+            store_vec_nt<T, N>(dx + r * ldd + at[k].c, o);
         }
     }
     if (!part) return;
     float* p = part + int64_t(blockIdx.x) * 2 * d;
-    if constexpr (ROWS == 1) {
+    if constexpr (ROWS > 1) {
+        // the wavefronts' sums, pairwise: the upper half's through LDS to the lower half
+        __shared__ float sum[ROWS / 2][2][NP][N][kWave];
+        const int w = threadIdx.x / kWave;
 #pragma unroll
-        for (int k = 0; k < NP; ++k)
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int64_t c = (int64_t(k) * TPR + l) * N + i;
-                if (c < d) {
-                    p[c] = dg[k][i];
-                    p[d + c] = db[k][i];
-                }
-            }
-    } else {
-        // the wavefronts' sums, added in their order
-        __shared__ float sum[2][TPR * NP * N];
-        for (int q = 0; q < ROWS; ++q) {
-            if (int(threadIdx.x / TPR) == q) {
+        for (int half = ROWS / 2; half > 0; half /= 2) {
+            if (w >= half && w < 2 * half)
 #pragma unroll
                 for (int k = 0; k < NP; ++k)
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const int c = (k * TPR + l) * N + i;
-                        sum[0][c] = dg[k][i] + (q ? sum[0][c] : 0.f);
-                        sum[1][c] = db[k][i] + (q ? sum[1][c] : 0.f);
+                        sum[w - half][0][k][i][l] = dg[k][i];
+                        sum[w - half][1][k][i][l] = db[k][i];
                     }
-            }
+            __syncthreads();
+            if (w < half)
+#pragma unroll
+                for (int k = 0; k < NP; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        dg[k][i] += sum[w][0][k][i][l];
+                        db[k][i] += sum[w][1][k][i][l];
+                    }
             __syncthreads();
         }
-        for (int64_t c = threadIdx.x; c < d; c += threads_of<TPR>()) {
-            p[c] = sum[0][c];
-            p[d + c] = sum[1][c];
+        if (w > 0) return;
+    }
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+        if (at[k].skip >= N) break;
+        Vec<float, N> a, b;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            a[i] = dg[k][i];
+            b[i] = db[k][i];
         }
+        store_vec<float, N>(p + at[k].c, a);
+        store_vec<float, N>(p + d + at[k].c, b);
     }
 }
 
@@ -251,37 +309,40 @@ __global__ __launch_bounds__(kRowBlock) void norm_grad_long(const T* __restrict_
                                                             const float* __restrict__ rstd,
                                                             const PT* __restrict__ gamma, T* __restrict__ dx,
                                                             int64_t ldd) {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = 16 / int(sizeof(T));
     constexpr int64_t STEP = int64_t(kRowBlock) * N;
-    __shared__ float buf[kRowBlock / kWave];
-    for (int64_t r = blockIdx.x; r < m; r += gridDim.x) {
+    __shared__ float buf[2][2][kRowBlock / kWave];
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < m; r += gridDim.x, turn ^= 1) {
         const T *xr = x + r * ldx, *gr = dy + r * ldg;
         const float mu = mean[r], rs = rstd[r];
         float s1 = 0.f, s2 = 0.f;
         for (int64_t c = int64_t(threadIdx.x) * N; c < d; c += STEP) {
-            const PackV<T> v = load_pack(xr + c, d - c), w = load_pack(gr + c, d - c);
+            const Place at = place<N>(c, d);
+            const Vec<T, N> v = load_vec<T, N>(xr + at.c), w = load_vec<T, N>(gr + at.c);
             float g[N];
-            load_params<T, PT>(gamma, c, d, 1.f, g);
+            load_params<N>(gamma, at.c, 1.f, g);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float a = float(w[i]) * g[i];
+                const float a = i >= at.skip ? float(w[i]) * g[i] : 0.f;
                 s1 += a;
                 s2 = fmaf(a, (float(v[i]) - mu) * rs, s2);
             }
         }
-        s1 = row_sum<kRowBlock>(s1, buf) / float(d);
-        s2 = row_sum<kRowBlock>(s2, buf) / float(d);
+        s1 = row_sum<kRowBlock>(s1, buf[turn][0]) / float(d);
+        s2 = row_sum<kRowBlock>(s2, buf[turn][1]) / float(d);
         for (int64_t c = int64_t(threadIdx.x) * N; c < d; c += STEP) {
-            const PackV<T> v = load_pack(xr + c, d - c), w = load_pack(gr + c, d - c);
+            const Place at = place<N>(c, d);
+            const Vec<T, N> v = load_vec<T, N>(xr + at.c), w = load_vec<T, N>(gr + at.c);
             float g[N];
-            load_params<T, PT>(gamma, c, d, 1.f, g);
-            PackV<T> o;
+            load_params<N>(gamma, at.c, 1.f, g);
+            Vec<T, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float h = (float(v[i]) - mu) * rs;
                 o[i] = T(rs * (float(w[i]) * g[i] - s1 - h * s2));
             }
-            store_pack_nt(dx + r * ldd + c, o, d - c);
+            store_vec_nt<T, N>(dx + r * ldd + at.c, o);
         }
     }
 }
@@ -293,13 +354,13 @@ __global__ __launch_bounds__(kBlock) void norm_params_long(const T* __restrict__
                                                            const T* __restrict__ x, int64_t ldx, int64_t m, int64_t d,
                                                            const float* __restrict__ mean,
                                                            const float* __restrict__ rstd, float* __restrict__ part) {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = 16 / int(sizeof(T));
     __shared__ float sum[2][kWave * N];
     const int w = threadIdx.x / kWave, l = lane_id();
-    const int64_t c = (int64_t(blockIdx.x) * kWave + l) * N;
+    const Place at = place<N>((int64_t(blockIdx.x) * kWave + l) * N, d);
     float dg[N] = {}, db[N] = {};
     for (int64_t r = int64_t(blockIdx.y) * kWavesPerBlock + w; r < m; r += int64_t(gridDim.y) * kWavesPerBlock) {
-        const PackV<T> v = load_pack(x + r * ldx + c, d - c), g = load_pack(dy + r * ldg + c, d - c);
+        const Vec<T, N> v = load_vec<T, N>(x + r * ldx + at.c), g = load_vec<T, N>(dy + r * ldg + at.c);
         const float mu = mean[r], rs = rstd[r];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -316,13 +377,12 @@ __global__ __launch_bounds__(kBlock) void norm_params_long(const T* __restrict__
             }
         __syncthreads();
     }
-    float* p = part + int64_t(blockIdx.y) * 2 * d;
-    for (int i = threadIdx.x; i < kWave * N; i += kBlock) {
-        const int64_t cc = int64_t(blockIdx.x) * kWave * N + i;
-        if (cc < d) {
-            p[cc] = sum[0][i];
-            p[d + cc] = sum[1][i];
-        }
+    if (w > 0 || at.skip >= N) return;
+    float* p = part + int64_t(blockIdx.y) * 2 * d + at.c;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        p[i] = sum[0][l * N + i];
+        p[d + i] = sum[1][l * N + i];
     }
 }
 
@@ -333,139 +393,154 @@ template <typename PT>
 __global__ __launch_bounds__(kJoinBlock) void norm_params_join(const float* __restrict__ part, int64_t groups,
                                                                int64_t d, PT* __restrict__ dgamma,
                                                                PT* __restrict__ dbeta) {
-    __shared__ float sum[kJoinBlock / kWave][kWave];
+    constexpr int W = kJoinBlock / kWave;
+    __shared__ float sum[W][kWave];
     PT* out = blockIdx.y ? dbeta : dgamma;
     if (!out) return;
     const int w = threadIdx.x / kWave, l = lane_id();
     for (int64_t c0 = int64_t(blockIdx.x) * kWave; c0 < d; c0 += int64_t(gridDim.x) * kWave) {
         const int64_t c = c0 + l;
         float s = 0.f;
-        if (c < d)
-            for (int64_t q = w; q < groups; q += kJoinBlock / kWave) s += part[(2 * q + blockIdx.y) * d + c];
+        if (c < d) {
+#pragma unroll 8
+            for (int64_t q = w; q < groups; q += W) s += part[(2 * q + blockIdx.y) * d + c];
+        }
         sum[w][l] = s;
         __syncthreads();
         if (w == 0 && c < d) {
             s = 0.f;
 #pragma unroll
-            for (int i = 0; i < kJoinBlock / kWave; ++i) s += sum[i][l];
+            for (int i = 0; i < W; ++i) s += sum[i][l];
             out[c] = PT(s);
         }
         __syncthreads();
     }
 }
 
-// packs held per thread, and threads per row, for rows of `packs` packs
-constexpr int kWavePacks = 2;
-constexpr int64_t kLongGroups = 64;
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// workgroups of the gradient: four per compute unit of 256 threads, fewer of
-// more (each writes 2 d sums)
-inline int64_t grad_groups(int64_t m, int64_t packs) {
-    if (packs <= kWavePacks * kWave) return std::min<int64_t>((m + 3) / 4, 1024);
-    return std::min<int64_t>(m, packs <= 2 * kBlock ? 512 : 256);
+// Packs per row that the gradient's threads hold, at most (registers: two rows
+// of x and dy, gamma and two sums per column): four of four columns per
+// thread, or two of eight.
+template <typename T>
+constexpr int grad_block_packs() {
+    return sizeof(T) == 4 ? 4 : 2;
 }
+inline int64_t packs_of(int64_t d, int dt) { return ceil_div(d * dtype_bytes(dt), 16); }
+inline bool grad_is_long(int64_t packs, int dt) { return packs > int64_t(dt == kDtF32 ? 4 : 2) * kRowBlock; }
 
-template <typename F>
-inline void by_params(int dt, int pt, F f) {
-    by_dtype(dt, [&](auto e) {
-        if (pt == kDtF32)
-            f(e, float());
-        else
-            f(e, e);
-    });
+// Workgroups of the gradient (each writes 2 d sums): 16 wavefronts per
+// compute unit where there are rows enough.
+constexpr int64_t kLongGroups = 64;
+inline int64_t grad_groups(int64_t m, int64_t packs, int dt) {
+    if (grad_is_long(packs, dt)) return kLongGroups;
+    if (packs <= 2 * kWave) return std::min<int64_t>(ceil_div(m, kGradBlock / kWave), 512);
+    return std::min<int64_t>(m, packs <= 2 * kBlock ? 1024 : packs <= 2 * kGradBlock ? 512 : 256);
 }
 
 inline unsigned row_grid(int64_t blocks) { return unsigned(std::min<int64_t>(blocks, int64_t(1) << 20)); }
+
+template <typename F>
+inline void by_params(int dt, int pt, int64_t d, F f) {
+    by_width(dt, d, [&](auto e, auto n) {
+        if (pt == kDtF32)
+            f(e, float(), n);
+        else
+            f(e, e, n);
+    });
+}
+
+// f(threads per row, packs per thread) for a row of `packs` packs, of the
+// combinations (TPR, 1 .. MOST)
+template <int TPR, int MOST, typename F>
+inline void by_packs(int64_t packs, F f) {
+    if (packs <= int64_t(TPR) || MOST == 1)
+        f(std::integral_constant<int, TPR>(), std::integral_constant<int, 1>());
+    else if (packs <= 2 * int64_t(TPR) || MOST == 2)
+        f(std::integral_constant<int, TPR>(), std::integral_constant<int, MOST < 2 ? 1 : 2>());
+    else if (packs <= 3 * int64_t(TPR))
+        f(std::integral_constant<int, TPR>(), std::integral_constant<int, MOST < 3 ? 1 : 3>());
+    else
+        f(std::integral_constant<int, TPR>(), std::integral_constant<int, MOST < 4 ? 1 : 4>());
+}
 
 }  // namespace
 
 void layer_norm(const DenseRows& X, const void* gamma, const void* beta, int pt, float eps, const DenseRows& Y,
                 float* mean, float* rstd, hipStream_t s) {
-    by_params(X.dt, pt, [&](auto e, auto q) {
+    by_params(X.dt, pt, X.n, [&](auto e, auto q, auto n) {
         using T = decltype(e);
         using PT = decltype(q);
-        const int64_t m = X.m, d = X.n, packs = (d + Pack<T>::N - 1) / Pack<T>::N;
+        constexpr int N = decltype(n)::value;
+        const int64_t m = X.m, d = X.n, packs = ceil_div(d, N);
         const T* x = static_cast<const T*>(X.p);
         const PT *g = static_cast<const PT*>(gamma), *b = static_cast<const PT*>(beta);
         T* y = static_cast<T*>(Y.p);
-        if (packs <= kWave)
-            norm_kernel<T, PT, kWave, 1><<<row_grid((m + 3) / 4), kBlock, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld,
-                                                                                  mean, rstd);
-        else if (packs <= 2 * kWave)
-            norm_kernel<T, PT, kWave, 2><<<row_grid((m + 3) / 4), kBlock, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld,
-                                                                                  mean, rstd);
-        else if (packs <= 2 * kBlock)
-            norm_kernel<T, PT, kBlock, 2><<<row_grid(m), kBlock, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld, mean,
-                                                                        rstd);
-        else if (packs <= 4 * kBlock)
-            norm_kernel<T, PT, kBlock, 4><<<row_grid(m), kBlock, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld, mean,
-                                                                        rstd);
-        else if (packs <= 4 * kRowBlock)
-            norm_kernel<T, PT, kRowBlock, 4><<<row_grid(m), kRowBlock, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld,
-                                                                              mean, rstd);
-        else
-            norm_long<T, PT><<<row_grid(m), kRowBlock, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld, mean, rstd);
+        auto launch = [&](auto tpr, auto np) {
+            constexpr int TPR = decltype(tpr)::value, NP = decltype(np)::value;
+            constexpr int NT = TPR < kBlock ? kBlock : TPR;
+            norm_kernel<T, PT, N, TPR, NP><<<row_grid(ceil_div(m, NT / TPR)), NT, 0, s>>>(x, X.ld, m, d, g, b, eps, y,
+                                                                                         Y.ld, mean, rstd);
+        };
+        if constexpr (N == 1) {
+            by_packs<kWave, 1>(packs, launch);
+        } else {
+            if (packs <= 2 * kWave)
+                by_packs<kWave, 2>(packs, launch);
+            else if (packs <= 4 * kBlock)
+                by_packs<kBlock, 4>(packs, launch);
+            else if (packs <= 4 * kRowBlock)
+                by_packs<kRowBlock, 4>(packs, launch);
+            else
+                norm_long<T, PT><<<row_grid(m), kRowBlock, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld, mean, rstd);
+        }
     });
 }
 
-namespace {
-// rows whose packs the gradient's threads hold, at most (registers: the row of
-// x and of dy, gamma and two sums per column)
-template <typename T>
-constexpr int grad_block_packs() {
-    return sizeof(T) == 4 ? 4 : 2;
-}
-inline int64_t grad_most_packs(int dt) { return int64_t(dt == kDtF32 ? 4 : 2) * kRowBlock; }
-inline int64_t packs_of(int64_t d, int dt) { return (d * dtype_bytes(dt) + 15) / 16; }
-}  // namespace
-
 size_t layer_norm_grad_tmp_bytes(int64_t m, int64_t d, int dt, bool params) {
-    if (!params) return 0;
-    const int64_t packs = packs_of(d, dt);
-    const int64_t groups = packs > grad_most_packs(dt) ? kLongGroups : grad_groups(m, packs);
-    return size_t(groups) * 2 * size_t(d) * sizeof(float);
+    return params ? size_t(grad_groups(m, packs_of(d, dt), dt)) * 2 * size_t(d) * sizeof(float) : 0;
 }
 
 void layer_norm_grad(const DenseRows& G, const DenseRows& X, const float* mean, const float* rstd, const void* gamma,
                      int pt, const DenseRows& dX, void* dgamma, void* dbeta, void* tmp, hipStream_t s) {
-    by_params(X.dt, pt, [&](auto e, auto q) {
+    const int64_t groups = X.m ? grad_groups(X.m, packs_of(X.n, X.dt), X.dt) : 0;
+    by_params(X.dt, pt, X.n, [&](auto e, auto q, auto n) {
         using T = decltype(e);
         using PT = decltype(q);
-        constexpr int BP = grad_block_packs<T>();
-        const int64_t m = X.m, d = X.n, packs = packs_of(d, X.dt);
+        constexpr int N = decltype(n)::value;
+        const int64_t m = X.m, d = X.n, packs = ceil_div(d, N);
         const T *x = static_cast<const T*>(X.p), *dy = static_cast<const T*>(G.p);
         const PT* g = static_cast<const PT*>(gamma);
         T* dx = static_cast<T*>(dX.p);
         float* part = dgamma || dbeta ? static_cast<float*>(tmp) : nullptr;
-        int64_t groups = grad_groups(m, packs);
-        const unsigned nb = unsigned(groups);
-        if (m == 0)
-            ;  // (the parameters' gradients are zeros)
-        else if (packs <= kWave)
-            norm_grad_kernel<T, PT, kWave, 1><<<nb, kBlock, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx, dX.ld,
-                                                                    part);
-        else if (packs <= kWavePacks * kWave)
-            norm_grad_kernel<T, PT, kWave, kWavePacks><<<nb, kBlock, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g,
-                                                                             dx, dX.ld, part);
-        else if (packs <= 2 * kBlock)
-            norm_grad_kernel<T, PT, kBlock, 2><<<nb, kBlock, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx,
-                                                                     dX.ld, part);
-        else if (packs <= 2 * 512)
-            norm_grad_kernel<T, PT, 512, 2><<<nb, 512, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx, dX.ld,
-                                                               part);
-        else if (packs <= BP * kRowBlock)
-            norm_grad_kernel<T, PT, kRowBlock, BP><<<nb, kRowBlock, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g,
-                                                                            dx, dX.ld, part);
-        else {
-            norm_grad_long<T, PT><<<row_grid(m), kRowBlock, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx,
-                                                                    dX.ld);
-            groups = kLongGroups;
-            if (part)
-                norm_params_long<T><<<dim3(unsigned((packs + kWave - 1) / kWave), unsigned(groups)), kBlock, 0, s>>>(
-                    dy, G.ld, x, X.ld, m, d, mean, rstd, part);
+        auto launch = [&](auto tpr, auto np) {
+            constexpr int TPR = decltype(tpr)::value, NP = decltype(np)::value;
+            norm_grad_kernel<T, PT, N, TPR, NP><<<unsigned(groups), grad_threads<TPR>(), 0, s>>>(
+                dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx, dX.ld, part);
+        };
+        if (m > 0) {
+            if constexpr (N == 1) {
+                by_packs<kWave, 1>(packs, launch);
+            } else {
+                if (packs <= 2 * kWave) {
+                    by_packs<kWave, 2>(packs, launch);
+                } else if (packs <= 2 * kBlock) {
+                    by_packs<kBlock, 2>(packs, launch);
+                } else if (packs <= 2 * kGradBlock) {
+                    launch(std::integral_constant<int, kGradBlock>(), std::integral_constant<int, 2>());
+                } else if (!grad_is_long(packs, X.dt)) {
+                    by_packs<kRowBlock, grad_block_packs<T>()>(packs, launch);
+                } else {
+                    norm_grad_long<T, PT><<<row_grid(m), kRowBlock, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx,
+                                                                            dX.ld);
+                    if (part)
+                        norm_params_long<T><<<dim3(unsigned(ceil_div(packs, kWave)), unsigned(groups)), kBlock, 0, s>>>(
+                            dy, G.ld, x, X.ld, m, d, mean, rstd, part);
+                }
+            }
         }
-        if (dgamma || dbeta)
-            norm_params_join<PT><<<dim3(row_grid((d + kWave - 1) / kWave), 2), kJoinBlock, 0, s>>>(
+        if (dgamma || dbeta)  // (of no rows: zeros)
+            norm_params_join<PT><<<dim3(row_grid(ceil_div(d, kWave)), 2), kJoinBlock, 0, s>>>(
                 part, groups, d, static_cast<PT*>(dgamma), static_cast<PT*>(dbeta));
     });
 }

@@ -127,6 +127,25 @@ __device__ inline void store_vec_nt(T* p, Vec<T, N> v) {
     __builtin_nontemporal_store(v, reinterpret_cast<Vec<T, N>*>(p));
 }
 
+// Sum over the wavefront, in every lane: four steps within rows of 16 lanes
+// and two across them, each one instruction (a shuffle through LDS takes far
+// longer, and sums like these stand between a row's loads and its stores).
+__device__ inline float wave_total(float v) {
+    auto add = [&](auto ctrl, auto rows) {
+        const int o = __builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, decltype(rows)::value,
+                                                  0xf, false);
+        v += __int_as_float(o);
+    };
+    using std::integral_constant;
+    add(integral_constant<int, 0x111>(), integral_constant<int, 0xf>());  // from 1 lane below
+    add(integral_constant<int, 0x112>(), integral_constant<int, 0xf>());  // 2
+    add(integral_constant<int, 0x114>(), integral_constant<int, 0xf>());  // 4
+    add(integral_constant<int, 0x118>(), integral_constant<int, 0xf>());  // 8: lane 15 of a row has its sum
+    add(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());  // to rows 1 and 3 from the row before
+    add(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());  // to rows 2 and 3 from row 1
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
+}
+
 // f(element, width): the pack width for rows of d columns
 template <typename F>
 inline void by_width(int dt, int64_t d, F f) {
