@@ -434,7 +434,7 @@ inline bool grad_is_long(int64_t packs, int dt) { return packs > int64_t(dt == k
 constexpr int64_t kLongGroups = 64;
 inline int64_t grad_groups(int64_t m, int64_t packs, int dt) {
     if (grad_is_long(packs, dt)) return kLongGroups;
-    if (packs <= 2 * kWave) return std::min<int64_t>(ceil_div(m, kGradBlock / kWave), 512);
+    if (packs <= 2 * kWave) return std::min<int64_t>(ceil_div(m, kGradBlock / kWave), 256);
     return std::min<int64_t>(m, packs <= 2 * kBlock ? 1024 : packs <= 2 * kGradBlock ? 512 : 256);
 }
 

@@ -146,6 +146,31 @@ __device__ inline float wave_total(float v) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
 }
 
+// Maximum over the wavefront, in every lane (NaN is passed over).
+__device__ inline float wave_max(float v) {
+    auto step = [&](auto ctrl, auto rows) {
+        const int o = __builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), decltype(ctrl)::value,
+                                                  decltype(rows)::value, 0xf, false);
+        v = fmaxf(v, __int_as_float(o));
+    };
+    using std::integral_constant;
+    step(integral_constant<int, 0x111>(), integral_constant<int, 0xf>());
+    step(integral_constant<int, 0x112>(), integral_constant<int, 0xf>());
+    step(integral_constant<int, 0x114>(), integral_constant<int, 0xf>());
+    step(integral_constant<int, 0x118>(), integral_constant<int, 0xf>());
+    step(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());
+    step(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
+}
+
+// A workgroup's barrier for what it exchanges through LDS: unlike
+// __syncthreads it orders no access to memory, so loads in flight stay so.
+__device__ inline void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // f(element, width): the pack width for rows of d columns
 template <typename F>
 inline void by_width(int dt, int64_t d, F f) {

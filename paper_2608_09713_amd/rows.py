@@ -12,6 +12,8 @@ own.
 from __future__ import annotations
 
 import ctypes
+import functools
+import threading
 
 import torch
 
@@ -22,7 +24,7 @@ _byref = ctypes.byref
 
 
 def _rows(t, name):
-    """(_Dense of the tensor's rows, number of rows); the last dimension is the columns."""
+    """_Dense of the tensor's rows; the last dimension is the columns."""
     dt = _DTYPE.get(t.dtype)
     if dt is None:
         raise TypeError(f"{name} must be float32, float16 or bfloat16, not {t.dtype}")
@@ -41,6 +43,11 @@ def _rows(t, name):
     if v is None or v.stride(1) != 1 or (v.shape[0] > 1 and v.stride(0) < cols):
         raise ValueError(f"{name} must have rows of contiguous elements at one stride")
     return _sp._Dense(v.shape[0], cols, max(v.stride(0), cols), dt, v.data_ptr())
+
+
+def _like(t):
+    """A contiguous tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def _vector(t, name, n, dtypes, device):
@@ -99,30 +106,52 @@ def _tokens(t, ncols, name):
     return _sp._Entries(n, ncols, 0, None, 1, stride, 0, t.data_ptr(), t.element_size(), 0, None)
 
 
-def _run(fn, device, args, workspace):
-    """Call fn(*args) on the device's current stream; args may hold _STREAM and _ALLOC."""
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _run(fn, device, args, workspace)
-    arena = _sp._TorchArena(device) if workspace else None
-    stream = torch.cuda.current_stream(device).cuda_stream
-    rc = fn(*[stream if a is _STREAM else (_byref(arena.struct) if arena else None) if a is _ALLOC else a
-              for a in args])
+_local = threading.local()
+_raw_stream = torch._C._cuda_getCurrentRawStream  # (the handle alone: a Stream object costs 2 us of a call)
+
+
+def _arena(device):
+    """This thread's allocator for the device (its callbacks are made once; it
+    holds nothing between calls)."""
+    arenas = getattr(_local, "arenas", None)
+    if arenas is None:
+        arenas = _local.arenas = {}
+    arena = arenas.get(device)
+    if arena is None:
+        arena = arenas[device] = _sp._TorchArena(device)
+    return arena
+
+
+def _on_device(position, name):
+    """Decorator: the device of the named dense argument is the current one
+    during the call."""
+    def decorate(fn):
+        @functools.wraps(fn)
+        def call(*args, **kwargs):
+            t = args[position] if len(args) > position else kwargs.get(name)
+            if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+                with torch.cuda.device(t.device):
+                    return fn(*args, **kwargs)
+            return fn(*args, **kwargs)
+        return call
+    return decorate
+
+
+def _check(rc, arena=None):
     if rc != 0:
         raise _sp.SpsyrkError(rc, _sp.library().spsyrk_last_error_detail().decode())
-    if arena and arena.live:
+    if arena is not None and arena.live:
+        arena.live.clear()
         raise RuntimeError("library left allocations unreleased")
 
 
-_STREAM, _ALLOC = object(), object()
-
-
+@_on_device(1, "weight")
 def embed(rows, weight, scale=1.0):
     """Rows of the table ``weight`` (v x d): ``scale`` times ``weight[token]`` for
     a tensor of tokens (shape + (d,); zeros for tokens outside [0, v), which are
     padding), or ``scale * A @ weight`` for a DeviceCSR (m x d; its values, or
     ones, weight the entries)  (spsyrk_embed)."""
-    lib = _sp.library()
+    lib = _sp._lib or _sp.library()
     w = _rows(weight, "weight")
     if weight.dim() != 2:
         raise ValueError("weight must be v x d")
@@ -134,15 +163,18 @@ def embed(rows, weight, scale=1.0):
         _same_device(weight.device, rows.row_ptr, "rows")
     out = torch.empty((*shape, w.ncols), dtype=weight.dtype, device=weight.device)
     y = _sp._Dense(a.nrows, w.ncols, w.ncols, w.dtype, out.data_ptr())
-    _run(lib.spsyrk_embed, weight.device, (_byref(a), _byref(w), scale, _ALLOC, _STREAM, _byref(y)), csr)
+    arena = _arena(weight.device) if csr else None
+    _check(lib.spsyrk_embed(_byref(a), _byref(w), scale, _byref(arena.struct) if csr else None,
+                            _raw_stream(weight.device.index), _byref(y)), arena)
     return out
 
 
+@_on_device(1, "grad")
 def embed_grad(rows, grad, v, scale=1.0):
     """The gradient (v x d) of the table looked up by ``embed(rows, weight,
     scale)`` for the gradient ``grad`` of its result: ``scale * A.T @ grad``,
     summed by entries sorted by column (spsyrk_embed_grad)."""
-    lib = _sp.library()
+    lib = _sp._lib or _sp.library()
     g = _rows(grad, "grad")
     if isinstance(rows, torch.Tensor):
         a, first = _tokens(rows, v, "rows"), rows
@@ -151,7 +183,9 @@ def embed_grad(rows, grad, v, scale=1.0):
     _same_device(grad.device, first, "rows")
     out = torch.empty((v, g.ncols), dtype=grad.dtype, device=grad.device)
     w = _sp._Dense(v, g.ncols, g.ncols, g.dtype, out.data_ptr())
-    _run(lib.spsyrk_embed_grad, grad.device, (_byref(a), _byref(g), scale, _ALLOC, _STREAM, _byref(w)), True)
+    arena = _arena(grad.device)
+    _check(lib.spsyrk_embed_grad(_byref(a), _byref(g), scale, _byref(arena.struct), _raw_stream(grad.device.index),
+                                 _byref(w)), arena)
     return out
 
 
@@ -161,45 +195,48 @@ def _params(x, d, weight, bias, what):
     pt = x.dtype if first is None else first.dtype
     if pt not in (torch.float32, x.dtype):
         raise TypeError(f"{what}: weight and bias must be float32 or {x.dtype}, not {pt}")
-    return (_DTYPE[pt], _vector(weight, "weight", d, (pt,), x.device), _vector(bias, "bias", d, (pt,), x.device), pt)
+    return (_DTYPE[pt], _vector(weight, "weight", d, (pt,), x.device), _vector(bias, "bias", d, (pt,), x.device))
 
 
+@_on_device(0, "x")
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """(y, mean, rstd): y = (x - mean) rstd weight + bias over the last dimension,
     with the rows' mean and 1 / sqrt(var + eps) as float32 (spsyrk_layer_norm).
     ``weight`` and ``bias``: float32 or x's type, None for ones and zeros."""
-    lib = _sp.library()
+    lib = _sp._lib or _sp.library()
     a = _rows(x, "x")
-    pt, wp, bp, _ = _params(x, a.ncols, weight, bias, "layer_norm")
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    pt, wp, bp = _params(x, a.ncols, weight, bias, "layer_norm")
+    y = _like(x)
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
     o = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, y.data_ptr())
-    _run(lib.spsyrk_layer_norm, x.device,
-         (_byref(a), wp, bp, pt, eps, _STREAM, _byref(o), mean.data_ptr(), rstd.data_ptr()), False)
+    _check(lib.spsyrk_layer_norm(_byref(a), wp, bp, pt, eps, _raw_stream(x.device.index), _byref(o),
+                                 mean.data_ptr(), rstd.data_ptr()))
     return y, mean, rstd
 
 
+@_on_device(0, "grad")
 def layer_norm_grad(grad, x, mean, rstd, weight=None, bias=None):
     """(dx, dweight, dbias) of ``layer_norm(x, weight, bias)`` for the gradient
     ``grad`` of y; dweight and dbias have the parameters' type and are None for
     a parameter that is None (spsyrk_layer_norm_grad)."""
-    lib = _sp.library()
+    lib = _sp._lib or _sp.library()
     g, a = _rows(grad, "grad"), _rows(x, "x")
     if grad.shape != x.shape:
         raise ValueError("grad and x must have one shape")
     _same_device(x.device, grad, "grad")
-    pt, wp, _, pdt = _params(x, a.ncols, weight, bias, "layer_norm_grad")
+    pt, wp, _ = _params(x, a.ncols, weight, bias, "layer_norm_grad")
     mp = _vector(mean, "mean", a.nrows, (torch.float32,), x.device)
     rp = _vector(rstd, "rstd", a.nrows, (torch.float32,), x.device)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw = None if weight is None else torch.empty(weight.shape, dtype=pdt, device=x.device)
-    db = None if bias is None else torch.empty(bias.shape, dtype=pdt, device=x.device)
+    dx = _like(x)
+    dw = None if weight is None else torch.empty_like(weight)
+    db = None if bias is None else torch.empty_like(bias)
     o = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, dx.data_ptr())
-    _run(lib.spsyrk_layer_norm_grad, x.device,
-         (_byref(g), _byref(a), mp, rp, wp, pt, _ALLOC, _STREAM, _byref(o),
-          None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()),
-         dw is not None or db is not None)
+    arena = _arena(x.device)
+    _check(lib.spsyrk_layer_norm_grad(_byref(g), _byref(a), mp, rp, wp, pt, _byref(arena.struct),
+                                      _raw_stream(x.device.index), _byref(o),
+                                      None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()),
+           arena)
     return dx, dw, db
 
 
@@ -227,32 +264,36 @@ def _teacher(teacher, s, logits):
                         v.dtype, values.data_ptr())
 
 
+@_on_device(0, "logits")
 def distill(logits, teacher, temperature=1.0):
     """Loss (float32, one per row of ``logits``) of distilling the teacher's
     stored entries: temperature^2 times the divergence of the logits' softmax
     from the teacher's softmax over the row's entries (spsyrk_distill).
     ``teacher``: a DeviceCSR over the logits' columns, or a tuple (values,
     indices) as torch.topk returns; indices outside the columns are padding."""
-    lib = _sp.library()
+    lib = _sp._lib or _sp.library()
     s = _rows(logits, "logits")
     t = _teacher(teacher, s, logits)
     loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
-    _run(lib.spsyrk_distill, logits.device,
-         (_byref(s), _byref(t), temperature, _ALLOC, _STREAM, loss.data_ptr()), True)
+    arena = _arena(logits.device)
+    _check(lib.spsyrk_distill(_byref(s), _byref(t), temperature, _byref(arena.struct),
+                              _raw_stream(logits.device.index), loss.data_ptr()), arena)
     return loss
 
 
+@_on_device(0, "logits")
 def distill_grad(logits, teacher, temperature=1.0, weight=None):
     """(loss, gradient): ``distill`` together with the gradient, of the logits'
     type, of ``(weight * loss).sum()`` (``weight``: float32, one per row; None
     for ones)  (spsyrk_distill_grad)."""
-    lib = _sp.library()
+    lib = _sp._lib or _sp.library()
     s = _rows(logits, "logits")
     t = _teacher(teacher, s, logits)
     wp = _vector(weight, "weight", s.nrows, (torch.float32,), logits.device)
     loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
-    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    grad = _like(logits)
     g = _sp._Dense(s.nrows, s.ncols, s.ncols, s.dtype, grad.data_ptr())
-    _run(lib.spsyrk_distill_grad, logits.device,
-         (_byref(s), _byref(t), temperature, wp, _ALLOC, _STREAM, loss.data_ptr(), _byref(g)), True)
+    arena = _arena(logits.device)
+    _check(lib.spsyrk_distill_grad(_byref(s), _byref(t), temperature, wp, _byref(arena.struct),
+                                   _raw_stream(logits.device.index), loss.data_ptr(), _byref(g)), arena)
     return loss, grad
