@@ -2182,7 +2182,7 @@ void distill_call(const spsyrk_dense* S, const spsyrk_entries* teacher, float te
     check_aligned(loss, sizeof(float), "loss");
     if (weight) check_aligned(weight, sizeof(float), "weight");
     const bool grad = dS && x.n > 0;
-    const size_t bytes = distill_tmp_bytes(x.m, x.n, x.dt, grad);
+    const size_t bytes = distill_tmp_bytes(x, grad);
     void* tmp = bytes ? ar.get(bytes) : nullptr;
     distill(x, t, temperature, weight, loss, grad ? g : DenseRows(), tmp, s);
     check_launch();

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(kBlock) void tokens_kernel(Entries A, const T* __re
         T* dst = Y + row * ldy;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            if (at[k].skip >= N) break;
+            if (at[k].shift >= N) break;
             Vec<T, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[i] = T(float(v[k][i]) * scale);
@@ -207,7 +207,7 @@ __device__ inline void sum_tile(const Sums<T, P>& a, int64_t q, int64_t chunk, i
         float* dst = a.part + (2 * q + z) * a.dp;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            if (at[k].skip >= N) break;
+            if (at[k].shift >= N) break;
             Vec<float, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[i] = acc[k][i];
@@ -236,7 +236,7 @@ __device__ inline void sum_run(const Sums<T, P>& a, int64_t t0, int j, int r, in
                 o[i] = T(acc[k][i] * a.scale);
                 acc[k][i] = 0.f;
             }
-            if (at[k].skip < N) store_vec_nt<T, N>(dst + at[k].c, o);
+            if (at[k].shift < N) store_vec_nt<T, N>(dst + at[k].c, o);
         }
         ++j;
         if (j < r) next = start(j + 1);

@@ -65,8 +65,8 @@ __device__ inline void row_places(int l, int64_t d, Place (&at)[NP]) {
 }
 // whether element i of pack k belongs to this thread alone
 template <int NP>
-__device__ inline bool mine(const Place (&at)[NP], int k, int i) {
-    return k < NP - 1 || i >= at[k].skip;
+__device__ inline bool own(const Place (&at)[NP], int k, int i) {
+    return k < NP - 1 || i >= at[k].shift;
 }
 
 template <typename T, typename PT, int N, int TPR, int NP>
@@ -89,14 +89,14 @@ __global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void norm_kernel(
 #pragma unroll
         for (int k = 0; k < NP; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) s += mine(at, k, i) ? float(v[k][i]) : 0.f;
+            for (int i = 0; i < N; ++i) s += own(at, k, i) ? float(v[k][i]) : 0.f;
         const float mu = row_sum<TPR>(s, buf[turn][0]) / float(d);
         s = 0.f;
 #pragma unroll
         for (int k = 0; k < NP; ++k)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float z = mine(at, k, i) ? float(v[k][i]) - mu : 0.f;
+                const float z = own(at, k, i) ? float(v[k][i]) - mu : 0.f;
                 s = fmaf(z, z, s);
             }
         const float rs = 1.f / sqrtf(row_sum<TPR>(s, buf[turn][1]) / float(d) + eps);
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void norm_kernel(
         }
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            if (at[k].skip >= N) break;
+            if (at[k].shift >= N) break;
             float g[N], b[N];
             load_params<N>(gamma, at[k].c, 1.f, g);
             load_params<N>(beta, at[k].c, 0.f, b);
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(kRowBlock) void norm_long(const T* __restrict__ x, 
             const Place at = place<N>(c, d);
             const Vec<T, N> v = load_vec<T, N>(xr + at.c);
 #pragma unroll
-            for (int i = 0; i < N; ++i) s += i >= at.skip ? float(v[i]) : 0.f;
+            for (int i = 0; i < N; ++i) s += i >= at.shift ? float(v[i]) : 0.f;
         }
         const float mu = row_sum<kRowBlock>(s, buf[turn][0]) / float(d);
         s = 0.f;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kRowBlock) void norm_long(const T* __restrict__ x, 
             const Vec<T, N> v = load_vec<T, N>(xr + at.c);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float z = i >= at.skip ? float(v[i]) - mu : 0.f;
+                const float z = i >= at.shift ? float(v[i]) - mu : 0.f;
                 s = fmaf(z, z, s);
             }
         }
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float w = float(q.dy[k][i]), h = (float(q.x[k][i]) - q.mu) * q.rs;
-                const float a = mine(at, k, i) ? w * g[k][i] : 0.f;
+                const float a = own(at, k, i) ? w * g[k][i] : 0.f;
                 s1 += a;
                 s2 = fmaf(a, h, s2);
                 dg[k][i] = fmaf(w, h, dg[k][i]);
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
         s2 /= float(d);
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            if (at[k].skip >= N) break;
+            if (at[k].shift >= N) break;
             Vec<T, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
     }
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-        if (at[k].skip >= N) break;
+        if (at[k].shift >= N) break;
         Vec<float, N> a, b;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -324,7 +324,7 @@ __global__ __launch_bounds__(kRowBlock) void norm_grad_long(const T* __restrict_
             load_params<N>(gamma, at.c, 1.f, g);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float a = i >= at.skip ? float(w[i]) * g[i] : 0.f;
+                const float a = i >= at.shift ? float(w[i]) * g[i] : 0.f;
                 s1 += a;
                 s2 = fmaf(a, (float(v[i]) - mu) * rs, s2);
             }
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(kBlock) void norm_params_long(const T* __restrict__
             }
         __syncthreads();
     }
-    if (w > 0 || at.skip >= N) return;
+    if (w > 0 || at.shift >= N) return;
     float* p = part + int64_t(blockIdx.y) * 2 * d + at.c;
 #pragma unroll
     for (int i = 0; i < N; ++i) {

@@ -98,17 +98,32 @@ struct VecOf {
 template <typename T, int N>
 using Vec = typename VecOf<T, N>::V;
 
-// Where the N elements from column c on are taken in a row of d >= N columns:
-// a pack that would pass the row's end is moved back onto its last N columns.
-// Its first `skip` elements then belong to other packs too (all N if c >= d):
-// maps may write them twice, with one value; sums leave them out.
+// Where the N elements from column c on (c > -N) are taken in a row of d >= N
+// columns: a pack that would pass one of the row's ends is moved back into it.
+// Only those elements i with mine(shift, i) are then the pack's own, the others
+// belong to the next or the last pack too (none is if c >= d: shift >= N).
+// Maps may write them twice, with one value; sums leave them out.
 struct Place {
-    int c, skip;
+    int c, shift;
 };
 template <int N>
 __device__ inline Place place(int64_t c, int64_t d) {
-    const int64_t at = min(c, d - N);
+    const int64_t at = max(min(c, d - N), int64_t(0));
     return {int(at), int(min(c - at, int64_t(N)))};
+}
+template <int N>
+__device__ inline bool mine(int shift, int i) {
+    return uint32_t(i - shift) < uint32_t(N);
+}
+// Elements between the last 16-byte boundary and p.  Packs that start so many
+// columns before a row lie on boundaries: 16 bytes off them, and worst off
+// those of 4 bytes, cost up to half of a stream's rate.
+template <typename T, int N>
+__device__ inline int misaligned(const T* p) {
+    return N == 1 ? 0 : int(reinterpret_cast<uintptr_t>(p) % 16 / sizeof(T));
+}
+inline bool on_boundaries(const void* p, int64_t ld, int dt) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * dtype_bytes(dt) % 16 == 0;
 }
 template <typename T, int N>
 __device__ inline Vec<T, N> load_vec(const T* p) {
@@ -233,7 +248,7 @@ void layer_norm_grad(const DenseRows& G, const DenseRows& X, const float* mean, 
 
 // ---- distill.hip
 // loss of every row; with dS.p its gradient too, times weight (null: 1)
-size_t distill_tmp_bytes(int64_t m, int64_t v, int dt, bool grad);
+size_t distill_tmp_bytes(const DenseRows& S, bool grad);
 void distill(const DenseRows& S, const Entries& teacher, float temperature, const float* weight, float* loss,
              const DenseRows& dS, void* tmp, hipStream_t s);
 
