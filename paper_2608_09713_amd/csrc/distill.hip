@@ -178,32 +178,34 @@ __device__ inline RowEntries row_entries(const Entries& t, int64_t r) {
 // One term of the loss, in units of log 2.
 __device__ inline float loss_term(float p, float lp, float lq) { return p == 0.f ? 0.f : p * (lp - lq); }
 
-// The block's sums over the teacher's entries: all of them, strided.
-__device__ inline MaxSum teacher_sums(const Entries& t, const RowEntries& e, int64_t V, float c) {
-    MaxSum b = kNothing;
-    for (int64_t k = threadIdx.x; k < e.n; k += blockDim.x) {
+// The threads' parts of the sums over the teacher's entries, and of the loss:
+// every blockDim.x-th entry from the k-th on.
+__device__ inline void teacher_sums(MaxSum& b, const Entries& t, const RowEntries& e, int64_t k, int64_t V, float c) {
+    for (; k < e.n; k += blockDim.x) {
         const int64_t col = load_column(t.idx, t.ib, e.i0 + k);
         if (col >= 0 && col < V) add_value(b, load_value(t.val, t.vt, e.v0 + k), c);
     }
-    return b;
 }
 template <typename T>
-__device__ inline float teacher_loss(const Entries& t, const RowEntries& e, const T* row, int64_t V, float c,
-                                     const RowStat& st) {
-    float x = 0.f;
-    for (int64_t k = threadIdx.x; k < e.n; k += blockDim.x) {
+__device__ inline void teacher_loss(float& x, const Entries& t, const RowEntries& e, int64_t k, const T* row,
+                                    int64_t V, float c, const RowStat& st) {
+    for (; k < e.n; k += blockDim.x) {
         const int64_t col = load_column(t.idx, t.ib, e.i0 + k);
         if (col < 0 || col >= V) continue;
         const float lp = (load_value(t.val, t.vt, e.v0 + k) - st.tm) * c - st.tl2;
         x += loss_term(exp2_of(lp), lp, st.log2q(float(row[col]), c));
     }
-    return x;
 }
 
 // Loss of a row and what its gradient needs.
 constexpr int kAhead = 4;  // packs per thread in flight
-template <typename T, int N>
-__global__ __launch_bounds__(kRowBlock) void distill_rows(const T* __restrict__ S, int64_t lds, int64_t m, int64_t V,
+//
+// MOST: the threads of a row, at most.  Rows of more than 512 keep to 64
+// registers, so that two of them are on a compute unit (8192 x 65537 f32: 318
+// us, 370 without); for the others that would only spill (16384 x 32768 bf16:
+// 168 us, 204 so).
+template <typename T, int N, int MOST>
+__global__ __launch_bounds__(MOST, MOST > 512 ? 8 : 1) void distill_rows(const T* __restrict__ S, int64_t lds, int64_t m, int64_t V,
                                                           Entries t, float temp, const float* __restrict__ weight,
                                                           float* __restrict__ loss, RowStat* __restrict__ stat) {
     __shared__ MaxSum ms[2][kMostWaves];
@@ -214,26 +216,49 @@ __global__ __launch_bounds__(kRowBlock) void distill_rows(const T* __restrict__ 
     for (int64_t r = blockIdx.x; r < m; r += gridDim.x) {
         const T* row = S + r * lds;
         const RowEntries e = row_entries(t, r);
+        // the thread's first entry and its logit, on their way with the row
+        const int64_t k0 = threadIdx.x;
+        int64_t col = -1;
+        float val = 0.f, logit = 0.f;
+        if (k0 < e.n) {
+            col = load_column(t.idx, t.ib, e.i0 + k0);
+            val = load_value(t.val, t.vt, e.v0 + k0);
+            if (col >= V) col = -1;
+            if (col >= 0) logit = float(row[col]);
+        }
         MaxSum a = kNothing;
-        int64_t j = int64_t(threadIdx.x) * N - misaligned<T, N>(row);
-        for (; j + (kAhead - 1) * STEP <= V - N; j += kAhead * STEP) {
-            // (only the row's very first pack can start before it)
+        for (int64_t j = int64_t(threadIdx.x) * N - misaligned<T, N>(row); j < V; j += kAhead * STEP) {
             Vec<T, N> v[kAhead];
-            v[0] = load_vec_nt<T, N>(row + max(j, int64_t(0)));
+            // (only the row's very first pack can start before it)
+            if (j >= 0 && j + (kAhead - 1) * STEP <= V - N) {
 #pragma unroll
-            for (int k = 1; k < kAhead; ++k) v[k] = load_vec_nt<T, N>(row + j + k * STEP);
-            add_pack_base<T, N>(a, v[0], int(min(j, int64_t(0))), c);
+                for (int k = 0; k < kAhead; ++k) v[k] = load_vec_nt<T, N>(row + j + k * STEP);
 #pragma unroll
-            for (int k = 1; k < kAhead; ++k) add_pack_base<T, N>(a, v[k], 0, c);
+                for (int k = 0; k < kAhead; ++k) add_pack_base<T, N>(a, v[k], 0, c);
+            } else {
+                Place at[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    at[k] = place<N>(j + k * STEP, V);
+                    v[k] = load_vec_nt<T, N>(row + at[k].c);
+                }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (at[k].shift < N) add_pack_base<T, N>(a, v[k], at[k].shift, c);
+            }
         }
-        for (; j < V; j += STEP) {
-            const Place at = place<N>(j, V);
-            add_pack_base<T, N>(a, load_vec_nt<T, N>(row + at.c), at.shift, c);
-        }
+        MaxSum b = kNothing;
+        if (col >= 0) add_value(b, val, c);
+        teacher_sums(b, t, e, k0 + blockDim.x, V, c);
         bool none, far;
-        const RowStat st = row_stat<T, N>(a, teacher_sums(t, e, V, c), row, V, c, weight ? weight[r] : 1.f, temp, ms,
-                                          &none, &far);
-        const float x = wave_total(none ? 0.f : teacher_loss<T>(t, e, row, V, c, st));
+        const RowStat st = row_stat<T, N>(a, b, row, V, c, weight ? weight[r] : 1.f, temp, ms, &none, &far);
+        float x = 0.f;
+        if (!none) {
+            const float lp = (val - st.tm) * c - st.tl2;
+            if (col >= 0) x = loss_term(exp2_of(lp), lp, st.log2q(logit, c));
+            teacher_loss<T>(x, t, e, k0 + blockDim.x, row, V, c, st);
+        }
+        x = wave_total(x);
         if (lane_id() == 0) fs[w] = x;
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -400,7 +425,7 @@ __global__ __launch_bounds__(kRowBlock) void distill_fused(const T* S, int64_t l
         const float val = ahead.value(t.vt);
         MaxSum b = kNothing;
         if (e.n > NT)
-            b = teacher_sums(t, e, V, c);
+            teacher_sums(b, t, e, tid, V, c);
         else if (col >= 0)
             add_value(b, val, c);
         head[tid] = -1;
@@ -476,8 +501,12 @@ __global__ __launch_bounds__(kRowBlock) void distill_fused(const T* S, int64_t l
         }
         lds_barrier();
         float x = 0.f;
-        if (!none) x = !listed || far ? teacher_loss<T>(t, e, row, V, c, st)
-                                      : col >= 0 ? loss_term(p, lp, lq_s[tid]) : 0.f;
+        if (!none) {
+            if (!listed || far)
+                teacher_loss<T>(x, t, e, tid, row, V, c, st);
+            else if (col >= 0)
+                x = loss_term(p, lp, lq_s[tid]);
+        }
         x = wave_total(x);
         if (lane_id() == 0) lsum[w] = x;
         e = enext;
@@ -547,8 +576,11 @@ void distill(const DenseRows& S, const Entries& t, float temperature, const floa
             }
         }
         RowStat* stat = g ? static_cast<RowStat*>(tmp) : nullptr;
-        distill_rows<T, N><<<unsigned(std::min<int64_t>(m, int64_t(1) << 20)), nt, 0, s>>>(x, S.ld, m, V, t, temperature,
-                                                                                       weight, loss, stat);
+        const unsigned rows = unsigned(std::min<int64_t>(m, int64_t(1) << 20));
+        if (nt <= 512)
+            distill_rows<T, N, 512><<<rows, nt, 0, s>>>(x, S.ld, m, V, t, temperature, weight, loss, stat);
+        else if constexpr (N > 1)
+            distill_rows<T, N, kRowBlock><<<rows, nt, 0, s>>>(x, S.ld, m, V, t, temperature, weight, loss, stat);
         if constexpr (N > 1) {
             if (!stat) return;
             constexpr int64_t COLS = int64_t(kBlock) * kGradPacks * N;
