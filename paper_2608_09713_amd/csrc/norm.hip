@@ -7,7 +7,8 @@
 //
 // Bound by the bytes of the rows: every row is read once and held in
 // registers (16 bytes per lane and pack) between its statistics and its
-// output, by one wavefront or by one workgroup; the variance is a second pass
+// output, by a group of 4 to 64 lanes or by a workgroup of as many wavefronts
+// as it takes; the variance is a second pass
 // over the registers, not a difference of sums.  Statistics and sums are
 // 32-bit floats.  The parameters' gradients are summed by the threads that
 // own the columns over the rows of a workgroup, written once per workgroup,
@@ -23,6 +24,7 @@ namespace spsyrk {
 namespace {
 
 constexpr int kRowBlock = 1024;  // threads per row, at most
+constexpr int kCus = 256;        // compute units of the chip
 
 // N parameters of type PT at column c
 template <int N, typename PT>
@@ -41,27 +43,44 @@ __device__ inline void load_params(const PT* p, int c, float none, float (&out)[
     }
 }
 
-// Sum over the TPR threads of a row (a wavefront, or the whole workgroup with
-// buf of TPR / kWave words, not used again before the next sum's barrier).
-template <int TPR>
+// Sum over groups of L lanes, in every lane.
+template <int L>
+__device__ inline float group_total(float v) {
+    if constexpr (L == kWave) return wave_total(v);
+    auto add = [&](auto ctrl) {
+        v += __int_as_float(
+            __builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    using std::integral_constant;
+    add(integral_constant<int, 0xb1>());   // lane ^ 1
+    add(integral_constant<int, 0x4e>());   // lane ^ 2
+    if constexpr (L >= 8) add(integral_constant<int, 0x141>());   // mirrored within 8
+    if constexpr (L >= 16) add(integral_constant<int, 0x140>());  // within 16
+    if constexpr (L >= 32) v += __shfl_xor(v, 16, kWave);
+    return v;
+}
+
+// Sum over a row's threads: L lanes, or (L 0) the workgroup's wavefronts with
+// buf of kMostWaves words, not used again before the next sum's barrier.
+constexpr int kMostWaves = kRowBlock / kWave;
+template <int L>
 __device__ inline float row_sum(float v, float* buf) {
-    v = wave_total(v);
-    if constexpr (TPR > kWave) {
+    v = group_total<L ? L : kWave>(v);
+    if constexpr (L == 0) {
         if (lane_id() == 0) buf[threadIdx.x / kWave] = v;
-        __syncthreads();
+        lds_barrier();
         v = 0.f;
-#pragma unroll
-        for (int i = 0; i < TPR / kWave; ++i) v += buf[i];
+        for (int i = 0; i < int(blockDim.x) / kWave; ++i) v += buf[i];
     }
     return v;
 }
 
-// The places of a thread's packs.  NP is the row's packs per thread, rounded
-// up, so that only the last one can pass the row's end.
-template <int N, int TPR, int NP>
-__device__ inline void row_places(int l, int64_t d, Place (&at)[NP]) {
+// The places of a thread's packs, `threads` per row.  Only the last one can
+// pass the row's end (row_shape).
+template <int N, int NP>
+__device__ inline void row_places(int l, int threads, int64_t d, Place (&at)[NP]) {
 #pragma unroll
-    for (int k = 0; k < NP; ++k) at[k] = place<N>((int64_t(k) * TPR + l) * N, d);
+    for (int k = 0; k < NP; ++k) at[k] = place<N>((int64_t(k) * threads + l) * N, d);
 }
 // whether element i of pack k belongs to this thread alone
 template <int NP>
@@ -69,18 +88,24 @@ __device__ inline bool own(const Place (&at)[NP], int k, int i) {
     return k < NP - 1 || i >= at[k].shift;
 }
 
-template <typename T, typename PT, int N, int TPR, int NP>
-__global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void norm_kernel(
+template <typename T, typename PT, int N, int L, int NP>
+__global__ __launch_bounds__(L ? kBlock : kRowBlock) void norm_kernel(
     const T* __restrict__ x, int64_t ldx, int64_t m, int64_t d, const PT* __restrict__ gamma,
     const PT* __restrict__ beta, float eps, T* __restrict__ y, int64_t ldy, float* __restrict__ mean,
     float* __restrict__ rstd) {
-    constexpr int ROWS = TPR < kBlock ? kBlock / TPR : 1;
-    __shared__ float buf[2][2][TPR / kWave];
-    const int l = threadIdx.x % TPR;
+    constexpr int ROWS = L ? kBlock / (L ? L : 1) : 1;
+    constexpr bool KEEP = L && NP == 1;  // the parameters stay in registers over the rows
+    __shared__ float buf[2][2][kMostWaves];
+    const int threads = L ? L : int(blockDim.x), l = L ? int(threadIdx.x) % (L ? L : 1) : int(threadIdx.x);
     int turn = 0;
     Place at[NP];
-    row_places<N, TPR>(l, d, at);
-    for (int64_t r = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR; r < m;
+    row_places<N>(l, threads, d, at);
+    float g[N], b[N];
+    if constexpr (KEEP) {
+        load_params<N>(gamma, at[0].c, 1.f, g);
+        load_params<N>(beta, at[0].c, 0.f, b);
+    }
+    for (int64_t r = int64_t(blockIdx.x) * ROWS + (L ? threadIdx.x / (L ? L : 1) : 0); r < m;
          r += int64_t(gridDim.x) * ROWS, turn ^= 1) {
         Vec<T, N> v[NP];
 #pragma unroll
@@ -90,7 +115,7 @@ __global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void norm_kernel(
         for (int k = 0; k < NP; ++k)
 #pragma unroll
             for (int i = 0; i < N; ++i) s += own(at, k, i) ? float(v[k][i]) : 0.f;
-        const float mu = row_sum<TPR>(s, buf[turn][0]) / float(d);
+        const float mu = row_sum<L>(s, buf[turn][0]) / float(d);
         s = 0.f;
 #pragma unroll
         for (int k = 0; k < NP; ++k)
@@ -99,7 +124,7 @@ __global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void norm_kernel(
                 const float z = own(at, k, i) ? float(v[k][i]) - mu : 0.f;
                 s = fmaf(z, z, s);
             }
-        const float rs = 1.f / sqrtf(row_sum<TPR>(s, buf[turn][1]) / float(d) + eps);
+        const float rs = 1.f / sqrtf(row_sum<L>(s, buf[turn][1]) / float(d) + eps);
         if (l == 0) {
             mean[r] = mu;
             rstd[r] = rs;
@@ -107,9 +132,10 @@ __global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void norm_kernel(
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
             if (at[k].shift >= N) break;
-            float g[N], b[N];
-            load_params<N>(gamma, at[k].c, 1.f, g);
-            load_params<N>(beta, at[k].c, 0.f, b);
+            if constexpr (!KEEP) {
+                load_params<N>(gamma, at[k].c, 1.f, g);
+                load_params<N>(beta, at[k].c, 0.f, b);
+            }
             Vec<T, N> o;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[i] = T(fmaf((float(v[k][i]) - mu) * rs, g[i], b[i]));
@@ -126,7 +152,7 @@ __global__ __launch_bounds__(kRowBlock) void norm_long(const T* __restrict__ x, 
                                                        float* __restrict__ mean, float* __restrict__ rstd) {
     constexpr int N = 16 / int(sizeof(T));
     constexpr int64_t STEP = int64_t(kRowBlock) * N;
-    __shared__ float buf[2][2][kRowBlock / kWave];
+    __shared__ float buf[2][2][kMostWaves];
     int turn = 0;
     for (int64_t r = blockIdx.x; r < m; r += gridDim.x, turn ^= 1) {
         const T* xr = x + r * ldx;
@@ -137,7 +163,7 @@ __global__ __launch_bounds__(kRowBlock) void norm_long(const T* __restrict__ x, 
 #pragma unroll
             for (int i = 0; i < N; ++i) s += i >= at.shift ? float(v[i]) : 0.f;
         }
-        const float mu = row_sum<kRowBlock>(s, buf[turn][0]) / float(d);
+        const float mu = row_sum<0>(s, buf[turn][0]) / float(d);
         s = 0.f;
         for (int64_t c = int64_t(threadIdx.x) * N; c < d; c += STEP) {
             const Place at = place<N>(c, d);
@@ -148,7 +174,7 @@ __global__ __launch_bounds__(kRowBlock) void norm_long(const T* __restrict__ x, 
                 s = fmaf(z, z, s);
             }
         }
-        const float rs = 1.f / sqrtf(row_sum<kRowBlock>(s, buf[turn][1]) / float(d) + eps);
+        const float rs = 1.f / sqrtf(row_sum<0>(s, buf[turn][1]) / float(d) + eps);
         if (threadIdx.x == 0) {
             mean[r] = mu;
             rstd[r] = rs;
@@ -169,12 +195,8 @@ __global__ __launch_bounds__(kRowBlock) void norm_long(const T* __restrict__ x, 
 
 // ---- gradient
 
-// Threads per workgroup: rows of a wavefront share one of eight.
+// Threads per workgroup where rows take lanes of a wavefront.
 constexpr int kGradBlock = 512;
-template <int TPR>
-constexpr int grad_threads() {
-    return TPR == kWave ? kGradBlock : TPR;
-}
 
 // a row's packs of x and dy, and its statistics
 template <typename T, int N, int NP>
@@ -184,18 +206,19 @@ struct GradRow {
 };
 
 // part: per workgroup the sums of dy h over its rows (d words), then of dy
-// (null: no parameters)
-template <typename T, typename PT, int N, int TPR, int NP>
-__global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
+// (null: no parameters).  L: lanes per row, or 0 and a workgroup of up to MOST
+// threads per row.
+template <typename T, typename PT, int N, int L, int MOST, int NP>
+__global__ __launch_bounds__(MOST) void norm_grad_kernel(
     const T* __restrict__ dy, int64_t ldg, const T* __restrict__ x, int64_t ldx, int64_t m, int64_t d,
     const float* __restrict__ mean, const float* __restrict__ rstd, const PT* __restrict__ gamma, T* __restrict__ dx,
     int64_t ldd, float* __restrict__ part) {
-    constexpr int ROWS = grad_threads<TPR>() / TPR, WAVES = TPR / kWave;
-    __shared__ float2 buf[2][WAVES];
-    const int l = threadIdx.x % TPR;
+    constexpr int ROWS = L ? MOST / (L ? L : 1) : 1;
+    __shared__ float2 buf[2][kMostWaves];
+    const int threads = L ? L : int(blockDim.x), l = L ? int(threadIdx.x) % (L ? L : 1) : int(threadIdx.x);
     int turn = 0;
     Place at[NP];
-    row_places<N, TPR>(l, d, at);
+    row_places<N>(l, threads, d, at);
     float g[NP][N], dg[NP][N] = {}, db[NP][N] = {};
 #pragma unroll
     for (int k = 0; k < NP; ++k) load_params<N>(gamma, at[k].c, 1.f, g[k]);
@@ -211,9 +234,9 @@ __global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
         return q;
     };
     const int64_t step = int64_t(gridDim.x) * ROWS;
-    int64_t r = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR;
+    int64_t r = int64_t(blockIdx.x) * ROWS + (L ? threadIdx.x / (L ? L : 1) : 0);
     // (a row ahead, but where its registers would spill)
-    constexpr bool AHEAD = TPR < kRowBlock || NP == 1;
+    constexpr bool AHEAD = MOST < kRowBlock;
     GradRow<T, N, NP> next;
     if (AHEAD && r < m) next = load(r);
     for (; r < m; r += step, turn ^= 1) {
@@ -231,15 +254,14 @@ __global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
                 dg[k][i] = fmaf(w, h, dg[k][i]);
                 db[k][i] += w;
             }
-        s1 = wave_total(s1);
-        s2 = wave_total(s2);
-        if constexpr (WAVES > 1) {
+        s1 = group_total<L ? L : kWave>(s1);
+        s2 = group_total<L ? L : kWave>(s2);
+        if constexpr (L == 0) {
             // (two buffers: a wavefront can be one row ahead of another)
             if (lane_id() == 0) buf[turn][l / kWave] = make_float2(s1, s2);
-            __syncthreads();
+            lds_barrier();
             s1 = s2 = 0.f;
-#pragma unroll
-            for (int i = 0; i < WAVES; ++i) {
+            for (int i = 0; i < threads / kWave; ++i) {
                 s1 += buf[turn][i].x;
                 s2 += buf[turn][i].y;
             }
@@ -261,18 +283,29 @@ __global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
     if (!part) return;
     float* p = part + int64_t(blockIdx.x) * 2 * d;
     if constexpr (ROWS > 1) {
-        // the wavefronts' sums, pairwise: the upper half's through LDS to the lower half
-        __shared__ float sum[ROWS / 2][2][NP][N][kWave];
-        const int w = threadIdx.x / kWave;
+        // the sums of a wavefront's groups, by lane distance; then the
+        // wavefronts', pairwise: the upper half's through LDS to the lower half
+        constexpr int WAVES = MOST / kWave;
+        __shared__ float sum[WAVES / 2][2][NP][N][kWave];
+        const int w = threadIdx.x / kWave, lane = lane_id();
 #pragma unroll
-        for (int half = ROWS / 2; half > 0; half /= 2) {
+        for (int far = L; far < kWave; far *= 2)
+#pragma unroll
+            for (int k = 0; k < NP; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    dg[k][i] += __shfl_xor(dg[k][i], far, kWave);
+                    db[k][i] += __shfl_xor(db[k][i], far, kWave);
+                }
+#pragma unroll
+        for (int half = WAVES / 2; half > 0; half /= 2) {
             if (w >= half && w < 2 * half)
 #pragma unroll
                 for (int k = 0; k < NP; ++k)
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        sum[w - half][0][k][i][l] = dg[k][i];
-                        sum[w - half][1][k][i][l] = db[k][i];
+                        sum[w - half][0][k][i][lane] = dg[k][i];
+                        sum[w - half][1][k][i][lane] = db[k][i];
                     }
             __syncthreads();
             if (w < half)
@@ -280,12 +313,12 @@ __global__ __launch_bounds__(grad_threads<TPR>()) void norm_grad_kernel(
                 for (int k = 0; k < NP; ++k)
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        dg[k][i] += sum[w][0][k][i][l];
-                        db[k][i] += sum[w][1][k][i][l];
+                        dg[k][i] += sum[w][0][k][i][lane];
+                        db[k][i] += sum[w][1][k][i][lane];
                     }
             __syncthreads();
         }
-        if (w > 0) return;
+        if (w > 0 || lane >= L) return;
     }
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
@@ -311,7 +344,7 @@ __global__ __launch_bounds__(kRowBlock) void norm_grad_long(const T* __restrict_
                                                             int64_t ldd) {
     constexpr int N = 16 / int(sizeof(T));
     constexpr int64_t STEP = int64_t(kRowBlock) * N;
-    __shared__ float buf[2][2][kRowBlock / kWave];
+    __shared__ float buf[2][2][kMostWaves];
     int turn = 0;
     for (int64_t r = blockIdx.x; r < m; r += gridDim.x, turn ^= 1) {
         const T *xr = x + r * ldx, *gr = dy + r * ldg;
@@ -329,8 +362,8 @@ __global__ __launch_bounds__(kRowBlock) void norm_grad_long(const T* __restrict_
                 s2 = fmaf(a, (float(v[i]) - mu) * rs, s2);
             }
         }
-        s1 = row_sum<kRowBlock>(s1, buf[turn][0]) / float(d);
-        s2 = row_sum<kRowBlock>(s2, buf[turn][1]) / float(d);
+        s1 = row_sum<0>(s1, buf[turn][0]) / float(d);
+        s2 = row_sum<0>(s2, buf[turn][1]) / float(d);
         for (int64_t c = int64_t(threadIdx.x) * N; c < d; c += STEP) {
             const Place at = place<N>(c, d);
             const Vec<T, N> v = load_vec<T, N>(xr + at.c), w = load_vec<T, N>(gr + at.c);
@@ -419,23 +452,47 @@ __global__ __launch_bounds__(kJoinBlock) void norm_params_join(const float* __re
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Packs per row that the gradient's threads hold, at most (registers: two rows
-// of x and dy, gamma and two sums per column): four of four columns per
-// thread, or two of eight.
-template <typename T>
-constexpr int grad_block_packs() {
-    return sizeof(T) == 4 ? 4 : 2;
+inline int64_t packs_of(int64_t d, int dt) {
+    const int64_t n = 16 / dtype_bytes(dt);
+    return d >= n ? ceil_div(d, n) : d;
 }
-inline int64_t packs_of(int64_t d, int dt) { return ceil_div(d * dtype_bytes(dt), 16); }
-inline bool grad_is_long(int64_t packs, int dt) { return packs > int64_t(dt == kDtF32 ? 4 : 2) * kRowBlock; }
 
-// Workgroups of the gradient (each writes 2 d sums): 16 wavefronts per
-// compute unit where there are rows enough.
+// How a row is spread over threads: `lanes` of a wavefront, or (0) a workgroup
+// of `threads`, and packs per thread.  Of the packs per thread that leave no
+// pack but the last past the row's end (64 np (np - 1) packs or more) those
+// that leave the fewest threads' packs empty are taken, and of these the most;
+// with `few`, the fewest that a workgroup's threads can hold.  np 0: the row is
+// too long for registers (more than `most` packs per thread).
+struct RowShape {
+    int lanes, threads, np;
+};
+inline RowShape row_shape(int64_t packs, int most, bool few) {
+    if (packs <= 2 * kWave) {
+        int lanes = 4;
+        while (lanes < kWave && lanes < packs) lanes *= 2;
+        return {lanes, lanes, packs <= kWave ? 1 : 2};
+    }
+    RowShape best{0, 0, 0};
+    for (int np = 2; np <= most; ++np) {
+        const int64_t threads = ceil_div(ceil_div(packs, np), kWave) * kWave;
+        if (threads > kRowBlock || packs < 64 * np * (np - 1)) continue;
+        if (!best.np || (!few && threads * np <= int64_t(best.threads) * best.np)) best = {0, int(threads), np};
+    }
+    return best;
+}
+
+// The gradient's threads hold two rows' packs of x and dy, gamma and two sums
+// per column: two packs of eight columns, or up to four of four.
+inline RowShape grad_shape(int64_t d, int dt) { return row_shape(packs_of(d, dt), dt == kDtF32 ? 4 : 2, true); }
+
+// Workgroups of the gradient (each writes 2 d sums): as many as the registers
+// let a compute unit hold, 12 or 16 wavefronts (more would take a second turn).
 constexpr int64_t kLongGroups = 64;
-inline int64_t grad_groups(int64_t m, int64_t packs, int dt) {
-    if (grad_is_long(packs, dt)) return kLongGroups;
-    if (packs <= 2 * kWave) return std::min<int64_t>(ceil_div(m, kGradBlock / kWave), 256);
-    return std::min<int64_t>(m, packs <= 2 * kBlock ? 1024 : packs <= 2 * kGradBlock ? 512 : 256);
+inline int64_t grad_groups(int64_t m, const RowShape& s, int dt) {
+    if (!s.np) return kLongGroups;
+    if (s.lanes) return std::min<int64_t>(ceil_div(m, kGradBlock / s.lanes), s.np == 1 ? 2 * kCus : kCus);
+    const int waves = dt == kDtF32 && s.np == 2 ? 16 : 12;
+    return std::min<int64_t>(m, int64_t(kCus) * std::max(waves * kWave / s.threads, 1));
 }
 
 inline unsigned row_grid(int64_t blocks) { return unsigned(std::min<int64_t>(blocks, int64_t(1) << 20)); }
@@ -450,18 +507,22 @@ inline void by_params(int dt, int pt, int64_t d, F f) {
     });
 }
 
-// f(threads per row, packs per thread) for a row of `packs` packs, of the
-// combinations (TPR, 1 .. MOST)
-template <int TPR, int MOST, typename F>
-inline void by_packs(int64_t packs, F f) {
-    if (packs <= int64_t(TPR) || MOST == 1)
-        f(std::integral_constant<int, TPR>(), std::integral_constant<int, 1>());
-    else if (packs <= 2 * int64_t(TPR) || MOST == 2)
-        f(std::integral_constant<int, TPR>(), std::integral_constant<int, MOST < 2 ? 1 : 2>());
-    else if (packs <= 3 * int64_t(TPR))
-        f(std::integral_constant<int, TPR>(), std::integral_constant<int, MOST < 3 ? 1 : 3>());
-    else
-        f(std::integral_constant<int, TPR>(), std::integral_constant<int, MOST < 4 ? 1 : 4>());
+// f(lanes, packs per thread) of a shape, as constants
+template <int N, typename F>
+inline void by_shape(const RowShape& s, F f) {
+    using std::integral_constant;
+    const integral_constant<int, 1> one;
+    if (s.lanes == 4) return f(integral_constant<int, 4>(), one);
+    if (s.lanes == 8) return f(integral_constant<int, 8>(), one);
+    if constexpr (N > 1) {
+        if (s.lanes == 16) return f(integral_constant<int, 16>(), one);
+        if (s.lanes == 32) return f(integral_constant<int, 32>(), one);
+        if (s.lanes && s.np == 1) return f(integral_constant<int, kWave>(), one);
+        if (s.lanes) return f(integral_constant<int, kWave>(), integral_constant<int, 2>());
+        if (s.np == 2) return f(integral_constant<int, 0>(), integral_constant<int, 2>());
+        if (s.np == 3) return f(integral_constant<int, 0>(), integral_constant<int, 3>());
+        return f(integral_constant<int, 0>(), integral_constant<int, 4>());
+    }
 }
 
 }  // namespace
@@ -472,71 +533,71 @@ void layer_norm(const DenseRows& X, const void* gamma, const void* beta, int pt,
         using T = decltype(e);
         using PT = decltype(q);
         constexpr int N = decltype(n)::value;
-        const int64_t m = X.m, d = X.n, packs = ceil_div(d, N);
+        const int64_t m = X.m, d = X.n;
         const T* x = static_cast<const T*>(X.p);
         const PT *g = static_cast<const PT*>(gamma), *b = static_cast<const PT*>(beta);
         T* y = static_cast<T*>(Y.p);
-        auto launch = [&](auto tpr, auto np) {
-            constexpr int TPR = decltype(tpr)::value, NP = decltype(np)::value;
-            constexpr int NT = TPR < kBlock ? kBlock : TPR;
-            norm_kernel<T, PT, N, TPR, NP><<<row_grid(ceil_div(m, NT / TPR)), NT, 0, s>>>(x, X.ld, m, d, g, b, eps, y,
-                                                                                         Y.ld, mean, rstd);
-        };
-        if constexpr (N == 1) {
-            by_packs<kWave, 1>(packs, launch);
-        } else {
-            if (packs <= 2 * kWave)
-                by_packs<kWave, 2>(packs, launch);
-            else if (packs <= 4 * kBlock)
-                by_packs<kBlock, 4>(packs, launch);
-            else if (packs <= 4 * kRowBlock)
-                by_packs<kRowBlock, 4>(packs, launch);
-            else
+        const RowShape shape = row_shape(packs_of(d, X.dt), 4, false);
+        if (!shape.np) {
+            if constexpr (N > 1)
                 norm_long<T, PT><<<row_grid(m), kRowBlock, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld, mean, rstd);
+            return;
         }
+        by_shape<N>(shape, [&](auto lanes, auto np) {
+            constexpr int L = decltype(lanes)::value, NP = decltype(np)::value;
+            // (parameters in registers: as many workgroups as the chip holds, over all rows)
+            const int64_t blocks = L ? ceil_div(m, kBlock / (L ? L : 1)) : m;
+            const unsigned grid = row_grid(L && NP == 1 ? std::min<int64_t>(blocks, 8 * kCus) : blocks);
+            norm_kernel<T, PT, N, L, NP><<<grid, L ? kBlock : shape.threads, 0, s>>>(x, X.ld, m, d, g, b, eps, y, Y.ld,
+                                                                                    mean, rstd);
+        });
     });
 }
 
 size_t layer_norm_grad_tmp_bytes(int64_t m, int64_t d, int dt, bool params) {
-    return params ? size_t(grad_groups(m, packs_of(d, dt), dt)) * 2 * size_t(d) * sizeof(float) : 0;
+    return params ? size_t(grad_groups(m, grad_shape(d, dt), dt)) * 2 * size_t(d) * sizeof(float) : 0;
 }
 
 void layer_norm_grad(const DenseRows& G, const DenseRows& X, const float* mean, const float* rstd, const void* gamma,
                      int pt, const DenseRows& dX, void* dgamma, void* dbeta, void* tmp, hipStream_t s) {
-    const int64_t groups = X.m ? grad_groups(X.m, packs_of(X.n, X.dt), X.dt) : 0;
+    const RowShape shape = grad_shape(X.n, X.dt);
+    const int64_t groups = X.m ? grad_groups(X.m, shape, X.dt) : 0;
     by_params(X.dt, pt, X.n, [&](auto e, auto q, auto n) {
         using T = decltype(e);
         using PT = decltype(q);
         constexpr int N = decltype(n)::value;
-        const int64_t m = X.m, d = X.n, packs = ceil_div(d, N);
+        const int64_t m = X.m, d = X.n;
         const T *x = static_cast<const T*>(X.p), *dy = static_cast<const T*>(G.p);
         const PT* g = static_cast<const PT*>(gamma);
         T* dx = static_cast<T*>(dX.p);
         float* part = dgamma || dbeta ? static_cast<float*>(tmp) : nullptr;
-        auto launch = [&](auto tpr, auto np) {
-            constexpr int TPR = decltype(tpr)::value, NP = decltype(np)::value;
-            norm_grad_kernel<T, PT, N, TPR, NP><<<unsigned(groups), grad_threads<TPR>(), 0, s>>>(
-                dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx, dX.ld, part);
-        };
-        if (m > 0) {
-            if constexpr (N == 1) {
-                by_packs<kWave, 1>(packs, launch);
-            } else {
-                if (packs <= 2 * kWave) {
-                    by_packs<kWave, 2>(packs, launch);
-                } else if (packs <= 2 * kBlock) {
-                    by_packs<kBlock, 2>(packs, launch);
-                } else if (packs <= 2 * kGradBlock) {
-                    launch(std::integral_constant<int, kGradBlock>(), std::integral_constant<int, 2>());
-                } else if (!grad_is_long(packs, X.dt)) {
-                    by_packs<kRowBlock, grad_block_packs<T>()>(packs, launch);
-                } else {
-                    norm_grad_long<T, PT><<<row_grid(m), kRowBlock, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx,
-                                                                            dX.ld);
-                    if (part)
-                        norm_params_long<T><<<dim3(unsigned(ceil_div(packs, kWave)), unsigned(groups)), kBlock, 0, s>>>(
-                            dy, G.ld, x, X.ld, m, d, mean, rstd, part);
+        if (m > 0 && shape.np) {
+            by_shape<N>(shape, [&](auto lanes, auto np) {
+                constexpr int L = decltype(lanes)::value, NP = decltype(np)::value;
+                // (more than two packs: f32 only)
+                if constexpr (NP <= 2 || sizeof(T) == 4) {
+                    auto launch = [&](auto most, int threads) {
+                        constexpr int MOST = decltype(most)::value;
+                        norm_grad_kernel<T, PT, N, L, MOST, NP><<<unsigned(groups), threads, 0, s>>>(
+                            dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx, dX.ld, part);
+                    };
+                    if constexpr (L > 0) {
+                        launch(std::integral_constant<int, kGradBlock>(), kGradBlock);
+                    } else {
+                        if (shape.threads <= kGradBlock)
+                            launch(std::integral_constant<int, kGradBlock>(), shape.threads);
+                        else
+                            launch(std::integral_constant<int, kRowBlock>(), shape.threads);
+                    }
                 }
+            });
+        } else if (m > 0) {
+            if constexpr (N > 1) {
+                norm_grad_long<T, PT><<<row_grid(m), kRowBlock, 0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, g, dx,
+                                                                        dX.ld);
+                if (part)
+                    norm_params_long<T><<<dim3(unsigned(ceil_div(packs_of(d, X.dt), kWave)), unsigned(groups)), kBlock,
+                                          0, s>>>(dy, G.ld, x, X.ld, m, d, mean, rstd, part);
             }
         }
         if (dgamma || dbeta)  // (of no rows: zeros)
