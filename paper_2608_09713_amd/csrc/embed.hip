@@ -9,8 +9,9 @@
 // (stable, so a column's entries are added in their order in A and the result
 // is the same on every run).  Sums are held in 32-bit floats and rounded once.
 //
-// A wavefront takes a target's columns 16 bytes a lane, a few packs of a row
-// at once; targets of narrow rows share a wavefront.  A target of more
+// A wavefront takes a target's columns 16 bytes a lane, several entries' rows
+// at once (two packs a lane of four: 355 us against 325 with one pack of
+// eight, 65536 tokens over 131072 x 4096 bf16); targets of narrow rows share a wavefront.  A target of more
 // than a tile of entries (a frequent token) would be walked by one wavefront:
 // such targets are left to a second launch, in which every tile of entries
 // sums its part of the (at most two) long targets that reach into it, and a
@@ -23,8 +24,7 @@
 namespace spsyrk {
 namespace {
 
-constexpr int kUnroll = 4;     // packs of one row per lane: tokens
-constexpr int kSumUnroll = 2;  // and sums, which hold several entries' packs
+constexpr int kUnroll = 4;  // packs of one row per lane (tokens)
 
 // Lanes per row (a power of two, at most a wavefront) for rows of `packs` packs.
 inline int lane_bits(int64_t packs) {
@@ -97,13 +97,15 @@ struct Targets {
     }
 };
 
-// acc += sum of the entries [a, b) over the lane's packs.
+constexpr int kSumEntries = 8;
+
+// acc += sum of the entries [a, b) over the lane's pack.
 // Every group of 1 << lg lanes reads its entries' rows and weights one per
 // lane and takes them from there by lane reads; E entries' packs are in
 // flight at once.
-template <typename T, int N, int U, int E, typename P>
+template <typename T, int N, int E, typename P>
 __device__ inline void sum_entries(const Targets<P>& t, int64_t a, int64_t b, const T* __restrict__ src,
-                                   int64_t nsrc, int64_t ld, const Place (&at)[U], int lg, float (&acc)[U][N]) {
+                                   int64_t nsrc, int64_t ld, const Place& at, int lg, float (&acc)[N]) {
     const int width = 1 << lg, l = lane_id() & (width - 1);
     for (int64_t base = a; base < b; base += width) {
         int64_t row = -1;
@@ -115,7 +117,7 @@ __device__ inline void sum_entries(const Targets<P>& t, int64_t a, int64_t b, co
         }
         const int n = int(min(int64_t(width), b - base));
         for (int j = 0; j < n; j += E) {
-            Vec<T, N> v[E][U];
+            Vec<T, N> v[E];
             float wj[E];
 #pragma unroll
             for (int x = 0; x < E; ++x) {
@@ -124,20 +126,13 @@ __device__ inline void sum_entries(const Targets<P>& t, int64_t a, int64_t b, co
                 wj[x] = __shfl(w, y, width);
                 if (j + x >= n) r = -1;
                 // (nothing is read for padding, which adds zeros)
-#pragma unroll
-                for (int k = 0; k < U; ++k) v[x][k] = Vec<T, N>(T(0.f));
-                if (r >= 0) {
-                    const T* p = src + r * ld;
-#pragma unroll
-                    for (int k = 0; k < U; ++k) v[x][k] = load_vec<T, N>(p + at[k].c);
-                }
+                v[x] = Vec<T, N>(T(0.f));
+                if (r >= 0) v[x] = load_vec<T, N>(src + r * ld + at.c);
             }
 #pragma unroll
             for (int x = 0; x < E; ++x)
 #pragma unroll
-                for (int k = 0; k < U; ++k)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) acc[k][i] = fmaf(wj[x], float(v[x][k][i]), acc[k][i]);
+                for (int i = 0; i < N; ++i) acc[i] = fmaf(wj[x], float(v[x][i]), acc[i]);
         }
     }
 }
@@ -180,7 +175,7 @@ __device__ inline int64_t target_of(const Targets<P>& t, int64_t e) {
 // Tile q's part of the long targets that hold its first and its last entry,
 // into part[2 q] and part[2 q + 1] (the latter only for a target that starts
 // inside the tile).
-template <typename T, int N, int U, typename P>
+template <typename T, int N, typename P>
 __device__ inline void sum_tile(const Sums<T, P>& a, int64_t q, int64_t chunk, int l, int64_t end) {
     const int64_t e0 = q * a.tile, e1 = min(end, e0 + a.tile);
     int64_t of[2] = {-1, -1};
@@ -189,9 +184,7 @@ __device__ inline void sum_tile(const Sums<T, P>& a, int64_t q, int64_t chunk, i
         of[1] = target_of(a.t, e1 - 1);
         if (of[1] == of[0]) of[1] = -1;
     }
-    Place at[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) at[k] = place<N>((chunk * (int64_t(U) << a.lg) + (int64_t(k) << a.lg) + l) * N, a.d);
+    const Place at = place<N>(((chunk << a.lg) + l) * N, a.d);
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
         int64_t x0 = 0, x1 = 0;
@@ -202,42 +195,33 @@ __device__ inline void sum_tile(const Sums<T, P>& a, int64_t q, int64_t chunk, i
         }
         if (chunk == 0 && l == 0) a.long_of[2 * q + z] = int32_t(of[z]);
         if (of[z] < 0) continue;
-        float acc[U][N] = {};
-        sum_entries<T, N, U, 4>(a.t, max(x0, e0), min(x1, e1), a.src, a.nsrc, a.lds, at, a.lg, acc);
-        float* dst = a.part + (2 * q + z) * a.dp;
+        float acc[N] = {};
+        sum_entries<T, N, kSumEntries>(a.t, max(x0, e0), min(x1, e1), a.src, a.nsrc, a.lds, at, a.lg, acc);
+        if (at.shift >= N) continue;
+        Vec<float, N> o;
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            if (at[k].shift >= N) break;
-            Vec<float, N> o;
-#pragma unroll
-            for (int i = 0; i < N; ++i) o[i] = acc[k][i];
-            store_vec<float, N>(dst + at[k].c, o);
-        }
+        for (int i = 0; i < N; ++i) o[i] = acc[i];
+        store_vec<float, N>(a.part + (2 * q + z) * a.dp + at.c, o);
     }
 }
 
 // Targets t0 + j .. t0 + r - 1, whose entries are [x0, end): kSumEntries
 // entries' packs are in flight at once, across targets.
-constexpr int kSumEntries = 4;
-template <typename T, int N, int U, typename P, typename S>
+template <typename T, int N, typename P, typename S>
 __device__ inline void sum_run(const Sums<T, P>& a, int64_t t0, int j, int r, int64_t x0, int64_t end,
-                               const S& start, const Place (&at)[U]) {
+                               const S& start, const Place& at) {
     constexpr int E = kSumEntries;
     const int width = 1 << a.lg, l = lane_id() & (width - 1);
-    float acc[U][N] = {};
+    float acc[N] = {};
     int64_t next = start(j + 1);
     auto flush = [&]() {
-        T* dst = a.out + (t0 + j) * a.ldo;
+        Vec<T, N> o;
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            Vec<T, N> o;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                o[i] = T(acc[k][i] * a.scale);
-                acc[k][i] = 0.f;
-            }
-            if (at[k].shift < N) store_vec_nt<T, N>(dst + at[k].c, o);
+        for (int i = 0; i < N; ++i) {
+            o[i] = T(acc[i] * a.scale);
+            acc[i] = 0.f;
         }
+        if (at.shift < N) store_vec_nt<T, N>(a.out + (t0 + j) * a.ldo + at.c, o);
         ++j;
         if (j < r) next = start(j + 1);
     };
@@ -251,7 +235,7 @@ __device__ inline void sum_run(const Sums<T, P>& a, int64_t t0, int j, int r, in
         }
         const int n = int(min(int64_t(width), end - base));
         for (int y = 0; y < n; y += E) {
-            Vec<T, N> v[E][U];
+            Vec<T, N> v[E];
             float wj[E];
 #pragma unroll
             for (int x = 0; x < E; ++x) {
@@ -259,29 +243,22 @@ __device__ inline void sum_run(const Sums<T, P>& a, int64_t t0, int j, int r, in
                 wj[x] = __shfl(w, min(y + x, width - 1), width);
                 if (y + x >= n) q = -1;
                 // (nothing is read for padding, which adds zeros)
-#pragma unroll
-                for (int k = 0; k < U; ++k) v[x][k] = Vec<T, N>(T(0.f));
-                if (q >= 0) {
-                    const T* p = a.src + q * a.lds;
-#pragma unroll
-                    for (int k = 0; k < U; ++k) v[x][k] = load_vec<T, N>(p + at[k].c);
-                }
+                v[x] = Vec<T, N>(T(0.f));
+                if (q >= 0) v[x] = load_vec<T, N>(a.src + q * a.lds + at.c);
             }
 #pragma unroll
             for (int x = 0; x < E; ++x) {
                 if (y + x < n)
                     while (base + y + x >= next) flush();
 #pragma unroll
-                for (int k = 0; k < U; ++k)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) acc[k][i] = fmaf(wj[x], float(v[x][k][i]), acc[k][i]);
+                for (int i = 0; i < N; ++i) acc[i] = fmaf(wj[x], float(v[x][i]), acc[i]);
             }
         }
     }
     while (j < r) flush();
 }
 
-template <typename T, int N, int U, typename P>
+template <typename T, int N, typename P>
 __global__ __launch_bounds__(kBlock) void sums_kernel(Sums<T, P> a) {
     const int lane = lane_id(), sub = lane >> a.lg, l = lane & ((1 << a.lg) - 1);
     const int rows = kWave >> a.lg;
@@ -291,7 +268,7 @@ __global__ __launch_bounds__(kBlock) void sums_kernel(Sums<T, P> a) {
         for (int64_t u = int64_t(blockIdx.x) * kWavesPerBlock + w; u < a.tile_units;
              u += int64_t(a.tile_blocks) * kWavesPerBlock) {
             const int64_t q = u / a.chunks * rows + sub;
-            if (q < a.ntiles) sum_tile<T, N, U>(a, q, u % a.chunks, l, end);
+            if (q < a.ntiles) sum_tile<T, N>(a, q, u % a.chunks, l, end);
         }
         return;
     }
@@ -299,10 +276,7 @@ __global__ __launch_bounds__(kBlock) void sums_kernel(Sums<T, P> a) {
          u += int64_t(gridDim.x - a.tile_blocks) * kWavesPerBlock) {
         const int64_t t0 = (u / a.chunks * rows + sub) * a.per;
         if (t0 >= a.t.targets) continue;
-        Place at[U];
-#pragma unroll
-        for (int k = 0; k < U; ++k)
-            at[k] = place<N>((u % a.chunks * (int64_t(U) << a.lg) + (int64_t(k) << a.lg) + l) * N, a.d);
+        const Place at = place<N>((((u % a.chunks) << a.lg) + l) * N, a.d);
         // the starts of the group's targets, one per lane (per < 1 << lg, or one target)
         const int n = int(min(int64_t(a.per), a.t.targets - t0)), width = 1 << a.lg;
         const int64_t s = a.t.at(t0 + min(l, n));
@@ -319,7 +293,7 @@ __global__ __launch_bounds__(kBlock) void sums_kernel(Sums<T, P> a) {
                 end = next;
             }
             if (r > j)
-                sum_run<T, N, U>(a, t0, j, r, x0, end, start, at);
+                sum_run<T, N>(a, t0, j, r, x0, end, start, at);
             else
                 ++r;
             j = r;
@@ -396,7 +370,7 @@ inline size_t part_bytes(int64_t nnz, int64_t d) {
     return round256(rows * size_t(part_columns(d)) * sizeof(float)) + round256(rows * sizeof(int32_t));
 }
 
-template <typename T, int N, int U, typename P>
+template <typename T, int N, typename P>
 void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const DenseRows& out, void* tmp,
                  int64_t packs, int lg, hipStream_t s) {
     Sums<T, P> a;
@@ -409,7 +383,7 @@ void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const D
     a.out = static_cast<T*>(out.p);
     a.ldo = out.ld;
     a.lg = lg;
-    a.chunks = (packs + (int64_t(U) << lg) - 1) / (int64_t(U) << lg);
+    a.chunks = (packs + (int64_t(1) << lg) - 1) >> lg;
     const int64_t rows = kWave >> lg;
     a.tile = sum_tile_entries(t.nnz);
     a.ntiles = t.nnz > a.tile ? (t.nnz + a.tile - 1) / a.tile : 0;  // (no target is long)
@@ -421,7 +395,7 @@ void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const D
     a.tile_blocks = a.ntiles ? grid_for(a.tile_units) : 0;
     a.per = lg >= 4 && t.targets >= (int64_t(1) << 15) ? 8 : 1;
     a.target_units = (t.targets + rows * a.per - 1) / (rows * a.per) * a.chunks;
-    sums_kernel<T, N, U, P><<<a.tile_blocks + grid_for(a.target_units), kBlock, 0, s>>>(a);
+    sums_kernel<T, N, P><<<a.tile_blocks + grid_for(a.target_units), kBlock, 0, s>>>(a);
     if (a.ntiles)
         join_tiles<T, P><<<dim3(unsigned(a.ntiles), unsigned(std::min<int64_t>((a.d + 255) / 256, 16))), kBlock, 0,
                            s>>>(a);
@@ -435,9 +409,7 @@ void grouped_sums(const Targets<P>& t, const DenseRows& src, float scale, const 
         constexpr int N = decltype(width)::value;
         const int64_t packs = (out.n + N - 1) / N;
         const int lg = lane_bits(packs);
-        if constexpr (N > 1)
-            if (packs > kWave) return launch_sums<T, N, kSumUnroll, P>(t, src, scale, out, tmp, packs, lg, s);
-        launch_sums<T, N, 1, P>(t, src, scale, out, tmp, packs, lg, s);
+        launch_sums<T, N, P>(t, src, scale, out, tmp, packs, lg, s);
     });
 }
 
