@@ -23,6 +23,10 @@
 #include "internal.h"
 #include "rows.h"
 
+// Products and sums are fused where fmaf says so, and nowhere else: the loss
+// has the same bits alone and with the gradient.
+#pragma clang fp contract(off)
+
 namespace spsyrk {
 namespace {
 

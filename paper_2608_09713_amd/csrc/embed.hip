@@ -467,6 +467,13 @@ __device__ inline uint64_t lanes_of(uint32_t x, int bits, bool in) {
     return same;
 }
 
+// LDS accesses of a wavefront before and after it stay in order (the hardware
+// keeps them so; rows of hist are used by one wavefront each).
+__device__ inline void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Turns the counts hist[wavefront][x], x < n <= kSortBlock, into first places
 // from `first` on, by x and then by wavefront; returns x's first place to
 // thread x and the end to all.
@@ -560,10 +567,9 @@ __global__ __launch_bounds__(kSortBlock) void split_entries(Entries A, int lgbin
         const uint64_t same = lanes_of(g, bits, in);
         const uint32_t lower = __popcll(same & lanemask_lt());
         rank[k] = hist[w][g] + lower;
-        // (a wavefront's LDS accesses are in order, and only it uses this row)
-        __builtin_amdgcn_wave_barrier();
+        wave_order();
         if (in && lower == 0) hist[w][g] += __popcll(same);
-        __builtin_amdgcn_wave_barrier();
+        wave_order();
     }
     __syncthreads();
     uint32_t end;
@@ -653,9 +659,9 @@ __global__ __launch_bounds__(kSortBlock) void sort_groups(const uint2* __restric
                 // (the sums ask for the columns of their tiles' first and last entries)
                 if (pos % part == 0 || pos % part == part - 1 || pos == end - 1) key[pos] = r[k].x;
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_order();
             if (in && rank == 0) hist[w][bin] += __popcll(same);
-            __builtin_amdgcn_wave_barrier();
+            wave_order();
         }
     }
 }
