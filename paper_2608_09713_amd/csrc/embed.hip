@@ -125,7 +125,8 @@ __device__ inline void sum_entries(const Targets<P>& t, int64_t a, int64_t b, co
                 int64_t r = __shfl(row, y, width);
                 wj[x] = __shfl(w, y, width);
                 if (j + x >= n) r = -1;
-                // (nothing is read for padding, which adds zeros)
+                // (nothing is read for padding, which adds zeros whatever its weight)
+                if (r < 0) wj[x] = 0.f;
                 v[x] = Vec<T, N>(T(0.f));
                 if (r >= 0) v[x] = load_vec<T, N>(src + r * ld + at.c);
             }
@@ -242,7 +243,8 @@ __device__ inline void sum_run(const Sums<T, P>& a, int64_t t0, int j, int r, in
                 int64_t q = __shfl(row, min(y + x, width - 1), width);
                 wj[x] = __shfl(w, min(y + x, width - 1), width);
                 if (y + x >= n) q = -1;
-                // (nothing is read for padding, which adds zeros)
+                // (nothing is read for padding, which adds zeros whatever its weight)
+                if (q < 0) wj[x] = 0.f;
                 v[x] = Vec<T, N>(T(0.f));
                 if (q >= 0) v[x] = load_vec<T, N>(a.src + q * a.lds + at.c);
             }

@@ -84,6 +84,36 @@ def test_csr_rows_mostly_empty():
     check(sp.embed_grad(A, G.to(DEV), n), want, sums_tol(count, mag, want, torch.float32), "empty rows")
 
 
+@pytest.mark.parametrize("d", [2, 9, 30, 70, 700])
+def test_nan_beside_and_under_padding(d):
+    # what padding would have read or been weighted with is NaN or infinite;
+    # an infinite weight reaches its own target only
+    g = gen(d)
+    nan, inf = math.nan, math.inf
+    tok = torch.tensor([3, -1, 5, 9, 3, 4, -7], device=DEV)
+    W = normal((9, d), torch.float32, g).to(DEV)
+    W[[0, 1]] = nan
+    y = sp.embed(tok, W, 2.0)
+    assert not y[[1, 3, 6]].any() and torch.equal(y[[0, 2, 4, 5]], W[[3, 5, 3, 4]] * 2)
+    G = normal((7, d), torch.float32, g).to(DEV)
+    G[[1, 3, 6]] = nan
+    dW = sp.embed_grad(tok, G, 9)
+    assert torch.equal(dW[3], G[0] + G[4]) and torch.equal(dW[4], G[5]) and not dW[[0, 1, 2, 6, 7, 8]].any()
+    # CSR: rows of one to nine entries, the padded ones weighted NaN and infinity
+    rp = torch.tensor([0, 1, 3, 8, 17, 18], dtype=torch.int64, device=DEV)
+    ci = torch.tensor([2, -1, 3, 4, 99, 5, 6, -2, 2, 3, 4, 5, 6, 7, 8, -1, 2, 4], dtype=torch.int32, device=DEV)
+    w = torch.tensor([1.0, nan, 1, 1, inf, 1, 1, -inf, 1, 1, 1, 1, 1, 1, 1, nan, 1, inf], device=DEV)
+    A = sp.DeviceCSR(5, 9, rp, ci, w, 18)
+    y = sp.embed(A, W)
+    for r in range(4):
+        c = [int(x) for x in ci[int(rp[r]):int(rp[r + 1])] if 0 <= x < 9]
+        want = W[c].double().sum(0)
+        assert ((y[r].double() - want).abs() <= 12 * U * W[c].double().abs().sum(0)).all()
+    assert torch.equal(y[4], W[4] * inf)
+    dW = sp.embed_grad(A, torch.ones((5, d), device=DEV), 9)
+    assert torch.equal(dW[:, 0].cpu(), torch.tensor([0.0, 0, 3, 2, inf, 2, 2, 1, 1]))
+
+
 # ---- layer norm over row shapes
 
 @pytest.mark.parametrize("dtype", DTYPES)
