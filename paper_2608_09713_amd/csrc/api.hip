@@ -15,7 +15,6 @@
 #include "common.h"
 #include "dense_layout.h"
 #include "internal.h"
-#include "rows.h"
 #include "sort_layout.h"
 #include "spsyrk.h"
 
@@ -2026,258 +2025,4 @@ spsyrk_status spsyrk_timing_end(spsyrk_phase_times* out) {
 
 }  // extern "C"
 
-// ---- operators between sparse rows and dense rows
-
-namespace {
-
-bool known_dtype(int dt) { return dt >= kDtF32 && dt <= kDtBF16; }
-
-void require(bool ok, const char* what) {
-    if (!ok) {
-        set_detail("%s", what);
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-}
-
-void check_aligned(const void* p, size_t bytes, const char* name) {
-    if (reinterpret_cast<uintptr_t>(p) % bytes) {
-        set_detail("%s is not aligned to its elements of %zu bytes", name, bytes);
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-}
-
-void check_dims(int64_t rows, int64_t cols, const char* name) {
-    if (rows < 0 || cols < 0) {
-        set_detail("%s has a negative size", name);
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-    if (rows >= kLimit || cols >= kLimit) {
-        set_detail("%s: rows and columns must be below 2^31", name);
-        throw Fail{SPSYRK_ERR_SHAPE};
-    }
-}
-
-DenseRows dense_rows(const spsyrk_dense* d, const char* name) {
-    if (!d) {
-        set_detail("%s is null", name);
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-    check_dims(d->nrows, d->ncols, name);
-    if (!known_dtype(d->dtype)) {
-        set_detail("%s: unknown element type %d", name, int(d->dtype));
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-    if (d->ld < d->ncols || d->ld > (int64_t(1) << 40)) {
-        set_detail("%s: the row stride %lld must be at least the %lld columns and at most 2^40", name,
-                   (long long)d->ld, (long long)d->ncols);
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-    if (d->nrows > 0 && d->ncols > 0) {
-        if (!d->data) {
-            set_detail("%s: null data", name);
-            throw Fail{SPSYRK_ERR_INVALID_ARG};
-        }
-        check_aligned(d->data, size_t(dtype_bytes(d->dtype)), name);
-    }
-    DenseRows r;
-    r.m = d->nrows;
-    r.n = d->ncols;
-    r.ld = d->ld;
-    r.dt = d->dtype;
-    r.p = d->data;
-    return r;
-}
-
-void check_same(const DenseRows& a, const DenseRows& b, const char* what, bool rows) {
-    if (a.n != b.n || a.dt != b.dt || (rows && a.m != b.m)) {
-        set_detail("%s must agree in %scolumns and type", what, rows ? "rows, " : "");
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-}
-
-// values: whether the entries must have them (else they may be null)
-Entries entries_of(const spsyrk_entries* a, bool values, const char* name) {
-    if (!a) {
-        set_detail("%s is null", name);
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-    check_dims(a->nrows, a->ncols, name);
-    Entries e;
-    e.m = a->nrows;
-    e.n = a->ncols;
-    e.rp = a->row_ptr;
-    e.idx = a->col_idx;
-    e.ib = a->idx_bytes;
-    e.val = a->values;
-    e.vt = a->val_dtype;
-    if (e.rp) {
-        e.nnz = a->nnz;
-        check_aligned(e.rp, sizeof(int64_t), name);
-    } else {
-        // (the strides may be anything the caller's arrays hold; products of
-        // rows, entries and strides stay within 64 bits)
-        const int64_t most = int64_t(1) << 31;
-        require(a->per_row >= 0 && a->idx_stride >= 0 && a->val_stride >= 0 && a->idx_stride <= most &&
-                    a->val_stride <= most,
-                "rectangular rows: negative sizes or strides past 2^31");
-        e.per_row = a->per_row;
-        e.istride = a->idx_stride;
-        e.vstride = a->val_stride;
-        e.nnz = e.per_row > 0 && e.m > kLimit / e.per_row ? kLimit : e.m * e.per_row;
-    }
-    if (e.nnz < 0) {
-        set_detail("%s has a negative size", name);
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-    if (e.nnz >= kLimit) {
-        set_detail("%s: the entries must be below 2^31", name);
-        throw Fail{SPSYRK_ERR_SHAPE};
-    }
-    if ((e.ib != 4 && e.ib != 8) || !known_dtype(e.vt)) {
-        set_detail("%s: columns must be of 4 or 8 bytes and values of a known type", name);
-        throw Fail{SPSYRK_ERR_INVALID_ARG};
-    }
-    if (e.nnz > 0) {
-        if (!e.idx || (values && !e.val)) {
-            set_detail("%s: null col_idx%s", name, values ? " or values" : "");
-            throw Fail{SPSYRK_ERR_INVALID_ARG};
-        }
-        check_aligned(e.idx, size_t(e.ib), name);
-        if (e.val) check_aligned(e.val, size_t(dtype_bytes(e.vt)), name);
-    }
-    return e;
-}
-
-// tokens and CSR rows, as the lookup and its gradient take them
-Entries lookup_rows(const spsyrk_entries* A) {
-    const Entries e = entries_of(A, false, "A");
-    if (!e.rp) require(e.per_row == 1 && !e.val, "A: rectangular rows hold one entry each, without values");
-    return e;
-}
-
-void check_params(const DenseRows& X, const void* gamma, const void* other, int pt) {
-    require(pt == kDtF32 || pt == X.dt, "the parameters must be of 32-bit floats or of X's type");
-    if (gamma) check_aligned(gamma, size_t(dtype_bytes(pt)), "gamma");
-    if (other) check_aligned(other, size_t(dtype_bytes(pt)), "beta");
-}
-
-spsyrk_status rows_guarded(const spsyrk_allocator* al, void* stream, const std::function<void(Arena&, hipStream_t)>& f) {
-    spsyrk_csr_out unused;
-    return guarded(&unused, al, stream, f);
-}
-
-void distill_call(const spsyrk_dense* S, const spsyrk_entries* teacher, float temperature, const float* weight,
-                  float* loss, const spsyrk_dense* dS, Arena& ar, hipStream_t s) {
-    const DenseRows x = dense_rows(S, "S");
-    const Entries t = entries_of(teacher, true, "teacher");
-    require(t.m == x.m && t.n == x.n, "S and the teacher must agree in rows and columns");
-    require(temperature > 0.f && temperature <= 3.4e38f, "the temperature must be positive and finite");
-    DenseRows g;
-    if (dS) {
-        g = dense_rows(dS, "dS");
-        check_same(x, g, "S and dS", true);
-    }
-    if (x.m == 0) return;
-    require(loss != nullptr, "loss is null");
-    check_aligned(loss, sizeof(float), "loss");
-    if (weight) check_aligned(weight, sizeof(float), "weight");
-    const bool grad = dS && x.n > 0;
-    const size_t bytes = distill_tmp_bytes(x, grad);
-    void* tmp = bytes ? ar.get(bytes) : nullptr;
-    distill(x, t, temperature, weight, loss, grad ? g : DenseRows(), tmp, s);
-    check_launch();
-}
-
-}  // namespace
-
-extern "C" {
-
-spsyrk_status spsyrk_embed(const spsyrk_entries* A, const spsyrk_dense* W, float scale, const spsyrk_allocator* al,
-                           void* hip_stream, const spsyrk_dense* Y) {
-    return rows_guarded(al, hip_stream, [&](Arena& ar, hipStream_t s) {
-        const Entries a = lookup_rows(A);
-        const DenseRows w = dense_rows(W, "W"), y = dense_rows(Y, "Y");
-        require(a.n == w.m && a.m == y.m, "A must have W's rows as columns and Y's rows");
-        check_same(w, y, "W and Y", false);
-        if (y.m == 0 || y.n == 0) return;
-        if (!a.rp) {
-            embed_tokens(a, w, scale, y, s);
-        } else {
-            const size_t bytes = embed_csr_tmp_bytes(a.nnz, y.n);
-            embed_csr(a, w, scale, y, bytes ? ar.get(bytes) : nullptr, s);
-        }
-        check_launch();
-    });
-}
-
-spsyrk_status spsyrk_embed_grad(const spsyrk_entries* A, const spsyrk_dense* G, float scale,
-                                const spsyrk_allocator* al, void* hip_stream, const spsyrk_dense* dW) {
-    return rows_guarded(al, hip_stream, [&](Arena& ar, hipStream_t s) {
-        const Entries a = lookup_rows(A);
-        const DenseRows g = dense_rows(G, "G"), w = dense_rows(dW, "dW");
-        require(a.n == w.m && a.m == g.m, "A must have dW's rows as columns and G's rows");
-        check_same(g, w, "G and dW", false);
-        if (w.m == 0 || w.n == 0) return;
-        embed_grad(a, g, scale, w, ar.get(embed_grad_tmp_bytes(a, w.n)), s);
-        check_launch();
-    });
-}
-
-spsyrk_status spsyrk_layer_norm(const spsyrk_dense* X, const void* gamma, const void* beta, int param_dtype,
-                                float eps, void* hip_stream, const spsyrk_dense* Y, float* mean, float* rstd) {
-    return rows_guarded(nullptr, hip_stream, [&](Arena&, hipStream_t s) {
-        const DenseRows x = dense_rows(X, "X"), y = dense_rows(Y, "Y");
-        check_same(x, y, "X and Y", true);
-        check_params(x, gamma, beta, param_dtype);
-        require(x.n >= 1, "rows must have at least one column");
-        require(eps >= 0.f, "eps must not be negative");
-        if (x.m == 0) return;
-        require(mean && rstd, "mean or rstd is null");
-        check_aligned(mean, sizeof(float), "mean");
-        check_aligned(rstd, sizeof(float), "rstd");
-        layer_norm(x, gamma, beta, param_dtype, eps, y, mean, rstd, s);
-        check_launch();
-    });
-}
-
-spsyrk_status spsyrk_layer_norm_grad(const spsyrk_dense* G, const spsyrk_dense* X, const float* mean,
-                                     const float* rstd, const void* gamma, int param_dtype,
-                                     const spsyrk_allocator* al, void* hip_stream, const spsyrk_dense* dX,
-                                     void* dgamma, void* dbeta) {
-    return rows_guarded(al, hip_stream, [&](Arena& ar, hipStream_t s) {
-        const DenseRows g = dense_rows(G, "G"), x = dense_rows(X, "X"), dx = dense_rows(dX, "dX");
-        check_same(x, g, "X and G", true);
-        check_same(x, dx, "X and dX", true);
-        check_params(x, gamma, nullptr, param_dtype);
-        if (dgamma) check_aligned(dgamma, size_t(dtype_bytes(param_dtype)), "dgamma");
-        if (dbeta) check_aligned(dbeta, size_t(dtype_bytes(param_dtype)), "dbeta");
-        require(x.n >= 1, "rows must have at least one column");
-        if (x.m > 0) {
-            require(mean && rstd, "mean or rstd is null");
-            check_aligned(mean, sizeof(float), "mean");
-            check_aligned(rstd, sizeof(float), "rstd");
-        }
-        const size_t bytes = layer_norm_grad_tmp_bytes(x.m, x.n, x.dt, dgamma || dbeta);
-        if (x.m == 0 && !dgamma && !dbeta) return;
-        layer_norm_grad(g, x, mean, rstd, gamma, param_dtype, dx, dgamma, dbeta, bytes ? ar.get(bytes) : nullptr, s);
-        check_launch();
-    });
-}
-
-spsyrk_status spsyrk_distill(const spsyrk_dense* S, const spsyrk_entries* teacher, float temperature,
-                             const spsyrk_allocator* al, void* hip_stream, float* loss) {
-    return rows_guarded(al, hip_stream, [&](Arena& ar, hipStream_t s) {
-        distill_call(S, teacher, temperature, nullptr, loss, nullptr, ar, s);
-    });
-}
-
-spsyrk_status spsyrk_distill_grad(const spsyrk_dense* S, const spsyrk_entries* teacher, float temperature,
-                                  const float* weight, const spsyrk_allocator* al, void* hip_stream, float* loss,
-                                  const spsyrk_dense* dS) {
-    return rows_guarded(al, hip_stream, [&](Arena& ar, hipStream_t s) {
-        require(dS != nullptr, "dS is null");
-        distill_call(S, teacher, temperature, weight, loss, dS, ar, s);
-    });
-}
-
-}  // extern "C"
+#include "rows_api.inc"
