@@ -686,6 +686,42 @@ __global__ __launch_bounds__(kBlock) void sort_records(Entries A, uint32_t* __re
     }
 }
 
+// One launch for tokens that one workgroup holds: every group's workgroup reads
+// them all, one a thread, and sorts its own.
+template <typename I>
+__global__ __launch_bounds__(kSortBlock) void sort_few_tokens(Entries A, int groups, int lgbins,
+                                                              uint32_t* __restrict__ start, int part,
+                                                              uint32_t* __restrict__ key,
+                                                              uint32_t* __restrict__ row) {
+    __shared__ uint32_t hist[kSortWaves][kSortBins];
+    __shared__ uint32_t scratch[kSortWaves], lower_s[kSortWaves];
+    const int g = blockIdx.x, bins = 1 << lgbins, w = threadIdx.x / kWave;
+    const int64_t lo = int64_t(g) << lgbins, e = threadIdx.x;
+    int64_t t = e < A.nnz ? int64_t(static_cast<const I*>(A.idx)[e * A.istride]) : -1;
+    if (t >= A.n) t = -1;
+    for (int i = threadIdx.x; i < kSortWaves * bins; i += kSortBlock) hist[i >> lgbins][i & (bins - 1)] = 0;
+    const uint64_t lower = __ballot(t >= 0 && t < lo);
+    if (lane_id() == 0) lower_s[w] = __popcll(lower);
+    const bool in = t >= lo && t < lo + bins;
+    const uint32_t bin = in ? uint32_t(t - lo) : 0;
+    const uint64_t same = lanes_of(bin, lgbins, in);
+    const uint32_t rank = __popcll(same & lanemask_lt());
+    __syncthreads();
+    if (in && rank == 0) hist[w][bin] = __popcll(same);
+    uint32_t before = 0, end;
+#pragma unroll
+    for (int i = 0; i < kSortWaves; ++i) before += lower_s[i];
+    __syncthreads();
+    const uint32_t at = places(hist, bins, before, scratch, &end);
+    if (int(threadIdx.x) < bins && lo + threadIdx.x < A.n) start[lo + threadIdx.x] = at;
+    if (g == groups - 1 && threadIdx.x == 0) start[A.n] = end;
+    if (in) {
+        const uint32_t pos = hist[w][bin] + rank;
+        row[pos] = uint32_t(e);
+        if (pos % part == 0 || pos % part == part - 1 || pos == end - 1) key[pos] = uint32_t(t);
+    }
+}
+
 // log2 of the columns per group (-1: the entries go by the radix sort)
 inline int few_entries_bins(const Entries& A) {
     if (A.nnz > kFewEntries || A.n > int64_t(kSortBins) * kSortGroups) return -1;
@@ -781,15 +817,23 @@ void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRo
         auto split = [&](auto kernel) {
             kernel<<<tiles, kSortBlock, 0, s>>>(A, lgbins, groups, bits, rec, w[1], first);
         };
-        if (tiles > 0) {
+        const int part = int(sum_tile_entries(A.nnz));
+        const bool one = !A.rp && A.nnz <= kSortBlock;
+        if (one) {
+            auto sort = [&](auto kernel) {
+                kernel<<<groups, kSortBlock, 0, s>>>(A, groups, lgbins, start, part, key[0], row[0]);
+            };
+            A.ib == 4 ? sort(sort_few_tokens<int32_t>) : sort(sort_few_tokens<int64_t>);
+        } else if (tiles > 0) {
             if (tile == kSortBlock)
                 A.ib == 4 ? split(split_entries<int32_t, 1>) : split(split_entries<int64_t, 1>);
             else
                 A.ib == 4 ? split(split_entries<int32_t, kSortItems>) : split(split_entries<int64_t, kSortItems>);
         }
         // (row[0] and w[0] hold the pairs)
-        sort_groups<<<groups, kSortBlock, 0, s>>>(rec, w[1], first, tiles, tile, groups, lgbins, A.n, start,
-                                                  int(sum_tile_entries(A.nnz)), key[0], row[0]);
+        if (!one)
+            sort_groups<<<groups, kSortBlock, 0, s>>>(rec, w[1], first, tiles, tile, groups, lgbins, A.n, start, part,
+                                                      key[0], row[0]);
         if (A.val) {
             w[0] = reinterpret_cast<float*>(row[0]) + 1;
             step = 2;

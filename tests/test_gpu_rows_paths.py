@@ -37,6 +37,19 @@ def test_token_gradient_over_many_columns(v, kind):
     check(sp.embed_grad(tok.to(DEV), G.to(DEV), v), want, sums_tol(count, mag, want, torch.float32), kind)
 
 
+@pytest.mark.parametrize("n", [63, 1023, 1024, 1025])
+@pytest.mark.parametrize("v", [1, 255, 257, 3001, 262_145, 524_288])
+def test_token_gradient_of_few_tokens(n, v):
+    # up to 1024 tokens one launch sorts them
+    g = gen(n + v)
+    for tok in (torch.randint(-2, v + 2, (n,), generator=g), torch.full((n,), v - 1), torch.full((n,), v)):
+        G = normal((n, 6), torch.float32, g)
+        want, mag = ref.lookup_grad(torch.arange(n), tok, torch.ones(n, dtype=torch.float64), G.double(), v, 1.0)
+        count = torch.bincount(tok[(tok >= 0) & (tok < v)], minlength=v)[:, None]
+        for t in (tok.to(DEV), tok.int().to(DEV)):
+            check(sp.embed_grad(t, G.to(DEV), v), want, sums_tol(count, mag, want, torch.float32), "few tokens")
+
+
 @pytest.mark.parametrize("n", [131072, 131073, 400_009])
 def test_token_gradient_of_many_tokens(n):
     # tiles of 1024 tokens up to 2^17 of them, of 4096 past that
