@@ -63,8 +63,9 @@ def _vector(t, name, n, dtypes, device):
 
 
 def _same_device(device, t, name):
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
+    """device: an index, as get_device gives (-1: the host)."""
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on device {device}, not on {t.device}")
 
 
 def _entries_csr(A, values, name):
@@ -83,11 +84,11 @@ def _entries_csr(A, values, name):
             raise TypeError(f"{name}: values must be float32, float16 or bfloat16, not {v.dtype}")
         if v.numel() < A.nnz or not v.is_contiguous():
             raise ValueError(f"{name}: values must be contiguous, of at least nnz entries")
-        _same_device(A.row_ptr.device, v, f"{name}.values")
+        _same_device(A.row_ptr.get_device(), v, f"{name}.values")
         vp = v.data_ptr()
     elif values:
         raise TypeError(f"{name}: values are required")
-    _same_device(A.row_ptr.device, A.col_idx, f"{name}.col_idx")
+    _same_device(A.row_ptr.get_device(), A.col_idx, f"{name}.col_idx")
     return _sp._Entries(A.nrows, A.ncols, A.nnz, A.row_ptr.data_ptr(), 0, 0, 0, A.col_idx.data_ptr(),
                         A.col_idx.element_size(), vt, vp)
 
@@ -107,18 +108,20 @@ def _tokens(t, ncols, name):
 
 
 _local = threading.local()
-_raw_stream = torch._C._cuda_getCurrentRawStream  # (the handle alone: a Stream object costs 2 us of a call)
+# (the handle and the index alone: a Stream object costs 2 us of a call)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 
 def _arena(device):
-    """This thread's allocator for the device (its callbacks are made once; it
-    holds nothing between calls)."""
+    """This thread's allocator for the device of an index (its callbacks are made
+    once; it holds nothing between calls)."""
     arenas = getattr(_local, "arenas", None)
     if arenas is None:
         arenas = _local.arenas = {}
     arena = arenas.get(device)
     if arena is None:
-        arena = arenas[device] = _sp._TorchArena(device)
+        arena = arenas[device] = _sp._TorchArena(torch.device("cuda", device))
     return arena
 
 
@@ -129,7 +132,7 @@ def _on_device(position, name):
         @functools.wraps(fn)
         def call(*args, **kwargs):
             t = args[position] if len(args) > position else kwargs.get(name)
-            if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != _current_device():
                 with torch.cuda.device(t.device):
                     return fn(*args, **kwargs)
             return fn(*args, **kwargs)
@@ -155,17 +158,18 @@ def embed(rows, weight, scale=1.0):
     w = _rows(weight, "weight")
     if weight.dim() != 2:
         raise ValueError("weight must be v x d")
+    dev = weight.get_device()
     if isinstance(rows, torch.Tensor):
         a, csr, shape = _tokens(rows, w.nrows, "rows"), False, rows.shape
-        _same_device(weight.device, rows, "rows")
+        _same_device(dev, rows, "rows")
     else:
         a, csr, shape = _entries_csr(rows, False, "rows"), True, (rows.nrows,)
-        _same_device(weight.device, rows.row_ptr, "rows")
+        _same_device(dev, rows.row_ptr, "rows")
     out = torch.empty((*shape, w.ncols), dtype=weight.dtype, device=weight.device)
     y = _sp._Dense(a.nrows, w.ncols, w.ncols, w.dtype, out.data_ptr())
-    arena = _arena(weight.device) if csr else None
+    arena = _arena(dev) if csr else None
     _check(lib.spsyrk_embed(_byref(a), _byref(w), scale, _byref(arena.struct) if csr else None,
-                            _raw_stream(weight.device.index), _byref(y)), arena)
+                            _raw_stream(dev), _byref(y)), arena)
     return out
 
 
@@ -175,16 +179,16 @@ def embed_grad(rows, grad, v, scale=1.0):
     scale)`` for the gradient ``grad`` of its result: ``scale * A.T @ grad``,
     summed by entries sorted by column (spsyrk_embed_grad)."""
     lib = _sp._lib or _sp.library()
-    g = _rows(grad, "grad")
+    g, dev = _rows(grad, "grad"), grad.get_device()
     if isinstance(rows, torch.Tensor):
         a, first = _tokens(rows, v, "rows"), rows
     else:
         a, first = _entries_csr(rows, False, "rows"), rows.row_ptr
-    _same_device(grad.device, first, "rows")
+    _same_device(dev, first, "rows")
     out = torch.empty((v, g.ncols), dtype=grad.dtype, device=grad.device)
     w = _sp._Dense(v, g.ncols, g.ncols, g.dtype, out.data_ptr())
-    arena = _arena(grad.device)
-    _check(lib.spsyrk_embed_grad(_byref(a), _byref(g), scale, _byref(arena.struct), _raw_stream(grad.device.index),
+    arena = _arena(dev)
+    _check(lib.spsyrk_embed_grad(_byref(a), _byref(g), scale, _byref(arena.struct), _raw_stream(dev),
                                  _byref(w)), arena)
     return out
 
@@ -195,7 +199,8 @@ def _params(x, d, weight, bias, what):
     pt = x.dtype if first is None else first.dtype
     if pt not in (torch.float32, x.dtype):
         raise TypeError(f"{what}: weight and bias must be float32 or {x.dtype}, not {pt}")
-    return (_DTYPE[pt], _vector(weight, "weight", d, (pt,), x.device), _vector(bias, "bias", d, (pt,), x.device))
+    return (_DTYPE[pt], _vector(weight, "weight", d, (pt,), x.get_device()),
+            _vector(bias, "bias", d, (pt,), x.get_device()))
 
 
 @_on_device(0, "x")
@@ -210,7 +215,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
     o = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, y.data_ptr())
-    _check(lib.spsyrk_layer_norm(_byref(a), wp, bp, pt, eps, _raw_stream(x.device.index), _byref(o),
+    _check(lib.spsyrk_layer_norm(_byref(a), wp, bp, pt, eps, _raw_stream(x.get_device()), _byref(o),
                                  mean.data_ptr(), rstd.data_ptr()))
     return y, mean, rstd
 
@@ -224,17 +229,17 @@ def layer_norm_grad(grad, x, mean, rstd, weight=None, bias=None):
     g, a = _rows(grad, "grad"), _rows(x, "x")
     if grad.shape != x.shape:
         raise ValueError("grad and x must have one shape")
-    _same_device(x.device, grad, "grad")
+    _same_device(x.get_device(), grad, "grad")
     pt, wp, _ = _params(x, a.ncols, weight, bias, "layer_norm_grad")
-    mp = _vector(mean, "mean", a.nrows, (torch.float32,), x.device)
-    rp = _vector(rstd, "rstd", a.nrows, (torch.float32,), x.device)
+    mp = _vector(mean, "mean", a.nrows, (torch.float32,), x.get_device())
+    rp = _vector(rstd, "rstd", a.nrows, (torch.float32,), x.get_device())
     dx = _like(x)
     dw = None if weight is None else torch.empty_like(weight)
     db = None if bias is None else torch.empty_like(bias)
     o = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, dx.data_ptr())
-    arena = _arena(x.device)
+    arena = _arena(x.get_device())
     _check(lib.spsyrk_layer_norm_grad(_byref(g), _byref(a), mp, rp, wp, pt, _byref(arena.struct),
-                                      _raw_stream(x.device.index), _byref(o),
+                                      _raw_stream(x.get_device()), _byref(o),
                                       None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()),
            arena)
     return dx, dw, db
@@ -244,15 +249,15 @@ def _teacher(teacher, s, logits):
     """_Entries of a DeviceCSR, or of a (values, indices) pair with the logits' leading dimensions."""
     if not isinstance(teacher, tuple):
         e = _entries_csr(teacher, True, "teacher")
-        _same_device(logits.device, teacher.row_ptr, "teacher")
+        _same_device(logits.get_device(), teacher.row_ptr, "teacher")
         return e
     values, indices = teacher
     if values.shape != indices.shape or values.shape[:-1] != logits.shape[:-1]:
         raise ValueError("the teacher's values and indices must have one shape, and the logits' leading dimensions")
     if indices.dtype not in (torch.int32, torch.int64):
         raise TypeError(f"the teacher's indices must be int32 or int64, not {indices.dtype}")
-    _same_device(logits.device, values, "teacher values")
-    _same_device(logits.device, indices, "teacher indices")
+    _same_device(logits.get_device(), values, "teacher values")
+    _same_device(logits.get_device(), indices, "teacher indices")
     v = _rows(values, "teacher values")
     k = v.ncols
     stride = k
@@ -275,9 +280,9 @@ def distill(logits, teacher, temperature=1.0):
     s = _rows(logits, "logits")
     t = _teacher(teacher, s, logits)
     loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
-    arena = _arena(logits.device)
+    arena = _arena(logits.get_device())
     _check(lib.spsyrk_distill(_byref(s), _byref(t), temperature, _byref(arena.struct),
-                              _raw_stream(logits.device.index), loss.data_ptr()), arena)
+                              _raw_stream(logits.get_device()), loss.data_ptr()), arena)
     return loss
 
 
@@ -289,11 +294,11 @@ def distill_grad(logits, teacher, temperature=1.0, weight=None):
     lib = _sp._lib or _sp.library()
     s = _rows(logits, "logits")
     t = _teacher(teacher, s, logits)
-    wp = _vector(weight, "weight", s.nrows, (torch.float32,), logits.device)
+    wp = _vector(weight, "weight", s.nrows, (torch.float32,), logits.get_device())
     loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
     grad = _like(logits)
     g = _sp._Dense(s.nrows, s.ncols, s.ncols, s.dtype, grad.data_ptr())
-    arena = _arena(logits.device)
+    arena = _arena(logits.get_device())
     _check(lib.spsyrk_distill_grad(_byref(s), _byref(t), temperature, wp, _byref(arena.struct),
-                                   _raw_stream(logits.device.index), loss.data_ptr(), _byref(g)), arena)
+                                   _raw_stream(logits.get_device()), loss.data_ptr(), _byref(g)), arena)
     return loss, grad
