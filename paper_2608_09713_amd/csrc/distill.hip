@@ -578,7 +578,9 @@ void distill(const DenseRows& S, const Entries& t, float temperature, const floa
                     if (nt < kRowBlock) return launch(integral_constant<int, 8>(), any, 16);
                     return launch(integral_constant<int, 8>(), most, 16);
                 }
+                if (packs <= 10 * nt) return launch(integral_constant<int, 10>(), most, 16);
                 if (packs <= 12 * nt) return launch(integral_constant<int, 12>(), most, 16);
+                if (packs <= 14 * nt) return launch(integral_constant<int, 14>(), most, 16);
                 return launch(integral_constant<int, kFusedPacks>(), most, 16);
             }
         }

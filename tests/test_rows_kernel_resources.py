@@ -18,7 +18,7 @@ def test_distillation_budgets():
     ks = _report("distill.hip")
     fused = {k: v for k, v in ks.items() if "distill_fused" in k}
     rows = {k: v for k, v in ks.items() if "distill_rows" in k}
-    assert len(fused) == 24 and len(rows) == 9
+    assert len(fused) == 30 and len(rows) == 9
     for name, r in fused.items():
         assert r["ScratchSize"] == 0 and r["VGPRs"] <= 128, (name, r)
     for name, r in rows.items():
