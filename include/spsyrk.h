@@ -424,7 +424,7 @@ spsyrk_status spsyrk_layer_norm_grad(const spsyrk_dense* G, const spsyrk_dense* 
  * of values / T over a row's entries,
  *     loss[r] = T^2 sum over the row's entries of p (log p - log q),
  * T^2 times the divergence of p from q on the entries' columns.  T =
- * temperature, finite and positive.  Logits of -inf have q = 0; a row without
+ * temperature, positive and neither denormal nor infinite.  Logits of -inf have q = 0; a row without
  * entries, one whose teacher values are all -inf and one whose logits are all
  * -inf have loss 0.  NaN or +inf in a row's logits or teacher values make its
  * loss NaN.  loss: m floats.

@@ -109,6 +109,13 @@ def test_distill(lib):
     assert loss(dense(1 << 30, 16), tokens(m=1 << 30, per=4, values=P)) == SHAPE
 
 
+def test_distill_temperatures_without_a_reciprocal(lib):
+    s, t = dense(4, 16), csr(values=P)
+    for T in (1e-40, 1.17e-38, -1e-40):
+        assert lib.spsyrk_distill(ref(s), ref(t), T, None, None, P) == INVALID
+        assert lib.spsyrk_distill_grad(ref(s), ref(t), T, None, None, None, P, ref(s)) == INVALID
+
+
 def test_binding():
     x = torch.zeros((4, 8))
     tok = torch.zeros(4, dtype=torch.int64)
