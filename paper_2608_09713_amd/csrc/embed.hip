@@ -10,12 +10,13 @@
 // is the same on every run).  Sums are held in 32-bit floats and rounded once.
 //
 // A wavefront takes a target's columns 16 bytes a lane, several entries' rows
-// at once (two packs a lane of four: 355 us against 325 with one pack of
-// eight, 65536 tokens over 131072 x 4096 bf16); targets of narrow rows share a wavefront.  A target of more
-// than a tile of entries (a frequent token) would be walked by one wavefront:
-// such targets are left to a second launch, in which every tile of entries
-// sums its part of the (at most two) long targets that reach into it, and a
-// third adds a target's parts in tile order.
+// at once (two packs a lane of four entries: 355 us against 325 with one pack
+// of eight, 65536 tokens over 131072 x 4096 bf16); targets of narrow rows share
+// a wavefront.  A target of more than a tile of entries (a frequent token)
+// would be walked by one wavefront: the first workgroups of the same launch
+// take tiles of entries instead, each of which sums its part of the (at most
+// two) long targets that reach into it, and a second launch adds a target's
+// parts in tile order.
 #include <algorithm>
 
 #include "internal.h"
@@ -442,7 +443,7 @@ __global__ __launch_bounds__(kBlock) void column_bounds(const uint32_t* __restri
 // Up to kFewEntries entries over up to 2^19 columns are sorted in two launches,
 // against three or four per digit and two more of the radix sort, which for so
 // few records is mostly launches and latency (65536 tokens of 131072: 17 us,
-// 65 by digits; 1.57 M weighted CSR entries of 200003: %s).
+// 65 by digits; 1.57 M weighted CSR entries of 200003: 67 us, 121 by digits).
 // The columns are dealt to at most kSortGroups groups of consecutive columns.
 // First, tiles of entries are split by group (stable, padding left out), with
 // every tile's first record of every group; then one workgroup per group takes
