@@ -10,7 +10,7 @@ import torch
 
 import paper_2608_09713_amd as sp
 from tests import rows_reference as ref
-from tests.test_gpu_rows import DEV, DTYPES, ROUND, TINY, U, check, check_distill, csr, gen, normal, sums_tol
+from tests.test_gpu_rows import DEV, DTYPES, K, ROUND, TINY, U, check, check_distill, csr, gen, normal, sums_tol
 
 pytestmark = pytest.mark.gpu
 
@@ -204,6 +204,37 @@ def test_distill_row_shapes(dtype, v):
     assert torch.equal(loss, sp.distill(s.to(DEV), (vals.to(DEV), cols.to(DEV)), 1.0))
     pick = list(range(0, m, max(1, m // 40)))
     check_distill(s[pick], [(cols[r], vals[r]) for r in pick], 1.0, w[pick], loss.cpu()[pick], grad.cpu()[pick], "shapes")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,packs", [(13_001, 26), (13_001, 300), (2600, 2047), (600, 8001), (600, 9251), (600, 11251),
+                                     (600, 13251), (300, 16001)])
+def test_distill_workgroups_take_many_rows(dtype, m, packs):
+    """More rows than the chip holds at once, at every number of packs per thread,
+    and rows that lie at other distances from a boundary than the ones before."""
+    v = packs * (16 // (torch.finfo(dtype).bits // 8)) - 3
+    g = torch.Generator(DEV).manual_seed(packs)
+    k = 20
+    s = torch.randn((m, v), generator=g, device=DEV).mul_(2.0).to(dtype)
+    # (at most one entry a stretch of columns, some of them at the row's ends)
+    cols = torch.arange(k, device=DEV) * (v // k) + torch.randint(0, v // k, (m, k), generator=g, device=DEV)
+    cols[::2, 0], cols[::2, k - 1] = 0, v - 1
+    vals = torch.randn((m, k), generator=g, device=DEV).to(dtype)
+    w = torch.rand(m, generator=g, device=DEV)
+    w[::7] = 0.0
+    loss, grad = sp.distill_grad(s, (vals, cols), 2.0, w)
+    assert torch.equal(loss, sp.distill(s, (vals, cols), 2.0))
+    pick = sorted({0, 1, 255, 256, 257, m // 2, m // 2 + 1, m - 258, m - 257, m - 2, m - 1} & set(range(m)))
+    rows = [(cols[r].cpu(), vals[r].cpu()) for r in pick]
+    check_distill(s[pick].cpu(), rows, 2.0, w[pick].cpu(), loss[pick].cpu(), grad[pick].cpu(), "many rows")
+    # every row of the gradient sums to nothing, up to the sum of its elements'
+    # bars (as in check_distill: z <= 11, a spread of 5 and sums of q and p of 1)
+    total, size = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    for r in range(0, m, 100):
+        part = grad[r:r + 100].double()
+        total[r:r + 100], size[r:r + 100] = part.sum(1).abs(), part.abs().sum(1)
+    bar = ROUND[dtype] * size + w * 2.0 * U * (4 * 11 + K + 4 * 5 + K + k) + v * TINY[dtype]
+    assert bool((total <= bar).all()), int((total > bar).sum())
 
 
 def test_distill_more_entries_than_threads_by_row():
