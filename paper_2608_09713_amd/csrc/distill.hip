@@ -578,6 +578,8 @@ void distill(const DenseRows& S, const Entries& t, float temperature, const floa
                     if (nt < kRowBlock) return launch(integral_constant<int, 8>(), any, 16);
                     return launch(integral_constant<int, 8>(), most, 16);
                 }
+                // (a pack that no thread needs costs its place in the loops: 8192 x
+                // 65537 bf16, 8193 packs, 486 us with ten a thread, 513 with twelve)
                 if (packs <= 10 * nt) return launch(integral_constant<int, 10>(), most, 16);
                 if (packs <= 12 * nt) return launch(integral_constant<int, 12>(), most, 16);
                 if (packs <= 14 * nt) return launch(integral_constant<int, 14>(), most, 16);
