@@ -353,21 +353,33 @@ __global__ __launch_bounds__(kBlock) void join_tiles(Sums<T, P> a) {
     }
 }
 
-// Entries per tile: 64, doubled for every fourfold of 2^16 entries, so that
-// neither a tile nor the parts of one target grow past the square root of
-// the entries by much.
-inline int64_t sum_tile_entries(int64_t nnz) {
-    int64_t t = 64;
-    while (t * t * 16 < nnz) t *= 2;
+// Entries per tile: 64 for up to 2^16 entries, doubled for every fourfold of
+// them, so that neither a tile nor the parts of one target grow past the square
+// root of the entries by much.
+inline int64_t doubled(int64_t t, int64_t per, int64_t nnz) {
+    while (t * t * per < nnz) t *= 2;
     return t;
+}
+inline int64_t row_tile(int64_t nnz) { return doubled(64, 16, nnz); }
+
+// The gradient's tiles start at 16: a frequent token's column, or a tile of it,
+// is a chain of reads, and short chains are what few entries need (4096 tokens
+// over 32000 x 64 bf16: 37 us with 64, 23 with 16; 8192 over 32000 x 4096: 141
+// and 135).  Rows of up to 256 columns, whose parts cost little, keep tiles half
+// as long (30000 tokens over 100000 x 64 bf16: 43 us, 37 so; 1.57 M entries over
+// 3000 x 250 f32: 337 and 296; but 8192 tokens over 32000 x 4096: 134 and 136).
+// Up to 1024 entries few columns are long, and parts cost more than they save
+// (512 tokens over 50000 x 1024: 26.3 us, 27.2 with tiles of 16).  Rows of a
+// CSR keep to the longer tiles, as typical ones would otherwise go through parts.
+inline int64_t column_tile(int64_t nnz, int64_t d) {
+    return nnz <= 1024 ? row_tile(nnz) : doubled(16, d <= 256 ? 64 : 16, nnz);
 }
 
 inline size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 
 inline int64_t part_columns(int64_t d) { return (d + 3) & ~int64_t(3); }
 
-inline size_t part_bytes(int64_t nnz, int64_t d) {
-    const int64_t tile = sum_tile_entries(nnz);
+inline size_t part_bytes(int64_t nnz, int64_t tile, int64_t d) {
     if (nnz <= tile) return 0;
     const size_t rows = size_t((nnz + tile - 1) / tile) * 2;
     return round256(rows * size_t(part_columns(d)) * sizeof(float)) + round256(rows * sizeof(int32_t));
@@ -375,7 +387,7 @@ inline size_t part_bytes(int64_t nnz, int64_t d) {
 
 template <typename T, int N, typename P>
 void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const DenseRows& out, void* tmp,
-                 int64_t packs, int lg, hipStream_t s) {
+                 int64_t tile, int64_t packs, int lg, hipStream_t s) {
     Sums<T, P> a;
     a.t = t;
     a.src = static_cast<const T*>(src.p);
@@ -388,7 +400,7 @@ void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const D
     a.lg = lg;
     a.chunks = (packs + (int64_t(1) << lg) - 1) >> lg;
     const int64_t rows = kWave >> lg;
-    a.tile = sum_tile_entries(t.nnz);
+    a.tile = tile;
     a.ntiles = t.nnz > a.tile ? (t.nnz + a.tile - 1) / a.tile : 0;  // (no target is long)
     a.dp = part_columns(a.d);
     a.part = static_cast<float*>(tmp);
@@ -406,13 +418,13 @@ void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const D
 
 template <typename P>
 void grouped_sums(const Targets<P>& t, const DenseRows& src, float scale, const DenseRows& out, void* tmp,
-                  hipStream_t s) {
+                  int64_t tile, hipStream_t s) {
     by_width(out.dt, out.n, [&](auto e, auto width) {
         using T = decltype(e);
         constexpr int N = decltype(width)::value;
         const int64_t packs = (out.n + N - 1) / N;
         const int lg = lane_bits(packs);
-        launch_sums<T, N, P>(t, src, scale, out, tmp, packs, lg, s);
+        launch_sums<T, N, P>(t, src, scale, out, tmp, tile, packs, lg, s);
     });
 }
 
@@ -760,11 +772,13 @@ void embed_tokens(const Entries& A, const DenseRows& W, float scale, const Dense
     });
 }
 
-size_t embed_csr_tmp_bytes(int64_t nnz, int64_t d) { return part_bytes(nnz, d); }
+size_t embed_csr_tmp_bytes(int64_t nnz, int64_t d) {
+    return part_bytes(nnz, row_tile(nnz), d);
+}
 
 void embed_csr(const Entries& A, const DenseRows& W, float scale, const DenseRows& Y, void* tmp, hipStream_t s) {
     Targets<int64_t> t{A.rp, A.m, A.nnz, A.idx, A.ib, A.val, A.vt, nullptr, 1};
-    grouped_sums(t, W, scale, Y, tmp, s);
+    grouped_sums(t, W, scale, Y, tmp, row_tile(A.nnz), s);
 }
 
 // entries per tile of the two-launch sort
@@ -786,7 +800,7 @@ static size_t sort_buffer_bytes(int64_t nnz) {
 
 size_t embed_grad_tmp_bytes(const Entries& A, int64_t d) {
     return sort_buffer_bytes(A.nnz) * (A.val ? 6 : 4) + round256(size_t(A.n + 1) * sizeof(uint32_t)) +
-           sort_scratch_bytes(A) + part_bytes(A.nnz, d);
+           sort_scratch_bytes(A) + part_bytes(A.nnz, column_tile(A.nnz, d), d);
 }
 
 void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRows& dW, void* tmp, hipStream_t s) {
@@ -806,6 +820,7 @@ void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRo
         w[i] = A.val ? reinterpret_cast<float*>(take(words)) : nullptr;
     }
     void* sort_tmp = take(sort_scratch_bytes(A));
+    const int64_t sums_tile = column_tile(A.nnz, dW.n);
     int which = 0, step = 1;
     const int lgbins = few_entries_bins(A);
     if (lgbins >= 0) {
@@ -818,7 +833,7 @@ void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRo
         auto split = [&](auto kernel) {
             kernel<<<tiles, kSortBlock, 0, s>>>(A, lgbins, groups, bits, rec, w[1], first);
         };
-        const int part = int(sum_tile_entries(A.nnz));
+        const int part = int(sums_tile);
         const bool one = !A.rp && A.nnz <= kSortBlock;
         if (one) {
             auto sort = [&](auto kernel) {
@@ -846,7 +861,7 @@ void embed_grad(const Entries& A, const DenseRows& G, float scale, const DenseRo
     }
     if (lgbins < 0) column_bounds<<<thread_grid(A.n + 1), kBlock, 0, s>>>(key[which], A.nnz, A.n, start);
     Targets<uint32_t> t{start, A.n, A.nnz, row[which], 4, w[which], kDtF32, key[which], step};
-    grouped_sums(t, G, scale, dW, at, s);
+    grouped_sums(t, G, scale, dW, at, sums_tile, s);
 }
 
 }  // namespace spsyrk
