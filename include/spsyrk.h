@@ -424,10 +424,12 @@ spsyrk_status spsyrk_layer_norm_grad(const spsyrk_dense* G, const spsyrk_dense* 
  * of values / T over a row's entries,
  *     loss[r] = T^2 sum over the row's entries of p (log p - log q),
  * T^2 times the divergence of p from q on the entries' columns.  T =
- * temperature, positive and neither denormal nor infinite.  Logits of -inf have q = 0; a row without
- * entries, one whose teacher values are all -inf and one whose logits are all
- * -inf have loss 0.  NaN or +inf in a row's logits or teacher values make its
- * loss NaN.  loss: m floats.
+ * temperature, positive and neither denormal nor infinite.  Logits may be of
+ * any finite magnitude (large negative ones as masks); where the difference to
+ * the row's maximum, divided by T, leaves the floats' range, the logit counts
+ * as -inf.  Logits of -inf have q = 0; a row without entries, one whose teacher
+ * values are all -inf and one whose logits are all -inf have loss 0.  NaN or
+ * +inf in a row's logits or teacher values make its loss NaN.  loss: m floats.
  */
 spsyrk_status spsyrk_distill(const spsyrk_dense* S, const spsyrk_entries* teacher, float temperature,
                              const spsyrk_allocator* al, void* hip_stream, float* loss);

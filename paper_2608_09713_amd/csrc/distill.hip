@@ -36,8 +36,8 @@ constexpr int kCus = 256;  // compute units of the chip
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct RowStat {
-    // log2 q = (s - m0) c - b0 - l2: b0 is max c, or m0 the maximum; l2 is log2
-    // of the sum of exponentials relative to it, `sum`
+    // log2 q = (s - m0) c - b0 - l2: b0 is the maximum's base, or m0 the
+    // maximum; l2 is log2 of the sum of exponentials relative to it, `sum`
     float m0, b0, l2, sum;
     float tm, tl2;  // maximum and log2 of the sum of the teacher's entries
     float scale;    // weight T, 0 for a row without a gradient
@@ -93,21 +93,26 @@ __device__ inline void add_value(MaxSum& a, float x, float c) {
 // (NaN sums are something: only rows of nothing but -inf are empty)
 __device__ inline bool is_empty(MaxSum a) { return a.m == -INFINITY && a.s == 0.f; }
 
-// Sums over the logits are formed with s c - fl(max c), one operation: the
-// rounding of max c is a factor common to all exponentials and to their sum,
-// and leaves q = 2^(s c - fl(max c)) / sum as it is.  Only where max c leaves
-// the floats' range (logits near their largest or lowest value) would that not
-// do: such rows are done again from memory, differences first.
-__device__ inline float base_of(float m, float c) { return m * c == -INFINITY ? 0.f : m * c; }
+// Sums over the logits are formed with s c - b, one operation, where the base b
+// of a maximum is fl(max c): its rounding, a power of two 2^r with |r| up to half
+// an ulp of max c, is a factor common to all exponentials and to their sum, and
+// leaves q = 2^(s c - b) / sum as it is as long as 2^r is moderate.  So the
+// bases end at 2^24, where r is a half.  Below -2^24 (logits masked by a large
+// finite value) the base stays there: the exponents are then what they are,
+// negative and exact, and go to 0 under a later, ordinary maximum.  Rows whose
+// own maximum lies past 2^24 in either direction are done again from memory,
+// differences first.  (A maximum of -inf has the lowest base too: 2^-inf is 0.)
+constexpr float kMostBase = 16777216.f;
+__device__ inline float base_of(float m, float c) { return fmaxf(m * c, -kMostBase); }
 __device__ inline float scaled_base(MaxSum a, float m, float c) {
-    return a.m * c == -INFINITY ? a.s : a.s * exp2_of(a.m * c - m * c);
+    return a.s * exp2_of(base_of(a.m, c) - base_of(m, c));
 }
 __device__ inline MaxSum wave_merge_base(MaxSum a, float c) {
     const float m = wave_max(a.m);
     return {m, wave_total(scaled_base(a, m, c))};
 }
 __device__ inline bool out_of_range(float m, float c) {
-    return fabsf(m) < INFINITY && !(fabsf(m * c) < 1e30f);
+    return fabsf(m) < INFINITY && !(fabsf(m * c) < kMostBase);
 }
 template <typename T, int N>
 __device__ inline void add_pack_base(MaxSum& a, Vec<T, N> v, int shift, float c) {
