@@ -537,11 +537,12 @@ inline size_t fused_lds_bytes(int threads, int width) { return size_t(threads) *
 
 // Threads per row: eight packs each, so that many rows are on a compute unit
 // (more than eight where that takes over kRowBlock threads), but one per entry
-// of a typical row at least.  Loss and gradient take the same number, so that
+// of a typical row at least (and one wavefront where there is neither: rows of
+// no columns have losses too).  Loss and gradient take the same number, so that
 // they sum in one order.
 inline int row_threads(int64_t packs, const Entries& t) {
     const int64_t entries = t.rp ? 2 * (t.nnz / std::max<int64_t>(t.m, 1)) : t.per_row;
-    const int64_t n = std::max(ceil_div(packs, 8), std::min<int64_t>(entries, 256));
+    const int64_t n = std::max({ceil_div(packs, 8), std::min<int64_t>(entries, 256), int64_t(1)});
     // (whole rounds of the four SIMDs: loss over 8192 x 60000 bf16 with 15
     // wavefronts a row 259 us, with 16 205)
     const int64_t unit = n > 4 * kWave ? 4 * kWave : kWave;

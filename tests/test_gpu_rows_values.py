@@ -106,3 +106,24 @@ def test_small_temperatures(dtype, v):
     cols[2, 0], vals[2, 0] = s[2].float().argmax(), 20.0
     for T in (2.0 ** -10, 2.0 ** -20, 2.0 ** -30):
         check_both(s, vals, cols, T, "small temperature")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_no_columns(dtype):
+    """Rows of no columns have nothing to match, with and without entries."""
+    S = torch.zeros((5, 0), dtype=dtype, device=DEV)
+
+    def rows(lens):
+        rp = torch.tensor([0] + lens, device=DEV).cumsum(0)
+        nnz = sum(lens)
+        return sp.DeviceCSR(5, 0, rp, torch.zeros(nnz, dtype=torch.int32, device=DEV),
+                            torch.ones(nnz, device=DEV), nnz)
+
+    def pair(k):
+        return torch.ones((5, k), device=DEV), torch.zeros((5, k), dtype=torch.int64, device=DEV)
+
+    for teacher in (pair(0), pair(1), pair(300), rows([0] * 5), rows([0, 1, 0, 0, 0]), rows([9] * 5)):
+        loss = sp.distill(S, teacher)
+        assert loss.shape == (5,) and not loss.any()
+        loss, grad = sp.distill_grad(S, teacher, 2.0, torch.ones(5, device=DEV))
+        assert loss.shape == (5,) and not loss.any() and grad.shape == (5, 0) and grad.dtype == dtype
