@@ -380,7 +380,7 @@ __global__ __launch_bounds__(kRowBlock) void distill_fused(const T* S, int64_t l
     extern __shared__ int lists[];  // fused_lds_bytes(NT, N)
     int* const head = lists;               // first entry of a thread's columns (-1: none)
     int* const link = head + NT;           // of an entry: its pack in the thread << 16 | the next entry + 1
-    int* const col_s = link + NT;
+    int* const col_s = link + NT;          // or -1 - the entry that stands for it
     float* const p_s = reinterpret_cast<float*>(col_s + NT);
     float* const lq_s = p_s + NT;
     float* const dense = lq_s + NT;        // NT N
@@ -454,10 +454,27 @@ __global__ __launch_bounds__(kRowBlock) void distill_fused(const T* S, int64_t l
         }
         lds_barrier();
         ahead = entry(enext);
-        // the packs of this thread that have entries
+        // The packs of this thread that have entries.  Entries of one column are
+        // added up at the one that the list has first (of two, the sum has one
+        // value in either order, and the list may have either), and leave it: of
+        // their column stays where its logit will be found.
         uint32_t packs = 0;
         const int first = head[tid];
-        for (int x = first; x >= 0; x = (link[x] & 0xffff) - 1) packs |= 1u << (link[x] >> 16);
+        for (int x = first, before = -1; x >= 0;) {
+            const int l = link[x], k = l >> 16;
+            int y = x;
+            if (packs >> k & 1)
+                for (y = first; col_s[y] != col_s[x];) y = (link[y] & 0xffff) - 1;
+            if (y == x) {
+                packs |= 1u << k;
+                before = x;
+            } else {
+                p_s[y] += p_s[x];
+                col_s[x] = -1 - y;
+                link[before] = (link[before] & ~0xffff) | (l & 0xffff);
+            }
+            x = (l & 0xffff) - 1;
+        }
         // The next row's packs.  After the last row these are loads of nothing new:
         // under a condition they would have the sums wait for all packs at once.
         const T* const next = S + (more ? r + step : r) * lds;
@@ -514,7 +531,7 @@ __global__ __launch_bounds__(kRowBlock) void distill_fused(const T* S, int64_t l
             if (!listed || far)
                 teacher_loss<T>(x, t, e, tid, row, V, c, st);
             else if (col >= 0)
-                x = loss_term(p, lp, lq_s[tid]);
+                x = loss_term(p, lp, lq_s[col_s[tid] < 0 ? -1 - col_s[tid] : tid]);
         }
         x = wave_total(x);
         if (lane_id() == 0) lsum[w] = x;

@@ -127,3 +127,51 @@ def test_no_columns(dtype):
         assert loss.shape == (5,) and not loss.any()
         loss, grad = sp.distill_grad(S, teacher, 2.0, torch.ones(5, device=DEV))
         assert loss.shape == (5,) and not loss.any() and grad.shape == (5, 0) and grad.dtype == dtype
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("v", WIDTHS)
+def test_order_of_two_listings(dtype, v):
+    """A column listed twice in a row: the gradient has the same bits whichever
+    listing comes first, near each other or in different wavefronts' entries.
+
+    With log2(e) / T = 1 and whole teacher values the row's exponentials are
+    powers of two and their sum is exact, so that p itself has no order."""
+    g = gen(v + 4)
+    m, k, twice = 400, 100, 30
+    T = float(torch.tensor(1.4426950408889634))
+    s = normal((m, v), dtype, g, 2.0)
+    one = torch.rand((m, k - twice), generator=g).mul_(v).long().clamp_(max=v - 1)
+    cols = torch.cat([one, one[:, :twice]], 1)
+    vals = torch.randint(-9, 1, (m, k), generator=g).float()
+    other = torch.arange(k)
+    other[:twice], other[k - twice:] = torch.arange(k - twice, k), torch.arange(twice)
+    S = s.to(DEV)
+    loss, grad = sp.distill_grad(S, (vals.to(DEV), cols.to(DEV)), T)
+    # the two listings' values change places
+    swapped = sp.distill_grad(S, (vals[:, other].to(DEV), cols.to(DEV)), T)
+    assert bool((cols[:, other] == cols).all())
+    # columns that are listed three times or more have no such promise
+    count = torch.zeros((m, v)).scatter_add_(1, cols, torch.ones((m, k)))
+    kept = (count < 3).to(DEV)
+    assert int((count == 2).sum()) > 100
+    assert torch.equal(grad[kept], swapped[1][kept])
+    for _ in range(3):
+        again = sp.distill_grad(S, (vals.to(DEV), cols.to(DEV)), T)
+        assert torch.equal(again[0], loss) and torch.equal(again[1][kept], grad[kept])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("v", WIDTHS)
+def test_columns_listed_often(dtype, v):
+    """Rows filled up with one column, without mass or with it, and rows of few columns in turn."""
+    g = gen(v + 5)
+    k = 200
+    s = normal((4, v), dtype, g, 2.0)
+    cols = torch.stack([torch.randperm(v, generator=g)[:50].repeat(4) for _ in range(4)])
+    vals = normal((4, k), torch.float32, g)
+    cols[0, 20:], vals[0, 20:] = 0, -math.inf
+    cols[1, 20:] = 0
+    cols[2] = torch.arange(k) % 5
+    cols[3] = torch.arange(k) // 40
+    check_both(s, vals, cols, 1.0, "listed often")
