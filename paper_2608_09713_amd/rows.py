@@ -40,7 +40,7 @@ def _rows(t, name):
         v = t.view(-1, cols) if t.dim() != 2 else t
     except RuntimeError:
         v = None
-    if v is None or v.stride(1) != 1 or (v.shape[0] > 1 and v.stride(0) < cols):
+    if v is None or (cols > 1 and v.stride(1) != 1) or (v.shape[0] > 1 and v.stride(0) < cols):
         raise ValueError(f"{name} must have rows of contiguous elements at one stride")
     return _sp._Dense(v.shape[0], cols, max(v.stride(0), cols), dt, v.data_ptr())
 
@@ -262,7 +262,7 @@ def _teacher(teacher, s, logits):
     k = v.ncols
     stride = k
     if not indices.is_contiguous():
-        if indices.dim() != 2 or indices.stride(1) != 1:
+        if indices.dim() != 2 or (k > 1 and indices.stride(1) != 1):
             raise ValueError("the teacher's indices must be contiguous, or strided rows of contiguous elements")
         stride = indices.stride(0)
     return _sp._Entries(s.nrows, s.ncols, 0, None, k, stride, v.ld, indices.data_ptr(), indices.element_size(),

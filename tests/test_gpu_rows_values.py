@@ -175,3 +175,22 @@ def test_columns_listed_often(dtype, v):
     cols[2] = torch.arange(k) % 5
     cols[3] = torch.arange(k) // 40
     check_both(s, vals, cols, 1.0, "listed often")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_column_of_a_wider_tensor(dtype):
+    """Rows of one element are contiguous whatever the stride between columns."""
+    g = gen(7)
+    wide = normal((6, 12), dtype, g).to(DEV)
+    x, same = wide[:, 3::9], wide[:, 3:4].contiguous()
+    assert x.shape == (6, 1) and x.stride(1) != 1
+    tok = torch.tensor([5, 0, -1, 3], device=DEV)
+    assert torch.equal(sp.embed(tok, x, 2.0), sp.embed(tok, same, 2.0))
+    assert torch.equal(sp.embed_grad(tok, x[:4], 9), sp.embed_grad(tok, same[:4], 9))
+    for got, want in zip(sp.layer_norm(x), sp.layer_norm(same)):
+        assert torch.equal(got, want)
+    S = normal((6, 40), dtype, g).to(DEV)
+    cols = torch.randint(0, 40, (6, 12), generator=g).to(DEV)
+    got = sp.distill_grad(S, (x, cols[:, 3::9]))
+    want = sp.distill_grad(S, (same, cols[:, 3:4].contiguous()))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
