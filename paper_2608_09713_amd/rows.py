@@ -7,7 +7,9 @@ whose last dimension is contiguous; rows may be strided (a slice of columns).
 Leading dimensions count as rows where they can be walked with one stride.
 Work is enqueued on the current stream of the tensors' device and nothing waits
 for it.  Autograd does not record these calls: every gradient is a call of its
-own.
+own.  ``embed``, ``layer_norm`` and ``distill`` refuse inputs that require a
+gradient while gradients are recorded, as it would be lost; call them under
+``torch.no_grad()`` or on detached tensors.
 """
 from __future__ import annotations
 
@@ -43,6 +45,14 @@ def _rows(t, name):
     if v is None or (cols > 1 and v.stride(1) != 1) or (v.shape[0] > 1 and v.stride(0) < cols):
         raise ValueError(f"{name} must have rows of contiguous elements at one stride")
     return _sp._Dense(v.shape[0], cols, max(v.stride(0), cols), dt, v.data_ptr())
+
+
+def _unrecorded(gradient, *tensors):
+    """Refuses inputs whose gradient autograd would be expected to pass on."""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise RuntimeError("autograd does not record this call, and an input requires a gradient: call it under "
+                               f"torch.no_grad() or on detached tensors, and take the gradient from {gradient}")
 
 
 def _like(t):
@@ -155,6 +165,7 @@ def embed(rows, weight, scale=1.0):
     padding), or ``scale * A @ weight`` for a DeviceCSR (m x d; its values, or
     ones, weight the entries)  (spsyrk_embed)."""
     lib = _sp._lib or _sp.library()
+    _unrecorded("embed_grad", weight, None if isinstance(rows, torch.Tensor) else rows.values)
     w = _rows(weight, "weight")
     if weight.dim() != 2:
         raise ValueError("weight must be v x d")
@@ -209,6 +220,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     with the rows' mean and 1 / sqrt(var + eps) as float32 (spsyrk_layer_norm).
     ``weight`` and ``bias``: float32 or x's type, None for ones and zeros."""
     lib = _sp._lib or _sp.library()
+    _unrecorded("layer_norm_grad", x, weight, bias)
     a = _rows(x, "x")
     pt, wp, bp = _params(x, a.ncols, weight, bias, "layer_norm")
     y = _like(x)
@@ -277,6 +289,7 @@ def distill(logits, teacher, temperature=1.0):
     ``teacher``: a DeviceCSR over the logits' columns, or a tuple (values,
     indices) as torch.topk returns; indices outside the columns are padding."""
     lib = _sp._lib or _sp.library()
+    _unrecorded("distill_grad", logits, teacher[0] if isinstance(teacher, tuple) else teacher.values)
     s = _rows(logits, "logits")
     t = _teacher(teacher, s, logits)
     loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
