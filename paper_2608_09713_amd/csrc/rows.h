@@ -27,70 +27,10 @@ inline void by_dtype(int dt, F f) {
         f(__bf16());
 }
 
-// 16 bytes of elements.  The vector type is aligned as one element: gfx950
-// loads and stores 16 bytes at any element's address with one instruction, so
-// rows of odd lengths and strides go through the same code as aligned ones.
-template <typename T>
-struct Pack;
-template <>
-struct Pack<float> {
-    static constexpr int N = 4;
-    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
-};
-template <>
-struct Pack<_Float16> {
-    static constexpr int N = 8;
-    typedef _Float16 V __attribute__((ext_vector_type(8), aligned(2)));
-};
-template <>
-struct Pack<__bf16> {
-    static constexpr int N = 8;
-    typedef __bf16 V __attribute__((ext_vector_type(8), aligned(2)));
-};
-template <typename T>
-using PackV = typename Pack<T>::V;
-
-// The pack at p, of which the first `valid` elements exist (others read as
-// `fill`; nothing past them is touched).
-template <typename T>
-__device__ inline PackV<T> load_pack(const T* p, int64_t valid, float fill = 0.f) {
-    constexpr int N = Pack<T>::N;
-    if (valid >= N) return *reinterpret_cast<const PackV<T>*>(p);
-    PackV<T> v;
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = i < valid ? p[i] : T(fill);
-    return v;
-}
-
-// the same for data read once (a streamed load)
-template <typename T>
-__device__ inline PackV<T> load_pack_nt(const T* p, int64_t valid, float fill = 0.f) {
-    if (valid >= Pack<T>::N) return __builtin_nontemporal_load(reinterpret_cast<const PackV<T>*>(p));
-    return load_pack(p, valid, fill);
-}
-
-template <typename T>
-__device__ inline void store_pack(T* p, PackV<T> v, int64_t valid) {
-    constexpr int N = Pack<T>::N;
-    if (valid >= N) {
-        *reinterpret_cast<PackV<T>*>(p) = v;
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < valid) p[i] = v[i];
-}
-
-template <typename T>
-__device__ inline void store_pack_nt(T* p, PackV<T> v, int64_t valid) {
-    if (valid >= Pack<T>::N)
-        __builtin_nontemporal_store(v, reinterpret_cast<PackV<T>*>(p));
-    else
-        store_pack(p, v, valid);
-}
-
-// N elements, aligned as one (see above): a whole pack, or one element for
-// rows shorter than a pack.
+// N elements: a pack of 16 bytes, or one element for rows shorter than a pack.
+// The vector type is aligned as one element: gfx950 loads and stores 16 bytes at
+// any element's address with one instruction, so rows of odd lengths and strides
+// go through the same code as aligned ones.
 template <typename T, int N>
 struct VecOf {
     typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
