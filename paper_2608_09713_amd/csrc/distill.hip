@@ -210,9 +210,9 @@ __device__ inline void teacher_loss(float& x, const Entries& t, const RowEntries
 constexpr int kAhead = 4;  // packs per thread in flight
 //
 // MOST: the threads of a row, at most.  Rows of more than 512 keep to 64
-// registers, so that two of them are on a compute unit (8192 x 65537 f32: 318
-// us, 370 without); for the others that would only spill (16384 x 32768 bf16:
-// 168 us, 204 so).
+// registers, so that two of them are on a compute unit (8192 x 65537 f32: 316
+// us, 371 without); for the others that would only spill (16384 x 32768 bf16:
+// 178 us, 191 so).
 template <typename T, int N, int MOST>
 __global__ __launch_bounds__(MOST, MOST > 512 ? 8 : 1) void distill_rows(const T* __restrict__ S, int64_t lds, int64_t m, int64_t V,
                                                           Entries t, float temp, const float* __restrict__ weight,
@@ -561,7 +561,7 @@ inline int row_threads(int64_t packs, const Entries& t) {
     const int64_t entries = t.rp ? 2 * (t.nnz / std::max<int64_t>(t.m, 1)) : t.per_row;
     const int64_t n = std::max({ceil_div(packs, 8), std::min<int64_t>(entries, 256), int64_t(1)});
     // (whole rounds of the four SIMDs: loss over 8192 x 60000 bf16 with 15
-    // wavefronts a row 259 us, with 16 205)
+    // wavefronts a row 251 us, with 16 190)
     const int64_t unit = n > 4 * kWave ? 4 * kWave : kWave;
     return int(std::min<int64_t>(ceil_div(n, unit) * unit, kRowBlock));
 }
@@ -602,7 +602,7 @@ void distill(const DenseRows& S, const Entries& t, float temperature, const floa
                     return launch(integral_constant<int, 8>(), most, 16);
                 }
                 // (a pack that no thread needs costs its place in the loops: 8192 x
-                // 65537 bf16, 8193 packs, 486 us with ten a thread, 513 with twelve)
+                // 65537 bf16, 8193 packs, 490 us with ten a thread, 516 with twelve)
                 if (packs <= 10 * nt) return launch(integral_constant<int, 10>(), most, 16);
                 if (packs <= 12 * nt) return launch(integral_constant<int, 12>(), most, 16);
                 if (packs <= 14 * nt) return launch(integral_constant<int, 14>(), most, 16);

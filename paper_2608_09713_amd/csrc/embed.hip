@@ -367,9 +367,9 @@ inline int64_t row_tile(int64_t nnz) { return doubled(64, 16, nnz); }
 // over 32000 x 64 bf16: 37 us with 64, 23 with 16; 8192 over 32000 x 4096: 141
 // and 135).  Rows of up to 256 columns, whose parts cost little, keep tiles half
 // as long (30000 tokens over 100000 x 64 bf16: 43 us, 37 so; 1.57 M entries over
-// 3000 x 250 f32: 337 and 296; but 8192 tokens over 32000 x 4096: 134 and 136).
+// 3000 x 250 f32: 338 and 301; but 8192 tokens over 32000 x 4096: 134 and 136).
 // Up to 1024 entries few columns are long, and parts cost more than they save
-// (512 tokens over 50000 x 1024: 26.3 us, 27.2 with tiles of 16).  Rows of a
+// (512 tokens over 50000 x 1024: 26.6 us, 27.7 with tiles of 16).  Rows of a
 // CSR keep to the longer tiles, as typical ones would otherwise go through parts.
 inline int64_t column_tile(int64_t nnz, int64_t d) {
     return nnz <= 1024 ? row_tile(nnz) : doubled(16, d <= 256 ? 64 : 16, nnz);
@@ -408,6 +408,17 @@ void launch_sums(const Targets<P>& t, const DenseRows& src, float scale, const D
                                            round256(size_t(a.ntiles) * 2 * size_t(a.dp) * sizeof(float)));
     a.tile_units = (a.ntiles + rows - 1) / rows * a.chunks;
     a.tile_blocks = a.ntiles ? grid_for(a.tile_units) : 0;
+    // Eight targets of a group of lanes follow one another where there are many
+    // (from 2^15 on), so that short ones do not wait for each other: gradients of
+    // 8192 tokens over 32768 x 4096 bf16 take 67 us, 139 with one target each, of
+    // 65536 over 32768 x 256 45 and 51, of 512 over 131072 x 1024 56 and 114.
+    // Where few targets hold many entries each, the wavefronts are too few then
+    // (65536 tokens over 4096 x 256: 64 us, 43 with one each; 16384 rows of 24
+    // over 4096 x 128 f32, looked up: 56 and 27).  The limit is on the safe side:
+    // tables of 16384 and 32000 rows under few tokens are past the turn already
+    // (8192 tokens over 32000 x 4096: 135 us with one each, 66 with eight), while
+    // a lookup of long rows is not yet (65537 rows of 24 over 200003 x 250 f32:
+    // 273 us with eight, 250 with one).
     a.per = lg >= 4 && t.targets >= (int64_t(1) << 15) ? 8 : 1;
     a.target_units = (t.targets + rows * a.per - 1) / (rows * a.per) * a.chunks;
     sums_kernel<T, N, P><<<a.tile_blocks + grid_for(a.target_units), kBlock, 0, s>>>(a);
