@@ -445,6 +445,43 @@ spsyrk_status spsyrk_distill_grad(const spsyrk_dense* S, const spsyrk_entries* t
                                   const float* weight, const spsyrk_allocator* al, void* hip_stream, float* loss,
                                   const spsyrk_dense* dS);
 
+/*
+ * Operators of a training step
+ * ----------------------------
+ * Everything said above of the operators between sparse rows and dense rows
+ * (arrays, types, ordering, workspace, errors) holds for these.
+ */
+
+/*
+ * Softmax cross entropy of a linear layer: with z = scale X W^T over the v
+ * columns that are W's rows,
+ *     lse[r] = log sum exp z[r],  loss[r] = lse[r] - z[r][target of r].
+ * X: m x d, W: v x d, of one type, d >= 1, v >= 1.  targets: m x v, rectangular
+ * rows of one entry and no values; a row whose target lies outside [0, v) is
+ * padding and has loss 0.  The logits are formed in 32 bits, piece by piece,
+ * and not kept.  Logits that are NaN or infinite make their row's loss NaN or
+ * infinite.  loss: m floats; lse: m floats, or NULL.
+ */
+spsyrk_status spsyrk_linear_cross_entropy(const spsyrk_dense* X, const spsyrk_dense* W, const spsyrk_entries* targets,
+                                          float scale, const spsyrk_allocator* al, void* hip_stream, float* loss,
+                                          float* lse);
+
+/*
+ * The same loss together with the gradients of sum over the rows of
+ * weight[r] loss[r]: with G = weight (softmax(z) - onehot(target)),
+ *     dX = scale G W (m x d),  dW = scale G^T X (v x d), of X's type.
+ * weight: m floats, NULL for ones.  Rows of weight 0 and padding take no part:
+ * their dX is zero and dW has nothing of them, whatever X holds there.  For
+ * 16-bit types G is rounded to X's type before the products (exponentials as
+ * well), the target's entry from its 32-bit logit.  Workspace: up to about
+ * 4 GB for the exponentials of some rows at a time and their transpose, a
+ * transposed copy of W, and 4 v d bytes where the rows take several turns.
+ */
+spsyrk_status spsyrk_linear_cross_entropy_grad(const spsyrk_dense* X, const spsyrk_dense* W,
+                                               const spsyrk_entries* targets, float scale, const float* weight,
+                                               const spsyrk_allocator* al, void* hip_stream, float* loss,
+                                               const spsyrk_dense* dX, const spsyrk_dense* dW);
+
 /* Static description of a status code. */
 const char* spsyrk_status_string(spsyrk_status s);
 

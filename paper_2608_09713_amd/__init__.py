@@ -100,7 +100,9 @@ def _declare_rows(lib):
             ("spsyrk_layer_norm", [dense, ptr, ptr, i32, f32, ptr, dense, ptr, ptr]),
             ("spsyrk_layer_norm_grad", [dense, dense, ptr, ptr, ptr, i32, alloc, ptr, dense, ptr, ptr]),
             ("spsyrk_distill", [dense, entries, f32, alloc, ptr, ptr]),
-            ("spsyrk_distill_grad", [dense, entries, f32, ptr, alloc, ptr, ptr, dense])):
+            ("spsyrk_distill_grad", [dense, entries, f32, ptr, alloc, ptr, ptr, dense]),
+            ("spsyrk_linear_cross_entropy", [dense, dense, entries, f32, alloc, ptr, ptr, ptr]),
+            ("spsyrk_linear_cross_entropy_grad", [dense, dense, entries, f32, ptr, alloc, ptr, ptr, dense, dense])):
         fn = getattr(lib, name)
         fn.restype = i32
         fn.argtypes = args
@@ -181,6 +183,7 @@ EXPORTS = ("spsyrk_lower", "spsyrk_lower_plan", "spsyrk_lower_execute", "spsyrk_
            "spsyrk_symm", "spsyrk_symm_noalloc",
            "spsyrk_embed", "spsyrk_embed_grad", "spsyrk_layer_norm", "spsyrk_layer_norm_grad",
            "spsyrk_distill", "spsyrk_distill_grad",
+           "spsyrk_linear_cross_entropy", "spsyrk_linear_cross_entropy_grad",
            "spsyrk_status_string",
            "spsyrk_last_error_detail", "spsyrk_last_stats", "spsyrk_abi_version", "spsyrk_timing_begin",
            "spsyrk_timing_begin_phases", "spsyrk_timing_end", "spsyrk_debug_build", "spsyrk_debug_flags")
@@ -528,13 +531,19 @@ def timing_end() -> dict:
 
 
 _ROWS = ("embed", "embed_grad", "layer_norm", "layer_norm_grad", "distill", "distill_grad")
+_TRAINING = ("linear_cross_entropy", "linear_cross_entropy_grad")
 
 
 def __getattr__(name):
-    # the operators between sparse rows and dense rows (rows.py), which need
-    # torch at import, while this module leaves it to the first call
+    # the operators between sparse rows and dense rows (rows.py) and of a
+    # training step (training.py), which need torch at import, while this module
+    # leaves it to the first call
     if name in _ROWS:
         from . import rows
         fn = globals()[name] = getattr(rows, name)
+        return fn
+    if name in _TRAINING:
+        from . import training
+        fn = globals()[name] = getattr(training, name)
         return fn
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,0 +1,604 @@
+// Softmax cross entropy of a linear layer, and its gradient.
+//
+//     z = s x W^T,  lse = log sum exp z,  loss = lse - z[t];
+//     G = w (softmax(z) - onehot(t)),  dx = s G W,  dW = s G^T x.
+//
+// Bound by the matrix cores: one product for the loss, three for the gradient.
+// The logits are not kept.  A tile of the product (a piece of the vocabulary by
+// some rows) leaves each row's largest logit and the sum of the exponentials
+// below it; the rows' pieces are joined by a second launch.  The gradient takes
+// some rows at a time and keeps their exponentials, each relative to its tile's
+// largest, in the inputs' type: a rounding of at most half a step of each
+// probability, where a rounded logit would cost several.  `fold` makes G of
+// them, the target's entry from its 32-bit logit (its difference to 1 would
+// lose all digits of a row that is nearly sure), and lays down G and G^T for
+// the two products that follow.
+//
+// Exponentials are powers of two of differences times log2(e), so that logits
+// up to the floats' ends keep theirs.  A tile's base is at least the lowest
+// float, so that logits of -inf add nothing.
+#include <algorithm>
+#include <cmath>
+
+#include "internal.h"
+#include "product.h"
+#include "training.h"
+
+namespace spsyrk {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr int kCus = 256;  // compute units of the chip
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+// Powers of two that E is raised by: IEEE 16-bit floats end at 2^-24, so theirs
+// take the range up to 2^15.
+template <typename T>
+constexpr float kRaise = std::is_same<T, _Float16>::value ? 15.f : 0.f;
+
+__device__ inline int64_t target_of(const Targets& t, int64_t row) { return load_column(t.p, t.bytes, row * t.stride); }
+__device__ inline float exp_of(float difference) { return __builtin_amdgcn_exp2f(difference * kLog2e); }
+// a row's weight, 0 for padding
+__device__ inline float row_weight(const Targets& t, const float* weight, int64_t V, int64_t row) {
+    const int64_t c = target_of(t, row);
+    return c < 0 || c >= V ? 0.f : weight ? weight[row] : 1.f;
+}
+
+// what a tile leaves of a row: its largest logit, and the sum of exp(logit - largest)
+struct Piece {
+    float top, sum;
+};
+
+// ---- the product with its statistics
+
+template <typename T, int FM, int FN, int WM, int WN, bool KEEP>
+__global__ __launch_bounds__(WM* WN* kWave) void logits_kernel(Operand W, Operand X, int64_t steps, float scale, Targets t,
+                                                               int64_t tm, int64_t tn, Piece* __restrict__ pieces,
+                                                               float* __restrict__ hit, T* __restrict__ E,
+                                                               int64_t lde) {
+    using P = TileProduct<T, FM, FN, WM, WN>;
+    __shared__ __align__(1024) unsigned char buf0[P::BUFFER], buf1[P::BUFFER];
+    __shared__ float part[2][WM][P::BN];
+    const TileAt at = tile_at(blockIdx.x, tm, tn);
+    const int64_t m0 = int64_t(at.m) * P::BM, n0 = int64_t(at.n) * P::BN;
+    F4 acc[FM][FN] = {};
+    P::run(W, X, m0, n0, steps, 0, buf0, buf1, acc);
+
+    const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / WN, wn = w % WN;
+    const int64_t mw = m0 + wm * FM * 16 + 4 * (lane >> 4);
+    const int col = wn * FN * 16 + (lane & 15);
+    float top[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int64_t n = n0 + col + j * 16;
+        const int64_t target = n < X.rows ? target_of(t, n) : -1;
+        float mx = -__builtin_huge_valf();
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t m = mw + i * 16 + r;
+                const float v = m < W.rows ? acc[i][j][r] * scale : -__builtin_huge_valf();
+                if (m == target && m < W.rows) hit[n] = v;
+                acc[i][j][r] = v;
+                mx = fmaxf(mx, v);
+            }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+        top[j] = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        if (lane < 16) part[0][wm][col + j * 16] = top[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        float mx = -3.402823466e38f;
+#pragma unroll
+        for (int q = 0; q < WM; ++q) mx = fmaxf(mx, part[0][q][col + j * 16]);
+        top[j] = mx;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float e = exp_of(acc[i][j][r] - mx);
+                acc[i][j][r] = e;
+                s += e;
+            }
+        s += __shfl_xor(s, 16, kWave);
+        s += __shfl_xor(s, 32, kWave);
+        if (lane < 16) part[1][wm][col + j * 16] = s;
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < P::BN; q += P::THREADS) {
+        const int64_t n = n0 + q;
+        if (n >= X.rows) break;
+        float mx = -3.402823466e38f, s = 0.f;
+#pragma unroll
+        for (int i = 0; i < WM; ++i) {
+            mx = fmaxf(mx, part[0][i][q]);
+            s += part[1][i][q];
+        }
+        pieces[n * tm + at.m] = {mx, s};
+    }
+    if constexpr (KEEP) {
+        const float raise = __builtin_amdgcn_exp2f(kRaise<T>);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            __builtin_amdgcn_sched_barrier(0);  // (addresses of all packs at once would spill)
+            const int64_t n = n0 + col + j * 16;
+            if (n >= X.rows) continue;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int64_t m = mw + i * 16;
+                if (m >= lde) continue;  // (lde is a multiple of four, so a pack fits or stays out)
+                Vec<T, 4> o;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = T(acc[i][j][r] * raise);
+                store_vec<T, 4>(E + n * lde + m, o);
+            }
+        }
+    }
+}
+
+// A row's pieces joined: loss and lse (may be null).
+__global__ __launch_bounds__(kBlock) void join_pieces(const Piece* __restrict__ pieces, int64_t tm, int64_t rows,
+                                                      const float* __restrict__ hit, Targets t, int64_t V,
+                                                      float* __restrict__ loss, float* __restrict__ lse) {
+    for (int64_t n = int64_t(blockIdx.x) * kWavesPerBlock + threadIdx.x / kWave; n < rows;
+         n += int64_t(gridDim.x) * kWavesPerBlock) {
+        const Piece* p = pieces + n * tm;
+        float mx = -3.402823466e38f;
+        for (int64_t i = lane_id(); i < tm; i += kWave) mx = fmaxf(mx, p[i].top);
+        mx = wave_max(mx);
+        float s = 0.f;
+        for (int64_t i = lane_id(); i < tm; i += kWave) s = fmaf(p[i].sum, exp_of(p[i].top - mx), s);
+        s = wave_total(s);
+        if (lane_id() != 0) continue;
+        // (the difference of the two largest terms first: a small loss keeps its digits)
+        const float l = __builtin_amdgcn_logf(s) * kLn2;
+        const int64_t target = target_of(t, n);
+        loss[n] = target < 0 || target >= V ? 0.f : mx - hit[n] + l;
+        if (lse) lse[n] = mx + l;
+    }
+}
+
+// What G is divided by where it is held in 16 bits: the rows' largest weight, so
+// that rows of one weight have G = q - onehot whatever that weight is (of 1/N,
+// say, every row's target would have the same rounding), and for IEEE floats
+// 2^-14 times it, which takes G's entries to their range.
+__global__ __launch_bounds__(1024) void weight_unit(Targets t, const float* __restrict__ weight, int64_t V,
+                                                    int64_t rows, float below, float* __restrict__ unit) {
+    __shared__ float most[1024 / kWave];
+    float mx = 0.f;
+    for (int64_t n = threadIdx.x; n < rows; n += 1024) {
+        const float w = fabsf(row_weight(t, weight, V, n));
+        if (w < __builtin_huge_valf()) mx = fmaxf(mx, w);
+    }
+    mx = wave_max(mx);
+    if (lane_id() == 0) most[threadIdx.x / kWave] = mx;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int i = 0; i < 1024 / kWave; ++i) mx = fmaxf(mx, most[i]);
+    // (a normal number, and a weight of it or less divided by it no infinity)
+    unit[0] = (mx > 0.f ? fminf(fmaxf(mx, 0x1p-100f), 0x1p127f) : 1.f) * below;
+}
+
+// ---- layouts for the products
+
+constexpr int kSide = 64;  // of the tiles that are transposed
+
+// dst: rows of `cols` elements, zeros up to ldd
+template <typename T>
+__global__ __launch_bounds__(kBlock) void pack_rows(const T* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
+                                                    T* __restrict__ dst, int64_t ldd) {
+    constexpr int N = 16 / int(sizeof(T));
+    const int64_t packs = ldd / N;
+    for (int64_t q = int64_t(blockIdx.x) * kBlock + threadIdx.x; q < rows * packs; q += int64_t(gridDim.x) * kBlock) {
+        const int64_t r = q / packs, c = q % packs * N;
+        Vec<T, N> v;
+        if (c + N <= cols) {
+            v = load_vec<T, N>(src + r * ld + c);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = c + i < cols ? src[r * ld + c + i] : T(0.f);
+        }
+        store_vec<T, N>(dst + r * ldd + c, v);
+    }
+}
+
+// dst[c][r] = src[r][c], zeros for r from rows to ldd, and for rows without weight
+template <typename T, bool MASK>
+__global__ __launch_bounds__(kBlock) void pack_transposed(const T* __restrict__ src, int64_t ld, int64_t rows,
+                                                          int64_t cols, T* __restrict__ dst, int64_t ldd, Targets t,
+                                                          const float* __restrict__ weight, int64_t V) {
+    __shared__ T tile[kSide][kSide + 8 / sizeof(T)];
+    const int64_t across = (cols + kSide - 1) / kSide;
+    const int64_t r0 = blockIdx.x / across * kSide, c0 = blockIdx.x % across * kSide;
+    const int x = threadIdx.x % kSide;
+    for (int y = threadIdx.x / kSide; y < kSide; y += kBlock / kSide) {
+        const int64_t r = r0 + y, c = c0 + x;
+        bool there = r < rows && c < cols;
+        if constexpr (MASK) there = there && row_weight(t, weight, V, r) != 0.f;
+        tile[y][x] = there ? src[r * ld + c] : T(0.f);
+    }
+    __syncthreads();
+    for (int y = threadIdx.x / kSide; y < kSide; y += kBlock / kSide) {
+        const int64_t c = c0 + y, r = r0 + x;
+        if (c < cols && r < ldd) dst[c * ldd + r] = tile[x][y];
+    }
+}
+
+// G (in E's place, zeros from V to lde) and G^T (zeros from the rows to ldt) of
+// a tile of kSide rows and columns; piece: columns that share a base.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void fold(T* __restrict__ E, int64_t lde, int64_t rows, int64_t V,
+                                               const Piece* __restrict__ pieces, int64_t tm, int piece,
+                                               const float* __restrict__ lse, const float* __restrict__ loss,
+                                               Targets t, const float* __restrict__ weight,
+                                               const float* __restrict__ unit, T* __restrict__ GT, int64_t ldt) {
+    constexpr int N = 16 / int(sizeof(T)), PER = kSide / N;
+    __shared__ T tile[kSide][kSide + 8 / sizeof(T)];
+    const int64_t r0 = int64_t(blockIdx.y) * kSide, c0 = int64_t(blockIdx.x) * kSide;
+    for (int q = threadIdx.x; q < kSide * PER; q += kBlock) {
+        const int y = q / PER, x = q % PER * N;
+        const int64_t r = r0 + y, c = c0 + x;
+        Vec<T, N> o;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = T(0.f);
+        if (r < rows && c < lde) {
+            const float w = row_weight(t, weight, V, r) / (unit ? unit[0] : 1.f);
+            if (w != 0.f) {
+                const int64_t target = target_of(t, r);
+                const float f = w * __builtin_amdgcn_exp2f(
+                                        (pieces[r * tm + min(c, V - 1) / piece].top - lse[r]) * kLog2e - kRaise<T>);
+                const Vec<T, N> e = load_vec<T, N>(E + r * lde + c);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    float g = float(e[i]) * f;
+                    if (c + i == target) g = w * expm1f(-loss[r]);
+                    o[i] = c + i < V ? T(g) : T(0.f);
+                }
+            }
+            store_vec<T, N>(E + r * lde + c, o);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) tile[y][x + i] = o[i];
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < kSide * PER; q += kBlock) {
+        const int y = q / PER, x = q % PER * N;
+        const int64_t c = c0 + y, r = r0 + x;
+        if (c >= V || r >= ldt) continue;
+        Vec<T, N> o;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = tile[x + i][y];
+        store_vec<T, N>(GT + c * ldt + r, o);
+    }
+}
+
+// ---- plain products
+
+// What becomes of out[n][m]: rounded to T (kStore), a part of k as 32-bit
+// floats (kPart, part z behind rows x ldo each), or added to 32-bit floats
+// (kAdd; the first addition writes), the last time rounded to T as well.
+enum Into { kStore, kPart, kAdd };
+struct Product {
+    void* out = nullptr;  // T
+    int64_t ldo = 0;
+    float alpha = 1.f;
+    const float* unit = nullptr;  // times unit[0]
+    Targets t;                    // with t.p: rows n without weight are zeros
+    const float* weight = nullptr;
+    int64_t V = 0;
+    float* sums = nullptr;  // kPart, kAdd: rows of lds floats
+    int64_t lds = 0, plane = 0;
+    bool first = true, last = true;  // kAdd
+};
+
+template <typename T>
+__device__ inline void store_four(const Product& o, int64_t n, int64_t m, int64_t M, float alpha, bool keep, F4 v) {
+    T* p = static_cast<T*>(o.out) + n * o.ldo + m;
+    Vec<T, 4> q;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) q[r] = keep ? T(v[r] * alpha) : T(0.f);
+    if (m + 4 <= M) {
+        store_vec<T, 4>(p, q);
+    } else {
+        for (int r = 0; r < 4; ++r)
+            if (m + r < M) p[r] = q[r];
+    }
+}
+
+template <typename T, int FM, int FN, int WM, int WN, int INTO>
+__global__ __launch_bounds__(WM* WN* kWave) void product_kernel(Operand A, Operand B, int64_t steps, int64_t per,
+                                                                int64_t tm, int64_t tn, Product o) {
+    using P = TileProduct<T, FM, FN, WM, WN>;
+    __shared__ __align__(1024) unsigned char buf0[P::BUFFER], buf1[P::BUFFER];
+    const TileAt at = tile_at(blockIdx.x, tm, tn);
+    const int64_t m0 = int64_t(at.m) * P::BM, n0 = int64_t(at.n) * P::BN;
+    const int64_t s0 = int64_t(blockIdx.y) * per;
+    F4 acc[FM][FN] = {};
+    P::run(A, B, m0, n0, min(per, steps - s0), s0, buf0, buf1, acc);
+
+    const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / WN, wn = w % WN;
+    const float alpha = o.unit ? o.alpha * o.unit[0] : o.alpha;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        __builtin_amdgcn_sched_barrier(0);  // (addresses of all packs at once would spill)
+        const int64_t n = n0 + wn * FN * 16 + j * 16 + (lane & 15);
+        if (n >= B.rows) continue;
+        const bool keep = !o.t.p || INTO != kStore || row_weight(o.t, o.weight, o.V, n) != 0.f;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int64_t m = m0 + wm * FM * 16 + i * 16 + 4 * (lane >> 4);
+            if (m >= A.rows) continue;
+            if constexpr (INTO == kStore) {
+                store_four<T>(o, n, m, A.rows, alpha, keep, acc[i][j]);
+            } else {
+                // (lds is a multiple of four)
+                F4* p = reinterpret_cast<F4*>(o.sums + int64_t(blockIdx.y) * o.plane + n * o.lds + m);
+                F4 v = acc[i][j];
+                if (INTO == kAdd && !o.first) v += *p;
+                if (INTO == kAdd && o.last)
+                    store_four<T>(o, n, m, A.rows, alpha, true, v);
+                else
+                    *p = v;
+            }
+        }
+    }
+}
+
+// the parts of k added in their order
+template <typename T>
+__global__ __launch_bounds__(kBlock) void join_parts(Product o, int64_t parts, int64_t N, int64_t M) {
+    const float alpha = o.unit ? o.alpha * o.unit[0] : o.alpha;
+    const int64_t packs = o.lds / 4;
+    for (int64_t q = int64_t(blockIdx.x) * kBlock + threadIdx.x; q < N * packs; q += int64_t(gridDim.x) * kBlock) {
+        const int64_t n = q / packs, m = q % packs * 4;
+        if (m >= M) continue;
+        const float* p = o.sums + n * o.lds + m;
+        F4 v = *reinterpret_cast<const F4*>(p);
+        for (int64_t i = 1; i < parts; ++i) v += *reinterpret_cast<const F4*>(p + i * o.plane);
+        const bool keep = !o.t.p || row_weight(o.t, o.weight, o.V, n) != 0.f;
+        store_four<T>(o, n, m, M, alpha, keep, v);
+    }
+}
+
+// Tiles of 256 x 256 by eight wavefronts where they fill the chip, else of 128 x 128 by four.
+constexpr int kWide = 256, kNarrow = 128;
+inline bool wide_tiles(int64_t M, int64_t N) { return ceil_div(M, kWide) * ceil_div(N, kWide) >= kCus * 3 / 4; }
+inline int side_of(int64_t M, int64_t N) { return wide_tiles(M, N) ? kWide : kNarrow; }
+
+// parts of k for a product with too few tiles to fill the chip
+inline int64_t parts_of(int64_t M, int64_t N, int64_t steps) {
+    const int64_t side = side_of(M, N), tiles = ceil_div(M, side) * ceil_div(N, side);
+    const int64_t room = side == kWide ? kCus : 2 * kCus;
+    if (tiles == 0 || 2 * tiles > room) return 1;
+    return std::max<int64_t>(1, std::min<int64_t>({room / tiles, steps / 8, 64}));
+}
+
+template <typename T, typename F>
+void by_tile(int side, F f) {
+    using std::integral_constant;
+    if (side == kWide)
+        f(integral_constant<int, 8>(), integral_constant<int, 4>(), integral_constant<int, 2>(),
+          integral_constant<int, 4>());
+    else
+        f(integral_constant<int, 4>(), integral_constant<int, 4>(), integral_constant<int, 2>(),
+          integral_constant<int, 2>());
+}
+
+template <typename T, int INTO>
+void launch_product(const Operand& A, const Operand& B, int64_t steps, int64_t parts, const Product& o,
+                    hipStream_t s) {
+    const int side = side_of(A.rows, B.rows);
+    by_tile<T>(side, [&](auto fm, auto fn, auto wm, auto wn) {
+        constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
+                      WN = decltype(wn)::value;
+        const int64_t tm = ceil_div(A.rows, side), tn = ceil_div(B.rows, side);
+        product_kernel<T, FM, FN, WM, WN, INTO><<<dim3(unsigned(tm * tn), unsigned(parts)), WM * WN * kWave, 0, s>>>(
+            A, B, steps, ceil_div(steps, parts), tm, tn, o);
+    });
+}
+
+inline unsigned grid_of(int64_t items) { return unsigned(std::min<int64_t>(ceil_div(items, kBlock), 16 * kCus)); }
+
+// ---- a call's workspace, laid out once for its size and once for its use
+
+struct Carver {
+    char* base;
+    size_t used = 0;
+    template <typename T>
+    T* get(int64_t count) {
+        T* p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+        used += (size_t(count) * sizeof(T) + 1023) & ~size_t(1023);
+        return p;
+    }
+};
+
+inline Targets from_row(Targets t, int64_t row) {
+    t.p = static_cast<const char*>(t.p) + row * t.stride * t.bytes;
+    return t;
+}
+
+constexpr int64_t kKeptBytes = int64_t(2) << 30;  // exponentials of the rows taken at a time, at most
+
+// rows of k as an operand: as they are, or packed
+template <typename T>
+bool as_operand(const DenseRows& x) {
+    return on_boundaries(x.p, x.ld, x.dt) && x.n % (kStepBytes / int(sizeof(T))) == 0;
+}
+template <typename T>
+Operand operand_rows(const DenseRows& x, Carver& c, hipStream_t s) {
+    if (as_operand<T>(x)) return {x.p, x.ld, x.m};
+    const int64_t ld = round_up(x.n, kStepBytes / int(sizeof(T)));
+    T* p = c.get<T>(x.m * ld);
+    if (c.base && x.m > 0)
+        pack_rows<T><<<grid_of(x.m * ld * int64_t(sizeof(T)) / 16), kBlock, 0, s>>>(static_cast<const T*>(x.p), x.ld,
+                                                                                 x.m, x.n, p, ld);
+    return {p, ld, x.m};
+}
+template <typename T, bool MASK>
+Operand operand_columns(const DenseRows& x, const Targets& t, const float* weight, int64_t V, T* p, hipStream_t s) {
+    const int64_t ld = round_up(x.m, kStepBytes / int(sizeof(T)));
+    if (ld > 0)
+        pack_transposed<T, MASK><<<unsigned(ceil_div(x.n, kSide) * ceil_div(ld, kSide)), kBlock, 0, s>>>(
+            static_cast<const T*>(x.p), x.ld, x.m, x.n, p, ld, t, weight, V);
+    return {p, ld, x.n};
+}
+
+template <typename T>
+size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, float scale, float* loss, float* lse,
+                     char* tmp, hipStream_t s) {
+    Carver c{tmp};
+    const Operand x = operand_rows<T>(X, c, s), w = operand_rows<T>(W, c, s);
+    // rows at a time: 256 MB of pieces at most
+    const int64_t chunk =
+        std::max<int64_t>(kWide, std::min(X.m, (int64_t(1) << 25) / ceil_div(W.m, kNarrow) / kWide * kWide));
+    const int64_t most = std::min(X.m, chunk);
+    Piece* pieces = c.get<Piece>(most * ceil_div(W.m, kNarrow));
+    float* hit = c.get<float>(most);
+    if (!tmp) return c.used;
+    const int64_t steps = ceil_div(X.n, kStepBytes / int(sizeof(T)));
+    for (int64_t r0 = 0; r0 < X.m; r0 += chunk) {
+        const int64_t n = std::min(chunk, X.m - r0);
+        const Operand xr{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n};
+        const Targets tr = from_row(t, r0);
+        const int side = side_of(W.m, n);
+        const int64_t tm = ceil_div(W.m, side), tn = ceil_div(n, side);
+        by_tile<T>(side, [&](auto fm, auto fn, auto wm, auto wn) {
+            constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
+                          WN = decltype(wn)::value;
+            logits_kernel<T, FM, FN, WM, WN, false><<<unsigned(tm * tn), WM * WN * kWave, 0, s>>>(
+                w, xr, steps, scale, tr, tm, tn, pieces, hit, static_cast<T*>(nullptr), 0);
+        });
+        join_pieces<<<grid_of(n * kWave), kBlock, 0, s>>>(pieces, tm, n, hit, tr, W.m, loss + r0,
+                                                         lse ? lse + r0 : nullptr);
+    }
+    return 0;
+}
+
+template <typename T>
+size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets& t, float scale, const float* weight,
+                          float* loss, const DenseRows& dX, const DenseRows& dW, char* tmp, hipStream_t s) {
+    constexpr int64_t STEP = kStepBytes / int(sizeof(T));
+    const int64_t V = W.m, D = W.n, Vp = round_up(V, STEP);
+    // rows at a time: a whole number of steps (of dW's product) and of tiles
+    const int64_t chunk =
+        std::max<int64_t>(kWide, std::min({round_up(X.m, kWide), kKeptBytes / int64_t(sizeof(T)) / Vp / kWide * kWide,
+                                           int64_t(1) << 17}));
+    const int64_t chunks = ceil_div(X.m, chunk), most = std::min(X.m, chunk);
+    Carver c{tmp};
+    const Operand x = operand_rows<T>(X, c, s), w = operand_rows<T>(W, c, s);
+    Piece* pieces = c.get<Piece>(most * ceil_div(V, kNarrow));
+    float *hit = c.get<float>(most), *lse = c.get<float>(most), *unit = c.get<float>(1);
+    T* E = c.get<T>(most * Vp);
+    const int64_t mostp = round_up(most, STEP);
+    T *GT = c.get<T>(V * mostp), *WT = c.get<T>(D * Vp), *XT = c.get<T>(D * mostp);
+    const int64_t sumld = round_up(D, 4);
+    float* sums = chunks > 1 ? c.get<float>(V * sumld) : nullptr;
+    const int64_t steps_v = Vp / STEP, parts = parts_of(D, most, steps_v);
+    float* dxparts = parts > 1 ? c.get<float>(parts * most * sumld) : nullptr;
+    if (!tmp) return c.used;
+
+    constexpr bool HALF = sizeof(T) == 2;
+    if (HALF)
+        weight_unit<<<1, 1024, 0, s>>>(t, weight, V, X.m, std::is_same<T, _Float16>::value ? 0x1p-14f : 1.f, unit);
+    const Operand wt = X.m ? operand_columns<T, false>(W, Targets(), nullptr, 0, WT, s) : Operand();
+    Product out;
+    out.alpha = scale;
+    out.unit = HALF ? unit : nullptr;
+    for (int64_t r0 = 0; r0 < X.m || r0 == 0; r0 += chunk) {
+        const int64_t n = std::min(chunk, X.m - r0), np = round_up(n, STEP);
+        const Targets tr = from_row(t, r0);
+        const float* wr = weight ? weight + r0 : nullptr;
+        DenseRows xr = X;
+        xr.m = n;
+        xr.p = static_cast<char*>(X.p) + r0 * X.ld * int64_t(sizeof(T));
+        if (n > 0) {
+            const Operand xo{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n};
+            const int here = side_of(V, n);
+            const int64_t tm = ceil_div(V, here), tn = ceil_div(n, here);
+            by_tile<T>(here, [&](auto fm, auto fn, auto wm, auto wn) {
+                constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
+                              WN = decltype(wn)::value;
+                logits_kernel<T, FM, FN, WM, WN, true><<<unsigned(tm * tn), WM * WN * kWave, 0, s>>>(
+                    w, xo, ceil_div(D, STEP), scale, tr, tm, tn, pieces, hit, E, Vp);
+            });
+            join_pieces<<<grid_of(n * kWave), kBlock, 0, s>>>(pieces, tm, n, hit, tr, V, loss + r0, lse);
+            fold<T><<<dim3(unsigned(ceil_div(Vp, kSide)), unsigned(ceil_div(np, kSide))), kBlock, 0, s>>>(
+                E, Vp, n, V, pieces, tm, here, lse, loss + r0, tr, wr, out.unit, GT, np);
+            // dx = G W
+            Product dx = out;
+            dx.out = static_cast<T*>(dX.p) + r0 * dX.ld;
+            dx.ldo = dX.ld;
+            dx.t = tr;
+            dx.weight = wr;
+            dx.V = V;
+            const Operand g{E, Vp, n};
+            const int64_t p = std::min(parts, parts_of(D, n, steps_v));
+            if (p > 1) {
+                dx.sums = dxparts;
+                dx.lds = sumld;
+                dx.plane = n * sumld;
+                launch_product<T, kPart>(wt, g, steps_v, p, dx, s);
+                join_parts<T><<<grid_of(n * sumld / 4), kBlock, 0, s>>>(dx, p, n, D);
+            } else {
+                launch_product<T, kStore>(wt, g, steps_v, 1, dx, s);
+            }
+        }
+        // dW = G^T x
+        Product dw = out;
+        dw.out = dW.p;
+        dw.ldo = dW.ld;
+        dw.sums = sums;
+        dw.lds = sumld;
+        dw.first = r0 == 0;
+        dw.last = r0 + chunk >= X.m;
+        const Operand xt = operand_columns<T, true>(xr, tr, wr, V, XT, s);
+        const Operand gt{GT, np, V};
+        if (sums)
+            launch_product<T, kAdd>(xt, gt, np / STEP, 1, dw, s);
+        else
+            launch_product<T, kStore>(xt, gt, np / STEP, 1, dw, s);
+    }
+    return 0;
+}
+
+}  // namespace
+
+size_t linear_cross_entropy_tmp_bytes(const DenseRows& X, const DenseRows& W) {
+    size_t bytes = 0;
+    by_dtype(X.dt, [&](auto e) {
+        bytes = cross_entropy<decltype(e)>(X, W, Targets(), 1.f, nullptr, nullptr, nullptr, nullptr);
+    });
+    return bytes;
+}
+
+void linear_cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, float scale, float* loss,
+                          float* lse, void* tmp, hipStream_t s) {
+    by_dtype(X.dt, [&](auto e) {
+        cross_entropy<decltype(e)>(X, W, t, scale, loss, lse, static_cast<char*>(tmp), s);
+    });
+}
+
+size_t linear_cross_entropy_grad_tmp_bytes(const DenseRows& X, const DenseRows& W) {
+    size_t bytes = 0;
+    by_dtype(X.dt, [&](auto e) {
+        bytes = cross_entropy_grad<decltype(e)>(X, W, Targets(), 1.f, nullptr, nullptr, DenseRows(), DenseRows(),
+                                                nullptr, nullptr);
+    });
+    return bytes;
+}
+
+void linear_cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets& t, float scale,
+                               const float* weight, float* loss, const DenseRows& dX, const DenseRows& dW, void* tmp,
+                               hipStream_t s) {
+    by_dtype(X.dt, [&](auto e) {
+        cross_entropy_grad<decltype(e)>(X, W, t, scale, weight, loss, dX, dW, static_cast<char*>(tmp), s);
+    });
+}
+
+}  // namespace spsyrk
