@@ -58,7 +58,8 @@ def parse():
 # sources that no workload of this benchmark runs (the operators between sparse
 # rows and dense rows, and of a training step), and the line by which the entry
 # points include theirs
-OTHER_SOURCES = ("crossentropy.hip", "distill.hip", "embed.hip", "norm.hip", "product.h", "rows.h", "training.h")
+OTHER_SOURCES = ("adamw.hip", "blocknorm.hip", "crossentropy.hip", "distill.hip", "embed.hip", "norm.hip", "product.h",
+                 "row_shape.h", "rows.h", "training.h")
 OTHER_INCLUDE = b'\n#include "rows_api.inc"\n'
 
 

@@ -482,6 +482,86 @@ spsyrk_status spsyrk_linear_cross_entropy_grad(const spsyrk_dense* X, const spsy
                                                const spsyrk_allocator* al, void* hip_stream, float* loss,
                                                const spsyrk_dense* dX, const spsyrk_dense* dW);
 
+/*
+ * The norm after a block, its gate, the residual scale and the norm before the
+ * next block, in one pass over the rows:
+ *     u = B r1 post,  r1 = 1 / sqrt(mean B^2 + eps)     (no_norm: u = B),
+ *     Y = X + scale gate u,  H = Y r2 pre,  r2 = 1 / sqrt(mean Y^2 + eps).
+ * X, B, Y, H: m x d of one type, d >= 1.  post, pre: d elements of param_dtype
+ * (SPSYRK_FLOAT32 or X's type), NULL for ones; no_norm takes no post.  gate: g x
+ * d of SPSYRK_FLOAT32 or X's type, g >= 1 dividing m (each row holds for m / g
+ * rows one after another; g = m: for one each), or NULL for ones.  H and r2 are
+ * those of the unrounded sum.  rstd_post (NULL with no_norm), rstd_pre: m floats
+ * each, kept for the gradient.  eps >= 0.
+ */
+spsyrk_status spsyrk_block_norm(const spsyrk_dense* X, const spsyrk_dense* B, const spsyrk_dense* gate, float scale,
+                                const void* post, const void* pre, int param_dtype, int no_norm, float eps,
+                                void* hip_stream, const spsyrk_dense* Y, const spsyrk_dense* H, float* rstd_post,
+                                float* rstd_pre);
+
+/*
+ * The gradient of spsyrk_block_norm, for the gradients dY (NULL: none but by H)
+ * and dH, with Y and B, rstd_post (NULL: the block had no norm) and rstd_pre, and
+ * gate, scale, post and pre of the forward call: dX and dB (m x d of Y's type),
+ * dgate (of the gate's size and type, summed over the rows that share a row of
+ * it), dpost and dpre (d elements of param_dtype, summed over the rows).  dgate
+ * is required with a gate and NULL without; dpost and dpre may be NULL and are
+ * then left out.
+ */
+spsyrk_status spsyrk_block_norm_grad(const spsyrk_dense* dY, const spsyrk_dense* dH, const spsyrk_dense* Y,
+                                     const spsyrk_dense* B, const float* rstd_post, const float* rstd_pre,
+                                     const spsyrk_dense* gate, float scale, const void* post, const void* pre,
+                                     int param_dtype, const spsyrk_allocator* al, void* hip_stream,
+                                     const spsyrk_dense* dX, const spsyrk_dense* dB, const spsyrk_dense* dgate,
+                                     void* dpost, void* dpre);
+
+/*
+ * One AdamW step, in place, over any number of tensors of one kind:
+ *     m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *     w = w - lr weight_decay w - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * with g = grad, times *grad_scale if that is given.  w is held in 32 bits:
+ * master if given, which param then gets rounded, else param itself.
+ * States of 32 bits: m, v of n floats.  Of 8 bits: n codes each, signed for m and
+ * unsigned for v, and a float for every SPSYRK_ADAM_BLOCK elements of the tensor
+ * (and for what is left) in m_scale and v_scale, S below:
+ *     m = sign(c) (c / 127)^2 S,  v = (c / 255)^4 S,
+ * S the largest magnitude among them after the step, rounded to a float, and c
+ * the nearest code (by 127 sqrt(|m| / S), 255 (v / S)^(1/4)), at least 1 for v > 0.
+ * The update is that of the values before they are coded.  All zeros is a state
+ * to begin with.  A value that is not a finite float makes S NaN for its block.
+ * Tensors must not overlap each other; their arrays are as large as n says, and
+ * the call needs no workspace.  The rates are the host's: a captured call repeats
+ * them.  grad_scale is read on the device.
+ */
+#define SPSYRK_ADAM_BLOCK 256
+typedef struct spsyrk_adam_tensor {
+    int64_t n;
+    void* param;            /* of param_dtype */
+    const void* grad;       /* of grad_dtype */
+    float* master;          /* NULL, or of 16-bit parameters a copy in 32 bits (all tensors or none) */
+    void* m;
+    void* v;
+    float* m_scale;         /* 8-bit states */
+    float* v_scale;
+} spsyrk_adam_tensor;
+
+typedef struct spsyrk_adam_step {
+    int32_t param_dtype;    /* spsyrk_dtype */
+    int32_t grad_dtype;     /* SPSYRK_FLOAT32 or param_dtype */
+    int32_t state_bits;     /* 32 or 8 */
+    int64_t step;           /* 1 for the first */
+    double lr, beta1, beta2, eps, weight_decay;
+    const float* grad_scale; /* device, or NULL */
+} spsyrk_adam_step;
+
+spsyrk_status spsyrk_adamw(const spsyrk_adam_tensor* tensors, int64_t count, const spsyrk_adam_step* how,
+                           void* hip_stream);
+
+/* The values that 8-bit states stand for: n floats into m_out[i] and v_out[i] of
+ * tensor i (its param, grad and master are not used). */
+spsyrk_status spsyrk_adam_values(const spsyrk_adam_tensor* tensors, int64_t count, float* const* m_out,
+                                 float* const* v_out, void* hip_stream);
+
 /* Static description of a status code. */
 const char* spsyrk_status_string(spsyrk_status s);
 

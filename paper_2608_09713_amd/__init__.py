@@ -17,6 +17,12 @@ and of the operators between sparse rows and dense rows (``rows.py``):
     loss, dS = sp.distill_grad(S, F, temperature)   # F's rows as the teacher of the logits S
     dh, dgamma, dbeta = sp.layer_norm_grad(dy, h, mean, rstd, gamma, beta)
     dW = sp.embed_grad(A, dh, W.shape[0])
+
+and of a training step (``training.py``):
+
+    y, h, r1, r2 = sp.block_norm(x, block, gate, scale, post, pre)
+    loss, dx, dW = sp.linear_cross_entropy_grad(x, W, targets, row_weight=w)
+    sp.adamw(params, grads, states, lr, step)
 """
 from __future__ import annotations
 
@@ -90,8 +96,21 @@ class _Entries(ctypes.Structure):
                 ("val_dtype", ctypes.c_int32), ("values", ctypes.c_void_p)]
 
 
+class _AdamTensor(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("master", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class _AdamStep(ctypes.Structure):
+    _fields_ = [("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+                ("step", ctypes.c_int64), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
+                ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("grad_scale", ctypes.c_void_p)]
+
+
 def _declare_rows(lib):
-    """Signatures of the operators between sparse rows and dense rows."""
+    """Signatures of the operators between sparse rows and dense rows, and of a training step."""
     dense, entries, alloc = ctypes.POINTER(_Dense), ctypes.POINTER(_Entries), ctypes.POINTER(_Allocator)
     ptr, f32, i32 = ctypes.c_void_p, ctypes.c_float, ctypes.c_int
     for name, args in (
@@ -102,7 +121,12 @@ def _declare_rows(lib):
             ("spsyrk_distill", [dense, entries, f32, alloc, ptr, ptr]),
             ("spsyrk_distill_grad", [dense, entries, f32, ptr, alloc, ptr, ptr, dense]),
             ("spsyrk_linear_cross_entropy", [dense, dense, entries, f32, alloc, ptr, ptr, ptr]),
-            ("spsyrk_linear_cross_entropy_grad", [dense, dense, entries, f32, ptr, alloc, ptr, ptr, dense, dense])):
+            ("spsyrk_linear_cross_entropy_grad", [dense, dense, entries, f32, ptr, alloc, ptr, ptr, dense, dense]),
+            ("spsyrk_block_norm", [dense, dense, dense, f32, ptr, ptr, i32, i32, f32, ptr, dense, dense, ptr, ptr]),
+            ("spsyrk_block_norm_grad", [dense, dense, dense, dense, ptr, ptr, dense, f32, ptr, ptr, i32, alloc, ptr,
+                                        dense, dense, dense, ptr, ptr]),
+            ("spsyrk_adamw", [ptr, ctypes.c_int64, ctypes.POINTER(_AdamStep), ptr]),
+            ("spsyrk_adam_values", [ptr, ctypes.c_int64, ptr, ptr, ptr])):
         fn = getattr(lib, name)
         fn.restype = i32
         fn.argtypes = args
@@ -184,6 +208,7 @@ EXPORTS = ("spsyrk_lower", "spsyrk_lower_plan", "spsyrk_lower_execute", "spsyrk_
            "spsyrk_embed", "spsyrk_embed_grad", "spsyrk_layer_norm", "spsyrk_layer_norm_grad",
            "spsyrk_distill", "spsyrk_distill_grad",
            "spsyrk_linear_cross_entropy", "spsyrk_linear_cross_entropy_grad",
+           "spsyrk_block_norm", "spsyrk_block_norm_grad", "spsyrk_adamw", "spsyrk_adam_values",
            "spsyrk_status_string",
            "spsyrk_last_error_detail", "spsyrk_last_stats", "spsyrk_abi_version", "spsyrk_timing_begin",
            "spsyrk_timing_begin_phases", "spsyrk_timing_end", "spsyrk_debug_build", "spsyrk_debug_flags")
@@ -531,7 +556,8 @@ def timing_end() -> dict:
 
 
 _ROWS = ("embed", "embed_grad", "layer_norm", "layer_norm_grad", "distill", "distill_grad")
-_TRAINING = ("linear_cross_entropy", "linear_cross_entropy_grad")
+_TRAINING = ("linear_cross_entropy", "linear_cross_entropy_grad", "block_norm", "block_norm_grad",
+             "AdamState", "adam_state", "adam_values", "adamw", "adamw_plan")
 
 
 def __getattr__(name):

@@ -1,5 +1,6 @@
 """Operators of a training step: the cross entropy of a linear layer over many
-columns, forward and backward (C-ABI in ``include/spsyrk.h``).
+columns and the norms around a block, forward and backward, and an AdamW step
+over many tensors (C-ABI in ``include/spsyrk.h``).
 
 What ``rows.py`` says of tensors, streams and autograd holds here too: dense
 arguments are float32, float16 or bfloat16 rows of one GPU, work is enqueued on
@@ -8,12 +9,15 @@ an input whose gradient would be lost.
 """
 from __future__ import annotations
 
+import ctypes
+from typing import NamedTuple, Optional
+
 import torch
 
 import paper_2608_09713_amd as _sp
 
-from .rows import (_arena, _byref, _check, _like, _on_device, _raw_stream, _rows, _same_device, _tokens, _unrecorded,
-                   _vector)
+from .rows import (_DTYPE, _arena, _byref, _check, _like, _on_device, _raw_stream, _rows, _same_device, _tokens,
+                   _unrecorded, _vector)
 
 
 def _linear(x, weight, targets):
@@ -66,3 +70,283 @@ def linear_cross_entropy_grad(x, weight, targets, scale=1.0, row_weight=None):
                                                 _raw_stream(x.get_device()), loss.data_ptr(), _byref(ox),
                                                 _byref(ow)), arena)
     return loss, dx, dw
+
+
+def _block_params(x, d, post, pre, what):
+    """(type code, addresses) of the norms' weights."""
+    first = post if post is not None else pre
+    pt = x.dtype if first is None else first.dtype
+    if pt not in (torch.float32, x.dtype):
+        raise TypeError(f"{what}: post and pre must be float32 or {x.dtype}, not {pt}")
+    dev = x.get_device()
+    return _DTYPE[pt], _vector(post, "post", d, (pt,), dev), _vector(pre, "pre", d, (pt,), dev)
+
+
+def _gate(x, gate):
+    """_Dense of a gate (None: null)."""
+    if gate is None:
+        return None
+    g = _rows(gate, "gate")
+    if gate.dtype not in (torch.float32, x.dtype):
+        raise TypeError(f"gate must be float32 or {x.dtype}, not {gate.dtype}")
+    _same_device(x.get_device(), gate, "gate")
+    return g
+
+
+def _same_rows(x, t, name):
+    if t.shape != x.shape or t.dtype != x.dtype:
+        raise ValueError(f"{name} must have the shape and type {tuple(x.shape)}, {x.dtype}")
+    _same_device(x.get_device(), t, name)
+    return _rows(t, name)
+
+
+def _ref(x):
+    return None if x is None else _byref(x)
+
+
+@_on_device(0, "x")
+def block_norm(x, block, gate=None, scale=1.0, post=None, pre=None, norm_block=True, eps=1e-6):
+    """(y, h, rstd_post, rstd_pre) over the last dimension: u = block times
+    1 / sqrt(mean block^2 + eps) times ``post`` (``norm_block`` false: u = block,
+    and rstd_post is None); y = x + scale * gate * u; h = y / sqrt(mean y^2 + eps)
+    * ``pre``  (spsyrk_block_norm).  ``post``, ``pre``: float32 or x's type, None
+    for ones.  ``gate``: float32 or x's type, (d,), or (..., d) with rows that
+    divide x's: each holds for as many consecutive rows; None for ones."""
+    lib = _sp._lib or _sp.library()
+    _unrecorded("block_norm_grad", x, block, gate, post, pre)
+    a = _rows(x, "x")
+    b = _same_rows(x, block, "block")
+    g = _gate(x, gate)
+    pt, pp, qp = _block_params(x, a.ncols, post, pre, "block_norm")
+    dev = x.get_device()
+    y, h = _like(x), _like(x)
+    rstd_pre = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd_post = torch.empty_like(rstd_pre) if norm_block else None
+    oy = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, y.data_ptr())
+    oh = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, h.data_ptr())
+    _check(lib.spsyrk_block_norm(_byref(a), _byref(b), _ref(g), scale, pp, qp, pt, not norm_block, eps,
+                                 _raw_stream(dev), _byref(oy), _byref(oh),
+                                 None if rstd_post is None else rstd_post.data_ptr(), rstd_pre.data_ptr()))
+    return y, h, rstd_post, rstd_pre
+
+
+@_on_device(1, "dh")
+def block_norm_grad(dy, dh, y, block, rstd_post, rstd_pre, gate=None, scale=1.0, post=None, pre=None):
+    """(dx, dblock, dgate, dpost, dpre) of ``block_norm`` for the gradients ``dy``
+    (None: none) of y and ``dh`` of h, with its y, rstd_post (None: the block was
+    not normed) and rstd_pre; dgate, dpost and dpre have their arguments' types and
+    shapes and are None where those are  (spsyrk_block_norm_grad)."""
+    lib = _sp._lib or _sp.library()
+    e = _rows(dh, "dh")
+    a = _same_rows(dh, y, "y")
+    b = _same_rows(dh, block, "block")
+    f = None if dy is None else _same_rows(dh, dy, "dy")
+    g = _gate(y, gate)
+    pt, pp, qp = _block_params(y, a.ncols, post, pre, "block_norm_grad")
+    dev = dh.get_device()
+    r1 = _vector(rstd_post, "rstd_post", a.nrows, (torch.float32,), dev)
+    r2 = _vector(rstd_pre, "rstd_pre", a.nrows, (torch.float32,), dev)
+    if post is not None and rstd_post is None:
+        raise ValueError("a block without a norm has no weights of one: post must be None")
+    dx, db = _like(y), _like(y)
+    dgate = None if gate is None else _like(gate)
+    dpost = None if post is None else torch.empty_like(post)
+    dpre = None if pre is None else torch.empty_like(pre)
+    ox = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, dx.data_ptr())
+    ob = _sp._Dense(a.nrows, a.ncols, a.ncols, a.dtype, db.data_ptr())
+    og = None if g is None else _sp._Dense(g.nrows, g.ncols, g.ncols, g.dtype, dgate.data_ptr())
+    arena = _arena(dev)
+    _check(lib.spsyrk_block_norm_grad(_ref(f), _byref(e), _byref(a), _byref(b), r1, r2, _ref(g), scale, pp, qp, pt,
+                                      _byref(arena.struct), _raw_stream(dev), _byref(ox), _byref(ob), _ref(og),
+                                      None if dpost is None else dpost.data_ptr(),
+                                      None if dpre is None else dpre.data_ptr()), arena)
+    return dx, db, dgate, dpost, dpre
+
+
+ADAM_BLOCK = 256  # elements that share a scale in 8-bit states
+
+
+class AdamState(NamedTuple):
+    """A tensor's states: m and v in float32, or codes (int8 and uint8) with a
+    float32 scale for every 256 elements."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+def adam_state(param, bits=32):
+    """States of zeros for ``param``, of 32 or 8 bits per element."""
+    if bits == 32:
+        return AdamState(torch.zeros(param.shape, dtype=torch.float32, device=param.device),
+                         torch.zeros(param.shape, dtype=torch.float32, device=param.device))
+    if bits != 8:
+        raise ValueError("states have 32 or 8 bits")
+    blocks = -(-param.numel() // ADAM_BLOCK)
+    return AdamState(torch.zeros(param.shape, dtype=torch.int8, device=param.device),
+                     torch.zeros(param.shape, dtype=torch.uint8, device=param.device),
+                     torch.zeros(blocks, dtype=torch.float32, device=param.device),
+                     torch.zeros(blocks, dtype=torch.float32, device=param.device))
+
+
+def _state_bits(state, numel):
+    """8 or 32; checks a state's types and sizes."""
+    m, v, ms, vs = state
+    if m.dtype == torch.float32 and v.dtype == torch.float32 and ms is None and vs is None:
+        bits = 32
+    elif (m.dtype == torch.int8 and v.dtype == torch.uint8 and ms is not None and vs is not None
+          and ms.dtype == torch.float32 and vs.dtype == torch.float32):
+        bits = 8
+        if ms.numel() != -(-numel // ADAM_BLOCK) or vs.numel() != ms.numel():
+            raise ValueError(f"m_scale and v_scale must have one element for every {ADAM_BLOCK} of the tensor")
+    else:
+        raise TypeError("a state must be two float32 tensors, or int8 and uint8 codes with float32 scales")
+    if m.numel() != numel or v.numel() != numel:
+        raise ValueError("a state must have the tensor's size")
+    return bits
+
+
+_ptr = torch.Tensor.data_ptr
+
+
+class AdamWPlan:
+    """AdamW steps over the same tensors: their sizes and types are checked once.
+    The plan keeps the tensors; their addresses are read again at every step, so
+    it follows tensors whose storage was exchanged (``.data = ...``)."""
+
+    def __init__(self, params, grads, states, masters=None):
+        params, grads = list(params), list(grads)
+        states = [s if isinstance(s, AdamState) else AdamState(*s) for s in states]
+        masters = None if masters is None else list(masters)
+        if not len(params) == len(grads) == len(states) or (masters is not None and len(masters) != len(params)):
+            raise ValueError("params, grads, states and masters must have one length")
+        self.params, self.grads, self.states, self.masters = params, grads, states, masters
+        self._device = params[0].get_device() if params else -1
+        if params and not params[0].is_cuda:
+            raise TypeError("params must be device tensors")
+        groups = {}
+        for k, (p, g, s) in enumerate(zip(params, grads, states)):
+            w = None if masters is None else masters[k]
+            if p.dtype not in _DTYPE:
+                raise TypeError(f"params must be float32, float16 or bfloat16, not {p.dtype}")
+            if g.dtype not in (torch.float32, p.dtype):
+                raise TypeError(f"grads must be float32 or the parameter's type, not {g.dtype}")
+            n = p.numel()
+            if g.numel() != n:
+                raise ValueError("a gradient must have its parameter's size")
+            if w is not None:
+                if p.dtype == torch.float32:
+                    raise TypeError("float32 parameters have no master copy")
+                if w.dtype != torch.float32 or w.numel() != n:
+                    raise TypeError("a master copy must be float32, of its parameter's size")
+            bits = _state_bits(s, n)
+            for t in (p, g, w, *s):
+                if t is not None:
+                    if t.get_device() != self._device:
+                        raise ValueError("all tensors must be on one device")
+                    if not t.is_contiguous():
+                        raise ValueError("all tensors must be contiguous")
+            groups.setdefault((p.dtype, g.dtype, bits, w is not None), []).append(k)
+        # (one call for each kind of tensor)
+        self._calls = []
+        for (pt, gt, bits, wide), index in groups.items():
+            how = _sp._AdamStep(_DTYPE[pt], _DTYPE[gt], bits)
+            columns = [[params[k] for k in index], [grads[k] for k in index], [masters[k] for k in index] if wide else None]
+            columns += [[states[k][c] for k in index] for c in range(4 if bits == 8 else 2)]
+            table = (_sp._AdamTensor * len(index))()
+            for row, k in zip(table, index):
+                row.n = params[k].numel()
+            self._calls.append((how, table, columns, []))
+        self._follow()
+
+    def _follow(self):
+        """The tensors' present addresses into the tables."""
+        moved = False
+        for _, table, columns, last in self._calls:
+            now = [None if c is None else list(map(_ptr, c)) for c in columns]
+            if now == last:
+                continue
+            for name, column in zip(("param", "grad", "master", "m", "v", "m_scale", "v_scale"), now):
+                if column is not None:
+                    for row, p in zip(table, column):
+                        if row.n and not p:
+                            raise ValueError("a tensor of the plan has lost its storage")
+                        setattr(row, name, p)
+            last[:] = now
+            moved = True
+        if moved:
+            self._distinct()
+
+    def _distinct(self):
+        """Refuses tensors that are written twice in a step."""
+        spans = []
+        for t in (*self.params, *(self.masters or ()), *(x for s in self.states for x in s if x is not None)):
+            if t.numel():
+                spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
+        spans.sort()
+        for (_, end), (start, _) in zip(spans, spans[1:]):
+            if start < end:
+                raise ValueError("tensors that a step writes must not overlap (the same one twice?)")
+
+    def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None):
+        """One step, in place (``adamw``)."""
+        if not self._calls:
+            return
+        scale = None
+        if grad_scale is not None:
+            scale = _vector(grad_scale, "grad_scale", 1, (torch.float32,), self._device)
+        lib = _sp._lib or _sp.library()
+        self._follow()
+        with torch.cuda.device(self._device):
+            for how, table, _, _ in self._calls:
+                how.step, how.lr, how.eps, how.weight_decay, how.grad_scale = step, lr, eps, weight_decay, scale
+                how.beta1, how.beta2 = betas
+                _check(lib.spsyrk_adamw(table, len(table), _byref(how), _raw_stream(self._device)))
+
+
+def adamw_plan(params, grads, states, masters=None):
+    """An ``AdamWPlan``, for many steps over the same tensors: ``plan.step(lr,
+    step, betas, eps, weight_decay, grad_scale)`` is ``adamw`` over them."""
+    return AdamWPlan(params, grads, states, masters)
+
+
+def adamw(params, grads, states, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None,
+          masters=None):
+    """One AdamW step over many tensors, in place  (spsyrk_adamw): ``states`` from
+    ``adam_state``, one for each parameter; ``step`` counts from 1; ``grads`` of
+    float32 or the parameters' type, times ``grad_scale`` (a float32 device tensor
+    of one element) if given; ``masters``: float32 copies of 16-bit parameters,
+    which are stepped and rounded into them.  The rates are taken at the call: a
+    captured call repeats them."""
+    AdamWPlan(params, grads, states, masters).step(lr, step, betas, eps, weight_decay, grad_scale)
+
+
+def adam_values(states):
+    """[(m, v)] in float32 of every state (the tensors themselves for states of 32
+    bits)  (spsyrk_adam_values)."""
+    states = list(states)
+    out, narrow = [], []
+    for s in states:
+        if _state_bits(s, s[0].numel()) == 32:
+            out.append((s[0], s[1]))
+            continue
+        for t in s:
+            if not t.is_cuda:
+                raise TypeError("states must be device tensors")
+            if not t.is_contiguous():
+                raise ValueError("states must be contiguous")
+            _same_device(s[0].get_device(), t, "a state's tensor")
+        _same_device((narrow[0][0] if narrow else s)[0].get_device(), s[0], "a state")
+        out.append((torch.empty(s[0].shape, dtype=torch.float32, device=s[0].device),
+                    torch.empty(s[1].shape, dtype=torch.float32, device=s[1].device)))
+        narrow.append((s, out[-1]))
+    if narrow:
+        lib = _sp._lib or _sp.library()
+        dev = narrow[0][0][0].get_device()
+        table = (_sp._AdamTensor * len(narrow))()
+        for row, (s, _) in zip(table, narrow):
+            row.n, row.m, row.v, row.m_scale, row.v_scale = s[0].numel(), *map(_ptr, s)
+        ms, vs = ((ctypes.c_void_p * len(narrow))(*(o[k].data_ptr() for _, o in narrow)) for k in (0, 1))
+        with torch.cuda.device(dev):
+            _check(lib.spsyrk_adam_values(table, len(table), ms, vs, _raw_stream(dev)))
+    return out
