@@ -24,61 +24,87 @@
 namespace spsyrk {
 namespace {
 
-constexpr int kAt = 8;                        // elements per thread and turn: 16 bytes of the shortest type
-constexpr int kChunk = kBlock * kAt;          // elements of a workgroup
-constexpr int kTensors = 56;                  // in a launch's arguments (4 KB)
-static_assert(kAdamBlock == 32 * kAt, "half a wavefront holds the elements of a scale");
+constexpr int kAt = 4;  // elements of a pack: 16 bytes of 32-bit floats
+// Packs of a thread, a workgroup's width apart, and threads of a workgroup.  States
+// of 32 bits: the widest chunks are read and written fastest (160 M elements of
+// bf16 with copies: 980 us by 128 threads, 902 by 256, 888 by 1024; two packs a
+// thread 967).  Of 8 bits, where a wavefront's arithmetic counts, two packs by
+// 256 threads (64 M: 280 us with the values, one pack 290, by 1024 threads 296).
+template <bool NARROW>
+constexpr int kPacks = NARROW ? 2 : 1;
+template <bool NARROW>
+constexpr int kThreads = NARROW ? 256 : 1024;
+template <bool NARROW>
+constexpr int kWidth = kThreads<NARROW>* kAt;
+template <bool NARROW>
+constexpr int kChunk = kWidth<NARROW>* kPacks<NARROW>;  // elements of a workgroup
+static_assert(kAdamBlock == kWave * kAt, "a wavefront's pack holds the elements of a scale");
 
+// Tensors whose addresses a launch's arguments (4 KB) have room for: POINTERS of
+// AdamTensor's, in its order without those that the kernel does not use.
+template <int POINTERS>
 struct Batch {
-    AdamTensor t[kTensors];
-    uint32_t first[kTensors + 1];  // workgroup that a tensor starts with
-    int count;
+    static constexpr int MOST = (4096 - int(sizeof(AdamRates)) - 16) / (POINTERS * 8 + 12);
+    void* at[MOST][POINTERS];
+    int64_t n[MOST];
+    uint32_t first[MOST];  // workgroup that a tensor starts with; past the last one no workgroup's number
 };
-static_assert(sizeof(Batch) + sizeof(AdamRates) + 16 <= 4096, "launch arguments");
+template <int POINTERS>
+constexpr bool fits = sizeof(Batch<POINTERS>) + sizeof(AdamRates) + 8 <= 4096;
+static_assert(fits<4> && fits<5> && fits<6> && fits<7>, "launch arguments");
 
-__device__ inline int tensor_of(const Batch& b) {
-    int lo = 0, hi = b.count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (b.first[mid] <= blockIdx.x)
-            lo = mid;
-        else
-            hi = mid;
+// This workgroup's tensor, by one look at all starts (a search would take a
+// chain of reads, each as long as the whole step of a small tensor).
+template <bool NARROW, bool MASTER, int POINTERS>
+__device__ inline AdamTensor tensor_of(const Batch<POINTERS>& b, int64_t* chunk) {
+    int k = -1;
+    constexpr int MOST = Batch<POINTERS>::MOST;
+#pragma unroll
+    for (int q = 0; q < MOST; q += kWave) {
+        const int i = q + lane_id();
+        k += __builtin_popcountll(__ballot(i < MOST && b.first[min(i, MOST - 1)] <= blockIdx.x));
     }
-    return lo;
+    k = int(uniform(uint32_t(k)));
+    *chunk = blockIdx.x - b.first[k];
+    AdamTensor t{};
+    void* const* p = b.at[k];
+    t.n = b.n[k];
+    t.p = p[0];
+    t.g = p[1];
+    t.m = p[2];
+    t.v = p[3];
+    if constexpr (NARROW) {
+        t.m_scale = static_cast<float*>(p[4]);
+        t.v_scale = static_cast<float*>(p[5]);
+    }
+    if constexpr (MASTER) t.master = static_cast<float*>(p[POINTERS - 1]);
+    return t;
 }
 
-// up to kAt elements from i on; those past n are `none`
-template <typename T>
+// the elements of the pack from i on that lie in [0, n); the others are 0 (FULL:
+// all of them do)
+template <bool FULL, typename T>
 __device__ inline void load_some(const T* p, int64_t i, int64_t n, float (&out)[kAt]) {
-    constexpr int N = std::min(kAt, 16 / int(sizeof(T)));
-    if (i + kAt <= n) {
+    if (FULL || (i >= 0 && i + kAt <= n)) {
+        const Vec<T, kAt> v = load_vec_nt<T, kAt>(p + i);
 #pragma unroll
-        for (int q = 0; q < kAt / N; ++q) {
-            const Vec<T, N> v = load_vec_nt<T, N>(p + i + q * N);
-#pragma unroll
-            for (int k = 0; k < N; ++k) out[q * N + k] = float(v[k]);
-        }
+        for (int k = 0; k < kAt; ++k) out[k] = float(v[k]);
     } else {
 #pragma unroll
-        for (int k = 0; k < kAt; ++k) out[k] = i + k < n ? float(p[i + k]) : 0.f;
+        for (int k = 0; k < kAt; ++k) out[k] = i + k >= 0 && i + k < n ? float(p[i + k]) : 0.f;
     }
 }
-template <typename T>
+template <bool FULL, typename T>
 __device__ inline void store_some(T* p, int64_t i, int64_t n, const float (&v)[kAt]) {
-    constexpr int N = std::min(kAt, 16 / int(sizeof(T)));
-    if (i + kAt <= n) {
+    if (FULL || (i >= 0 && i + kAt <= n)) {
+        Vec<T, kAt> o;
 #pragma unroll
-        for (int q = 0; q < kAt / N; ++q) {
-            Vec<T, N> o;
-#pragma unroll
-            for (int k = 0; k < N; ++k) o[k] = T(v[q * N + k]);
-            store_vec_nt<T, N>(p + i + q * N, o);
-        }
+        for (int k = 0; k < kAt; ++k) o[k] = T(v[k]);
+        store_vec_nt<T, kAt>(p + i, o);
     } else {
 #pragma unroll
         for (int k = 0; k < kAt; ++k)
-            if (i + k < n) p[i + k] = T(v[k]);
+            if (i + k >= 0 && i + k < n) p[i + k] = T(v[k]);
     }
 }
 
@@ -87,72 +113,75 @@ __device__ inline float stepped(float w, float m, float v, const AdamRates& r) {
     return fmaf(-r.lr_decay, w, w) - r.lr_m * m / (sqrtf(v * r.inv_v) + r.eps);
 }
 
-template <typename P, bool MASTER>
+template <bool FULL, typename P, bool MASTER>
 __device__ inline void load_parameters(const AdamTensor& t, int64_t i, float (&w)[kAt]) {
     if constexpr (MASTER)
-        load_some(t.master, i, t.n, w);
+        load_some<FULL>(t.master, i, t.n, w);
     else
-        load_some(static_cast<const P*>(t.p), i, t.n, w);
+        load_some<FULL>(static_cast<const P*>(t.p), i, t.n, w);
 }
-template <typename P, bool MASTER>
+template <bool FULL, typename P, bool MASTER>
 __device__ inline void store_parameters(const AdamTensor& t, int64_t i, const float (&w)[kAt]) {
-    if constexpr (MASTER) store_some(t.master, i, t.n, w);
-    store_some(static_cast<P*>(t.p), i, t.n, w);
+    if constexpr (MASTER) store_some<FULL>(t.master, i, t.n, w);
+    store_some<FULL>(static_cast<P*>(t.p), i, t.n, w);
+}
+
+template <bool FULL, typename P, typename G, bool MASTER>
+__device__ inline void step_wide(const AdamTensor& t, int64_t i0, const AdamRates& r) {
+    float w[kPacks<false>][kAt], g[kPacks<false>][kAt], m[kPacks<false>][kAt], v[kPacks<false>][kAt];
+#pragma unroll
+    for (int j = 0; j < kPacks<false>; ++j) {
+        const int64_t i = i0 + j * kWidth<false>;
+        load_some<FULL>(static_cast<const G*>(t.g), i, t.n, g[j]);
+        load_some<FULL>(static_cast<const float*>(t.m), i, t.n, m[j]);
+        load_some<FULL>(static_cast<const float*>(t.v), i, t.n, v[j]);
+        load_parameters<FULL, P, MASTER>(t, i, w[j]);
+    }
+    const float gs = r.grad_scale ? r.grad_scale[0] : 1.f;
+    __builtin_amdgcn_sched_barrier(0);  // (all loads are under way before the first is used)
+#pragma unroll
+    for (int j = 0; j < kPacks<false>; ++j) {
+        const int64_t i = i0 + j * kWidth<false>;
+#pragma unroll
+        for (int q = 0; q < kAt; ++q) {
+            const float x = g[j][q] * gs;
+            m[j][q] = fmaf(r.b1, m[j][q], r.a1 * x);
+            v[j][q] = fmaf(r.b2, v[j][q], r.a2 * x * x);
+            w[j][q] = stepped(w[j][q], m[j][q], v[j][q], r);
+        }
+        store_some<FULL>(static_cast<float*>(t.m), i, t.n, m[j]);
+        store_some<FULL>(static_cast<float*>(t.v), i, t.n, v[j]);
+        store_parameters<FULL, P, MASTER>(t, i, w[j]);
+    }
 }
 
 template <typename P, typename G, bool MASTER>
-__global__ __launch_bounds__(kBlock) void adamw_wide(Batch b, AdamRates r) {
-    const int k = tensor_of(b);
-    const AdamTensor t = b.t[k];
-    const int64_t i = int64_t(blockIdx.x - b.first[k]) * kChunk + int64_t(threadIdx.x) * kAt;
-    if (i >= t.n) return;
-    float w[kAt], g[kAt], m[kAt], v[kAt];
-    load_some(static_cast<const G*>(t.g), i, t.n, g);
-    load_some(static_cast<const float*>(t.m), i, t.n, m);
-    load_some(static_cast<const float*>(t.v), i, t.n, v);
-    load_parameters<P, MASTER>(t, i, w);
-    const float gs = r.grad_scale ? r.grad_scale[0] : 1.f;
-#pragma unroll
-    for (int q = 0; q < kAt; ++q) {
-        const float x = g[q] * gs;
-        m[q] = fmaf(r.b1, m[q], r.a1 * x);
-        v[q] = fmaf(r.b2, v[q], r.a2 * x * x);
-        w[q] = stepped(w[q], m[q], v[q], r);
-    }
-    store_some(static_cast<float*>(t.m), i, t.n, m);
-    store_some(static_cast<float*>(t.v), i, t.n, v);
-    store_parameters<P, MASTER>(t, i, w);
-}
-
-// largest over 32 lanes, in every one of them
-__device__ inline float half_max(float v) {
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
-    return v;
-}
-// whether any of the 32 lanes' flags is set
-__device__ inline bool half_any(bool x) {
-    const uint64_t all = __ballot(x);
-    return uint32_t(lane_id() < 32 ? all : all >> 32) != 0;
+__global__ __launch_bounds__(kThreads<false>) void adamw_wide(Batch<MASTER ? 5 : 4> b, AdamRates r) {
+    int64_t chunk;
+    const AdamTensor t = tensor_of<false, MASTER>(b, &chunk);
+    // (packs start on 16-byte boundaries of the states, wherever the tensor does)
+    const int head = int(reinterpret_cast<uintptr_t>(t.m) / sizeof(float) % kAt);
+    const int64_t c0 = chunk * kChunk<false> - head, i0 = c0 + threadIdx.x * kAt;
+    if (c0 >= 0 && c0 + kChunk<false> <= t.n)
+        step_wide<true, P, G, MASTER>(t, i0, r);
+    else
+        step_wide<false, P, G, MASTER>(t, i0, r);
 }
 
 // The code of y >= 0 for the scale S > 0: nearest in c, where y = (c / LEVELS)^POWER S.
+// 32 bits give LEVELS times the root within 2^-13 (6 units of 2^-24 relative, 255
+// levels); what is nearer to a border than twice that is compared with it in 64 bits.
 template <int LEVELS, int POWER>
 __device__ inline int code_of(double y, float S) {
     const float up = S < 0x1p-60f ? 0x1p80f : 1.f;  // (so that S has a reciprocal)
     float x = float(y * up) * __builtin_amdgcn_rcpf(S * up);
-    x = sqrtf(x);
-    if constexpr (POWER == 4) x = sqrtf(x);
-    const int c = min(int(rintf(x * LEVELS)), LEVELS);
-    // the border below c and the one above it, in 64 bits
-    auto border = [&](double c2) {
-        double q = c2 * (1.0 / LEVELS);
-        q *= q;
-        if constexpr (POWER == 4) q *= q;
-        return q * double(S);
-    };
-    if (c < LEVELS && y > border(c + 0.5)) return c + 1;
-    if (c > 0 && y < border(c - 0.5)) return c - 1;
-    return c;
+    x = __builtin_amdgcn_sqrtf(x);
+    if constexpr (POWER == 4) x = __builtin_amdgcn_sqrtf(x);
+    x = fminf(x * LEVELS, float(LEVELS));
+    const float c = rintf(x);
+    if (fabsf(x - c) <= 0.5f - 0x1p-12f) return int(c);
+    const double border = (floorf(x) + 0.5) * (1.0 / LEVELS), q = border * border;
+    return int(floorf(x)) + (y > (POWER == 4 ? q * q : q) * double(S) ? 1 : 0);
 }
 
 __device__ inline double value_m(int c, float S) {
@@ -165,9 +194,9 @@ __device__ inline double value_v(int c, float S) {
     return q * q * double(S);
 }
 
-template <typename C>
+template <bool FULL, typename C>
 __device__ inline void load_codes(const C* p, int64_t i, int64_t n, int (&out)[kAt]) {
-    if (i + kAt <= n) {
+    if (FULL || i + kAt <= n) {
         const Vec<C, kAt> v = *reinterpret_cast<const Vec<C, kAt>*>(p + i);
 #pragma unroll
         for (int k = 0; k < kAt; ++k) out[k] = v[k];
@@ -176,9 +205,9 @@ __device__ inline void load_codes(const C* p, int64_t i, int64_t n, int (&out)[k
         for (int k = 0; k < kAt; ++k) out[k] = i + k < n ? p[i + k] : 0;
     }
 }
-template <typename C>
+template <bool FULL, typename C>
 __device__ inline void store_codes(C* p, int64_t i, int64_t n, const int (&v)[kAt]) {
-    if (i + kAt <= n) {
+    if (FULL || i + kAt <= n) {
         Vec<C, kAt> o;
 #pragma unroll
         for (int k = 0; k < kAt; ++k) o[k] = C(v[k]);
@@ -190,98 +219,140 @@ __device__ inline void store_codes(C* p, int64_t i, int64_t n, const int (&v)[kA
     }
 }
 
-template <typename P, typename G, bool MASTER>
-__global__ __launch_bounds__(kBlock) void adamw_narrow(Batch b, AdamRates r) {
-    const int k = tensor_of(b);
-    const AdamTensor t = b.t[k];
-    const int64_t i = int64_t(blockIdx.x - b.first[k]) * kChunk + int64_t(threadIdx.x) * kAt;
-    const int64_t block = i / kAdamBlock;
-    const bool there = block * kAdamBlock < t.n;  // (the same for all that share a scale)
-    float w[kAt], g[kAt];
-    int mc[kAt], vc[kAt];
-    load_some(static_cast<const G*>(t.g), i, t.n, g);
-    load_codes(static_cast<const int8_t*>(t.m), i, t.n, mc);
-    load_codes(static_cast<const uint8_t*>(t.v), i, t.n, vc);
-    load_parameters<P, MASTER>(t, i, w);
-    const float ms = there ? t.m_scale[block] : 0.f, vs = there ? t.v_scale[block] : 0.f;
+template <bool FULL, typename P, typename G, bool MASTER>
+__device__ inline void step_narrow(const AdamTensor& t, int64_t i0, const AdamRates& r) {
     const float gs = r.grad_scale ? r.grad_scale[0] : 1.f;
-    double m[kAt], v[kAt];
-    float most_m = 0.f, most_v = 0.f;
-    bool bad = false;
+    float w[kPacks<true>][kAt], g[kPacks<true>][kAt], ms[kPacks<true>], vs[kPacks<true>];
+    int mc[kPacks<true>][kAt], vc[kPacks<true>][kAt];
 #pragma unroll
-    for (int q = 0; q < kAt; ++q) {
-        const double x = double(g[q]) * double(gs);
-        m[q] = fma(r.d1, value_m(mc[q], ms), (1.0 - r.d1) * x);
-        v[q] = fma(r.d2, value_v(vc[q], vs), (1.0 - r.d2) * (x * x));
-        if (i + q >= t.n) m[q] = v[q] = 0.0;
-        const float fm = float(m[q]), fv = float(v[q]);
-        bad = bad || !(fabsf(fm) < __builtin_huge_valf()) || !(fv < __builtin_huge_valf());
-        most_m = fmaxf(most_m, fabsf(fm));
-        most_v = fmaxf(most_v, fv);
-        w[q] = stepped(w[q], fm, fv, r);
+    for (int j = 0; j < kPacks<true>; ++j) {
+        const int64_t i = i0 + j * kWidth<true>, block = i / kAdamBlock;
+        load_some<FULL>(static_cast<const G*>(t.g), i, t.n, g[j]);
+        load_codes<FULL>(static_cast<const int8_t*>(t.m), i, t.n, mc[j]);
+        load_codes<FULL>(static_cast<const uint8_t*>(t.v), i, t.n, vc[j]);
+        load_parameters<FULL, P, MASTER>(t, i, w[j]);
+        const bool there = FULL || block * kAdamBlock < t.n;  // (the same for the wavefront)
+        ms[j] = there ? t.m_scale[block] : 0.f;
+        vs[j] = there ? t.v_scale[block] : 0.f;
     }
-    most_m = half_max(most_m);
-    most_v = half_max(most_v);
-    if (half_any(bad)) most_m = most_v = __builtin_nanf("");  // (a scale of NaN: all its values are)
 #pragma unroll
-    for (int q = 0; q < kAt; ++q) {
-        mc[q] = most_m > 0.f ? code_of<127, 2>(fabs(m[q]), most_m) : 0;
-        if (m[q] < 0.0) mc[q] = -mc[q];
-        vc[q] = most_v > 0.f ? code_of<255, 4>(v[q], most_v) : 0;
-        if (v[q] > 0.0 && most_v > 0.f) vc[q] = max(vc[q], 1);
+    for (int j = 0; j < kPacks<true>; ++j) {
+        const int64_t i = i0 + j * kWidth<true>, block = i / kAdamBlock;
+        if (!FULL && block * kAdamBlock >= t.n) return;
+        double m[kAt], v[kAt];
+        float most_m = 0.f, most_v = 0.f;
+        bool bad = false;
+#pragma unroll
+        for (int q = 0; q < kAt; ++q) {
+            const double x = double(g[j][q]) * double(gs);
+            m[q] = fma(r.d1, value_m(mc[j][q], ms[j]), (1.0 - r.d1) * x);
+            v[q] = fma(r.d2, value_v(vc[j][q], vs[j]), (1.0 - r.d2) * (x * x));
+            if (!FULL && i + q >= t.n) m[q] = v[q] = 0.0;
+            const float fm = float(m[q]), fv = float(v[q]);
+            bad = bad || !(fabsf(fm) < __builtin_huge_valf()) || !(fv < __builtin_huge_valf());
+            most_m = fmaxf(most_m, fabsf(fm));
+            most_v = fmaxf(most_v, fv);
+            w[j][q] = stepped(w[j][q], fm, fv, r);
+        }
+        most_m = wave_max(most_m);
+        most_v = wave_max(most_v);
+        if (__any(bad)) most_m = most_v = __builtin_nanf("");  // (a scale of NaN: all its values are)
+#pragma unroll
+        for (int q = 0; q < kAt; ++q) {
+            mc[j][q] = most_m > 0.f ? code_of<127, 2>(fabs(m[q]), most_m) : 0;
+            if (m[q] < 0.0) mc[j][q] = -mc[j][q];
+            vc[j][q] = most_v > 0.f ? code_of<255, 4>(v[q], most_v) : 0;
+            if (v[q] > 0.0 && most_v > 0.f) vc[j][q] = max(vc[j][q], 1);
+        }
+        store_codes<FULL>(static_cast<int8_t*>(t.m), i, t.n, mc[j]);
+        store_codes<FULL>(static_cast<uint8_t*>(t.v), i, t.n, vc[j]);
+        store_parameters<FULL, P, MASTER>(t, i, w[j]);
+        if (lane_id() == 0) {
+            t.m_scale[block] = most_m;
+            t.v_scale[block] = most_v;
+        }
     }
-    if (i < t.n) {
-        store_codes(static_cast<int8_t*>(t.m), i, t.n, mc);
-        store_codes(static_cast<uint8_t*>(t.v), i, t.n, vc);
-        store_parameters<P, MASTER>(t, i, w);
-    }
-    if (there && i % kAdamBlock == 0) {
-        t.m_scale[block] = most_m;
-        t.v_scale[block] = most_v;
-    }
+}
+
+template <typename P, typename G, bool MASTER>
+__global__ __launch_bounds__(kThreads<true>) void adamw_narrow(Batch<MASTER ? 7 : 6> b, AdamRates r) {
+    int64_t chunk;
+    const AdamTensor t = tensor_of<true, MASTER>(b, &chunk);
+    const int64_t c0 = chunk * kChunk<true>, i0 = c0 + threadIdx.x * kAt;
+    if (c0 + kChunk<true> <= t.n)
+        step_narrow<true, P, G, MASTER>(t, i0, r);
+    else
+        step_narrow<false, P, G, MASTER>(t, i0, r);
 }
 
 // the values that 8-bit states stand for, into 32-bit floats (t.p for m, t.master for v)
-__global__ __launch_bounds__(kBlock) void adam_values_kernel(Batch b) {
-    const int k = tensor_of(b);
-    const AdamTensor t = b.t[k];
-    const int64_t i = int64_t(blockIdx.x - b.first[k]) * kChunk + int64_t(threadIdx.x) * kAt;
-    if (i >= t.n) return;
-    int mc[kAt], vc[kAt];
-    load_codes(static_cast<const int8_t*>(t.m), i, t.n, mc);
-    load_codes(static_cast<const uint8_t*>(t.v), i, t.n, vc);
-    const float ms = t.m_scale[i / kAdamBlock], vs = t.v_scale[i / kAdamBlock];
-    float m[kAt], v[kAt];
+template <bool FULL>
+__device__ inline void values_of(const AdamTensor& t, int64_t i0) {
+    int mc[kPacks<true>][kAt], vc[kPacks<true>][kAt];
+    float ms[kPacks<true>], vs[kPacks<true>];
 #pragma unroll
-    for (int q = 0; q < kAt; ++q) {
-        m[q] = float(value_m(mc[q], ms));
-        v[q] = float(value_v(vc[q], vs));
+    for (int j = 0; j < kPacks<true>; ++j) {
+        const int64_t i = i0 + j * kWidth<true>, block = i / kAdamBlock;
+        load_codes<FULL>(static_cast<const int8_t*>(t.m), i, t.n, mc[j]);
+        load_codes<FULL>(static_cast<const uint8_t*>(t.v), i, t.n, vc[j]);
+        const bool there = FULL || block * kAdamBlock < t.n;
+        ms[j] = there ? t.m_scale[block] : 0.f;
+        vs[j] = there ? t.v_scale[block] : 0.f;
     }
-    store_some(static_cast<float*>(t.p), i, t.n, m);
-    store_some(t.master, i, t.n, v);
+#pragma unroll
+    for (int j = 0; j < kPacks<true>; ++j) {
+        const int64_t i = i0 + j * kWidth<true>;
+        float m[kAt], v[kAt];
+#pragma unroll
+        for (int q = 0; q < kAt; ++q) {
+            m[q] = float(value_m(mc[j][q], ms[j]));
+            v[q] = float(value_v(vc[j][q], vs[j]));
+        }
+        store_some<FULL>(static_cast<float*>(t.p), i, t.n, m);
+        store_some<FULL>(t.master, i, t.n, v);
+    }
+}
+
+__global__ __launch_bounds__(kThreads<true>) void adam_values_kernel(Batch<7> b) {
+    int64_t chunk;
+    const AdamTensor t = tensor_of<true, true>(b, &chunk);
+    const int64_t c0 = chunk * kChunk<true>, i0 = c0 + threadIdx.x * kAt;
+    if (c0 + kChunk<true> <= t.n)
+        values_of<true>(t, i0);
+    else
+        values_of<false>(t, i0);
 }
 
 // f(batch, workgroups) over the tensors, as many at a time as the arguments hold
-template <typename F>
+template <bool NARROW, bool MASTER, typename F>
 void by_batch(const AdamTensor* t, int64_t count, F f) {
-    Batch b;
-    b.count = 0;
+    constexpr int POINTERS = 4 + (NARROW ? 2 : 0) + (MASTER ? 1 : 0);
+    Batch<POINTERS> b;
+    int have = 0;
     int64_t blocks = 0;
     auto flush = [&] {
-        if (b.count) {
-            for (int q = b.count; q <= kTensors; ++q) b.first[q] = uint32_t(blocks);
-            f(b, unsigned(blocks));
-        }
-        b.count = 0;
+        for (int q = have; q < b.MOST; ++q) b.first[q] = 0xffffffffu;
+        if (have) f(b, unsigned(blocks));
+        have = 0;
         blocks = 0;
     };
     for (int64_t q = 0; q < count; ++q) {
         if (t[q].n <= 0) continue;
-        const int64_t more = (t[q].n + kChunk - 1) / kChunk;
-        // (a launch has fewer than 2^24 workgroups, 2^32 threads)
-        if (b.count == kTensors || (b.count && blocks + more >= (int64_t(1) << 23))) flush();
-        b.first[b.count] = uint32_t(blocks);
-        b.t[b.count++] = t[q];
+        const int64_t more = (t[q].n + kAt - 1 + kChunk<NARROW> - 1) / kChunk<NARROW>;  // (with what comes before the first pack)
+        // (a launch has at most 2^22 workgroups and so 2^32 threads, or those of one tensor)
+        if (have == b.MOST || (have && blocks + more > (int64_t(1) << 22) - 1)) flush();
+        void** p = b.at[have];
+        p[0] = t[q].p;
+        p[1] = const_cast<void*>(t[q].g);
+        p[2] = t[q].m;
+        p[3] = t[q].v;
+        if (NARROW) {
+            p[4] = t[q].m_scale;
+            p[5] = t[q].v_scale;
+        }
+        if (MASTER) p[POINTERS - 1] = t[q].master;
+        b.n[have] = t[q].n;
+        b.first[have++] = uint32_t(blocks);
         blocks += more;
     }
     flush();
@@ -291,38 +362,41 @@ void by_batch(const AdamTensor* t, int64_t count, F f) {
 
 void adamw(const AdamTensor* t, int64_t count, int param_dtype, int grad_dtype, int bits, bool master,
            const AdamRates& r, hipStream_t s) {
-    by_batch(t, count, [&](const Batch& b, unsigned blocks) {
-        by_dtype(param_dtype, [&](auto e) {
-            using P = decltype(e);
-            auto launch = [&](auto gt, auto wide) {
-                using G = decltype(gt);
-                constexpr bool MASTER = decltype(wide)::value;
-                if (bits == 32)
-                    adamw_wide<P, G, MASTER><<<blocks, kBlock, 0, s>>>(b, r);
-                else
-                    adamw_narrow<P, G, MASTER><<<blocks, kBlock, 0, s>>>(b, r);
-            };
-            const std::integral_constant<bool, false> no;
-            const std::integral_constant<bool, true> yes;
-            if constexpr (sizeof(P) == 4) {
+    by_dtype(param_dtype, [&](auto e) {
+        using P = decltype(e);
+        auto launch = [&](auto gt, auto wide) {
+            using G = decltype(gt);
+            constexpr bool MASTER = decltype(wide)::value;
+            if (bits == 32)
+                by_batch<false, MASTER>(t, count, [&](const auto& b, unsigned blocks) {
+                    adamw_wide<P, G, MASTER><<<blocks, kThreads<false>, 0, s>>>(b, r);
+                });
+            else
+                by_batch<true, MASTER>(t, count, [&](const auto& b, unsigned blocks) {
+                    adamw_narrow<P, G, MASTER><<<blocks, kThreads<true>, 0, s>>>(b, r);
+                });
+        };
+        const std::integral_constant<bool, false> no;
+        const std::integral_constant<bool, true> yes;
+        if constexpr (sizeof(P) == 4) {
+            launch(float(), no);
+        } else if (grad_dtype == kDtF32) {
+            if (master)
+                launch(float(), yes);
+            else
                 launch(float(), no);
-            } else if (grad_dtype == kDtF32) {
-                if (master)
-                    launch(float(), yes);
-                else
-                    launch(float(), no);
-            } else {
-                if (master)
-                    launch(P(), yes);
-                else
-                    launch(P(), no);
-            }
-        });
+        } else {
+            if (master)
+                launch(P(), yes);
+            else
+                launch(P(), no);
+        }
     });
 }
 
 void adam_values(const AdamTensor* t, int64_t count, hipStream_t s) {
-    by_batch(t, count, [&](const Batch& b, unsigned blocks) { adam_values_kernel<<<blocks, kBlock, 0, s>>>(b); });
+    by_batch<true, true>(t, count,
+                         [&](const auto& b, unsigned blocks) { adam_values_kernel<<<blocks, kThreads<true>, 0, s>>>(b); });
 }
 
 }  // namespace spsyrk

@@ -5,8 +5,8 @@
 //     y = x + s gate u,  h = y r2 pre,  r2 = 1 / sqrt(sum y^2 / d + eps);
 //     n2 = y r2,  a = dh pre,  Y = dy + r2 (a - n2 sum(a n2) / d),  dx = Y,
 //     n1 = b r1,  c = s gate Y post,  db = r1 (c - n1 sum(c n1) / d)   (or s gate Y),
-//     dpre = sum over rows of dh n2,  S = sum over rows of s Y n1,
-//     dgate = post S,  dpost = gate S.
+//     dpre = sum over rows of dh n2,  S = sum over rows of Y n1,
+//     dgate = s post S,  dpost = s gate S.
 //
 // Bound by the bytes of the rows: x and b (the gradient: dy, dh, y, b) are read
 // once, y and h (dx and db) written once, in one launch, a row in registers in
@@ -53,21 +53,48 @@ __device__ inline void store_any(void* p, bool wide, int64_t i, const float (&v)
     }
 }
 
-// N elements of either type that are loaded now and converted when they are used
-template <typename T, int N>
-struct Later {
-    Vec<T, N> narrow;
-    Vec<float, N> wide;
-    __device__ void load(const void* p, bool f32, int64_t i) {
-        if (f32)
-            wide = load_vec<float, N>(static_cast<const float*>(p) + i);
-        else
-            narrow = load_vec<T, N>(static_cast<const T*>(p) + i);
-    }
-    __device__ void get(bool f32, float (&out)[N]) const {
+// Column c of a row in registers (fewer than 2^16 columns): an unsigned 32-bit
+// offset, so that the row's address can stay in scalar registers.
+template <typename T>
+__device__ inline T* column(T* row, int c) {
+    typedef typename std::conditional<std::is_const<T>::value, const char, char>::type B;
+    return reinterpret_cast<T*>(reinterpret_cast<B*>(row) + uint32_t(c) * uint32_t(sizeof(T)));
+}
+
+// Keeps a pack of 16-bit elements as it is in its registers: what is made of it
+// before cannot be held, converted, in twice as many until it is used after.
+template <typename T>
+__device__ inline void keep_packed(Vec<T, 16 / int(sizeof(T))>& v) {
+    typedef unsigned U __attribute__((ext_vector_type(4)));
+    U u = __builtin_bit_cast(U, v);
+    asm volatile("" : "+v"(u));
+    v = __builtin_bit_cast(Vec<T, 16 / int(sizeof(T))>, u);
+}
+
+// N elements that are loaded now and converted when they are used: of T, or (ANY)
+// of T or 32-bit floats.
+template <typename T, int N, bool ANY>
+struct Held {
+    Vec<T, N> v;
+    __device__ void load(const void* p, bool, int64_t i, float none) {
+        if (p) {
+            v = load_vec<T, N>(static_cast<const T*>(p) + i);
+        } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) out[k] = f32 ? wide[k] : float(narrow[k]);
+            for (int k = 0; k < N; ++k) v[k] = T(none);
+        }
     }
+    __device__ float get(int k) const { return float(v[k]); }
+    __device__ void keep() {
+        if constexpr (sizeof(T) == 2 && N > 1) keep_packed<T>(v);
+    }
+};
+template <typename T, int N>
+struct Held<T, N, true> {
+    float v[N];
+    __device__ void load(const void* p, bool wide, int64_t i, float none) { load_any<T, N>(p, wide, i, none, v); }
+    __device__ float get(int k) const { return v[k]; }
+    __device__ void keep() {}
 };
 
 // a row's own gate, or one that `per` rows share
@@ -75,7 +102,22 @@ __device__ inline int64_t gate_row(const BlockGate& g, int64_t r) {
     return g.own ? r : int64_t(uint32_t(r) / uint32_t(g.per));
 }
 
-template <typename T, int N, int L, int MOST, int NP>
+// f(own) for the elements of a pack: whether each belongs to this thread alone.
+// Only the last wavefront of a row has a lane where some do not, so the others
+// go without the comparisons.
+template <int N, int NP, typename F>
+__device__ inline void each_own(const Place (&at)[NP], int k, F f) {
+    if (k < NP - 1 || at[k].shift == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f(i, true);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f(i, i >= at[k].shift);
+    }
+}
+
+// OWN: a gate of each row's own; else post gate is held, for the rows that share it.
+template <typename T, int N, int L, int MOST, int NP, bool ANY, bool OWN>
 __global__ __launch_bounds__(MOST) void after_block(
     const T* __restrict__ x, int64_t ldx, const T* __restrict__ b, int64_t ldb, int64_t m, int64_t d, BlockGate gate,
     float scale, BlockParams par, bool normed, float eps, T* __restrict__ y, int64_t ldy, T* __restrict__ h,
@@ -86,42 +128,45 @@ __global__ __launch_bounds__(MOST) void after_block(
     int turn = 0;
     Place at[NP];
     row_places<N>(l, threads, d, at);
+    using P = Held<T, N, ANY>;
     struct Row {
         Vec<T, N> x[NP], b[NP];
-        Later<T, N> gate[NP];
+        P gate[OWN ? NP : 1];
     };
     auto load = [&](int64_t r) {
         Row q;
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            q.x[k] = load_vec_nt<T, N>(x + r * ldx + at[k].c);
-            q.b[k] = load_vec_nt<T, N>(b + r * ldb + at[k].c);
+            q.x[k] = load_vec_nt<T, N>(column(x + r * ldx, at[k].c));
+            q.b[k] = load_vec_nt<T, N>(column(b + r * ldb, at[k].c));
+            if constexpr (OWN) q.gate[k].load(gate.p, gate.wide, r * gate.ld + at[k].c, 1.f);
         }
-        if (gate.own)
-#pragma unroll
-            for (int k = 0; k < NP; ++k) q.gate[k].load(gate.p, gate.wide, r * gate.ld + at[k].c);
         return q;
     };
     const int64_t step = int64_t(gridDim.x) * ROWS;
     int64_t r = int64_t(blockIdx.x) * ROWS + (L ? threadIdx.x / (L ? L : 1) : 0);
-    Row next;
-    if (r < m) next = load(r);
-    float post[NP][N], pre[NP][N], g[NP][N];
+    Row next = load(min(r, m - 1));
+    P post[NP], pre[NP];
+    float mul[OWN ? 1 : NP][N];
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-        load_any<T, N>(par.post, par.wide, at[k].c, 1.f, post[k]);
-        load_any<T, N>(par.pre, par.wide, at[k].c, 1.f, pre[k]);
+        post[k].load(par.post, par.wide, at[k].c, 1.f);
+        pre[k].load(par.pre, par.wide, at[k].c, 1.f);
     }
-    int64_t held = -1;  // the row of the gate that g has
+    int64_t held = -1;  // the row of the gate that mul has
     for (; r < m; r += step, turn ^= 1) {
         const Row q = next;
-        if (r + step < m) next = load(r + step);
-        if (!gate.own) {
+        next = load(min(r + step, m - 1));
+        if constexpr (!OWN) {
             const int64_t want = gate_row(gate, r);
             if (want != held) {
                 held = want;
 #pragma unroll
-                for (int k = 0; k < NP; ++k) load_any<T, N>(gate.p, gate.wide, want * gate.ld + at[k].c, 1.f, g[k]);
+                for (int k = 0; k < NP; ++k) {
+                    load_any<T, N>(gate.p, gate.wide, want * gate.ld + at[k].c, 1.f, mul[k]);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) mul[k][i] *= post[k].get(i);
+                }
             }
         }
         float r1 = 1.f;
@@ -129,11 +174,10 @@ __global__ __launch_bounds__(MOST) void after_block(
             float s = 0.f;
 #pragma unroll
             for (int k = 0; k < NP; ++k)
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float z = own(at, k, i) ? float(q.b[k][i]) : 0.f;
+                each_own<N>(at, k, [&](int i, bool mine) {
+                    const float z = mine ? float(q.b[k][i]) : 0.f;
                     s = fmaf(z, z, s);
-                }
+                });
             r1 = 1.f / sqrtf(row_sum<L>(s, buf[turn][0]) / float(d) + eps);
             if (l == 0) rstd_post[r] = r1;
         }
@@ -141,13 +185,19 @@ __global__ __launch_bounds__(MOST) void after_block(
         float v[NP][N], s = 0.f;
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            if (gate.own) q.gate[k].get(gate.wide, g[k]);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                v[k][i] = fmaf(float(q.b[k][i]) * post[k][i], g[k][i] * f, float(q.x[k][i]));
-                const float z = own(at, k, i) ? v[k][i] : 0.f;
-                s = fmaf(z, z, s);
+                float w;
+                if constexpr (OWN)
+                    w = q.gate[k].get(i) * post[k].get(i);
+                else
+                    w = mul[k][i];
+                v[k][i] = fmaf(float(q.b[k][i]) * f, w, float(q.x[k][i]));
             }
+            each_own<N>(at, k, [&](int i, bool mine) {
+                const float z = mine ? v[k][i] : 0.f;
+                s = fmaf(z, z, s);
+            });
         }
         const float r2 = 1.f / sqrtf(row_sum<L>(s, buf[turn][1]) / float(d) + eps);
         if (l == 0) rstd_pre[r] = r2;
@@ -158,10 +208,10 @@ __global__ __launch_bounds__(MOST) void after_block(
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 oy[i] = T(v[k][i]);
-                oh[i] = T(v[k][i] * r2 * pre[k][i]);
+                oh[i] = T(v[k][i] * r2 * pre[k].get(i));
             }
-            store_vec_nt<T, N>(y + r * ldy + at[k].c, oy);
-            store_vec_nt<T, N>(h + r * ldh + at[k].c, oh);
+            store_vec_nt<T, N>(column(y + r * ldy, at[k].c), oy);
+            store_vec_nt<T, N>(column(h + r * ldh, at[k].c), oh);
         }
     }
 }
@@ -245,6 +295,10 @@ struct Spread {
     __host__ __device__ int64_t grid() const { return slots * parts; }
 };
 
+// How the gate's rows go with the rows: split over workgroups, whole groups a
+// row's threads, or a row each.
+enum { kSplit, kWhole, kOwn };
+
 // workspace: the workgroups' sums of dh n2, then of S (split groups: one of each
 // part of a group; whole groups: a workgroup's sums of gate S)
 struct Sums {
@@ -257,6 +311,7 @@ struct GradArgs {
     const T *dy, *dh, *y, *b;
     int64_t ldy, ldh, ldo, ldb;
     int64_t m, d;
+    int threads;  // of a row, where it takes more than a wavefront
     const float *rstd_post, *rstd_pre;
     BlockGate gate;
     BlockParams par;
@@ -269,162 +324,219 @@ struct GradArgs {
     Spread go;
 };
 
-// the sums of a workgroup's rows: lanes' groups by lane distance, wavefronts
-// pairwise through LDS; complete in the first L lanes of the first wavefront
-template <int L, int WAVES, int N, int NP>
-__device__ inline void add_rows(float (&v)[NP][N], float* lds) {
-    const int w = threadIdx.x / kWave, lane = lane_id();
+// Sum over a row's threads: L lanes, or (L 0) `waves` wavefronts from `first` on
+// with buf of kMostWaves words, not used again before the next sum's barrier.
+template <int L>
+__device__ inline float rows_sum(float v, float* buf, int first, int waves) {
+    v = group_total<L ? L : kWave>(v);
+    if constexpr (L == 0) {
+        if (lane_id() == 0) buf[threadIdx.x / kWave] = v;
+        lds_barrier();
+        v = 0.f;
+        for (int i = 0; i < waves; ++i) v += buf[first + i];
+    }
+    return v;
+}
+
+// The sums of the rows that a workgroup has under way, complete in the first
+// row's threads.  L lanes: by lane distance in a wavefront, wavefronts pairwise
+// through LDS; else the rows' threads one after another.
+template <int L, int MOST, int N, int NP>
+__device__ inline void add_rows(float (&v)[NP][N], float* lds, int threads, int subs) {
+    if constexpr (L > 0) {
+        constexpr int WAVES = MOST / kWave;
+        const int w = threadIdx.x / kWave, lane = lane_id();
 #pragma unroll
-    for (int far = L; far < kWave; far *= 2)
-#pragma unroll
-        for (int k = 0; k < NP; ++k)
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[k][i] += __shfl_xor(v[k][i], far, kWave);
-#pragma unroll
-    for (int half = WAVES / 2; half > 0; half /= 2) {
-        if (w >= half && w < 2 * half)
+        for (int far = L; far < kWave; far *= 2)
 #pragma unroll
             for (int k = 0; k < NP; ++k)
 #pragma unroll
-                for (int i = 0; i < N; ++i) lds[(((w - half) * NP + k) * N + i) * kWave + lane] = v[k][i];
+                for (int i = 0; i < N; ++i) v[k][i] += __shfl_xor(v[k][i], far, kWave);
+#pragma unroll
+        for (int half = WAVES / 2; half > 0; half /= 2) {
+            if (w >= half && w < 2 * half)
+#pragma unroll
+                for (int k = 0; k < NP; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) lds[(((w - half) * NP + k) * N + i) * kWave + lane] = v[k][i];
+            __syncthreads();
+            if (w < half)
+#pragma unroll
+                for (int k = 0; k < NP; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[k][i] += lds[((w * NP + k) * N + i) * kWave + lane];
+            __syncthreads();
+        }
+    } else if (subs > 1) {
+        const int t = threadIdx.x;
+        if (t >= threads)
+#pragma unroll
+            for (int k = 0; k < NP; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) lds[(k * N + i) * MOST + t] = v[k][i];
         __syncthreads();
-        if (w < half)
+        if (t < threads)
+            for (int u = t + threads; u < threads * subs; u += threads)
 #pragma unroll
-            for (int k = 0; k < NP; ++k)
+                for (int k = 0; k < NP; ++k)
 #pragma unroll
-                for (int i = 0; i < N; ++i) v[k][i] += lds[((w * NP + k) * N + i) * kWave + lane];
+                    for (int i = 0; i < N; ++i) v[k][i] += lds[(k * N + i) * MOST + u];
         __syncthreads();
     }
 }
 
-template <typename T, int N, int L, int MOST, int NP, bool WHOLE>
+template <typename T, int N, int L, int MOST, int NP, bool ANY, int GATE>
 __global__ __launch_bounds__(MOST) void after_block_grad(GradArgs<T> a) {
-    constexpr int ROWS = L ? MOST / (L ? L : 1) : 1, WAVES = MOST / kWave;
+    constexpr bool WHOLE = GATE == kWhole, OWN = GATE == kOwn;
     __shared__ float buf[2][2][kMostWaves];
-    __shared__ float lds[ROWS > 1 ? WAVES / 2 * NP * N * kWave : 1];
-    const int threads = L ? L : int(blockDim.x), l = L ? int(threadIdx.x) % (L ? L : 1) : int(threadIdx.x);
-    const int sub = L ? int(threadIdx.x) / (L ? L : 1) : 0;
+    __shared__ float lds[L ? MOST / 2 * NP * N : MOST < kRowBlock ? MOST * NP * N : 1];
+    // rows under way in the workgroup (all of them take every step of the loops
+    // together, for their sums' barriers; `active`: whether this one has a row)
+    constexpr bool ONE = !L && MOST == kRowBlock;  // (one row)
+    const int threads = L ? L : ONE ? int(blockDim.x) : a.threads;
+    const int subs = L ? MOST / (L ? L : 1) : ONE ? 1 : int(blockDim.x) / threads;
+    const int sub = ONE ? 0 : int(threadIdx.x) / threads, l = ONE ? int(threadIdx.x) : int(threadIdx.x) % threads;
+    const int waves = threads / kWave, first = sub * waves;
     const int64_t d = a.d;
     const bool normed = a.rstd_post != nullptr;
     int turn = 0;
     Place at[NP];
     row_places<N>(l, threads, d, at);
+    using P = Held<T, N, ANY>;
     struct Row {
         Vec<T, N> dy[NP], dh[NP], y[NP], b[NP];
-        Later<T, N> gate[NP];
+        P gate[OWN ? NP : 1];
         float r1, r2;
     };
+    // (without a gradient of y dh is read in its place, and not used; without a
+    // norm of the block r2 in r1's)
+    const T* dy = a.dy ? a.dy : a.dh;
+    const int64_t ldy = a.dy ? a.ldy : a.ldh;
+    const float* rstd_post = normed ? a.rstd_post : a.rstd_pre;
     auto load = [&](int64_t r) {
         Row q;
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            q.dh[k] = load_vec_nt<T, N>(a.dh + r * a.ldh + at[k].c);
-            q.y[k] = load_vec_nt<T, N>(a.y + r * a.ldo + at[k].c);
-            q.b[k] = load_vec_nt<T, N>(a.b + r * a.ldb + at[k].c);
+            q.dh[k] = load_vec_nt<T, N>(column(a.dh + r * a.ldh, at[k].c));
+            q.y[k] = load_vec_nt<T, N>(column(a.y + r * a.ldo, at[k].c));
+            q.b[k] = load_vec_nt<T, N>(column(a.b + r * a.ldb, at[k].c));
+            q.dy[k] = load_vec_nt<T, N>(column(dy + r * ldy, at[k].c));
+            if constexpr (OWN) q.gate[k].load(a.gate.p, a.gate.wide, r * a.gate.ld + at[k].c, 1.f);
         }
-        if (a.dy)
-#pragma unroll
-            for (int k = 0; k < NP; ++k) q.dy[k] = load_vec_nt<T, N>(a.dy + r * a.ldy + at[k].c);
-        if (a.gate.own)
-#pragma unroll
-            for (int k = 0; k < NP; ++k) q.gate[k].load(a.gate.p, a.gate.wide, r * a.gate.ld + at[k].c);
-        q.r1 = normed ? a.rstd_post[r] : 1.f;
+        q.r1 = rstd_post[r];
         q.r2 = a.rstd_pre[r];
         return q;
     };
-    // the rows of this row's threads: j-th of group gi
-    const int64_t walkers = WHOLE ? int64_t(gridDim.x) * ROWS : a.go.slots;
-    const int64_t jstep = WHOLE ? 1 : a.go.parts * ROWS;
-    const int64_t j0 = WHOLE ? 0 : blockIdx.x % a.go.parts * ROWS + sub;
-    const int64_t g0 = WHOLE ? int64_t(blockIdx.x) * ROWS + sub : blockIdx.x / a.go.parts;
-    auto row_of = [&](int64_t gi, int64_t j) { return gi * a.go.per + j; };
-    constexpr bool AHEAD = MOST < kRowBlock;  // (a row ahead, but where its registers would spill)
-    Row next;
-    if (AHEAD && g0 < a.go.groups && j0 < a.go.per) next = load(row_of(g0, j0));
-
-    float post[NP][N], pre[NP][N], g[NP][N], sum_pre[NP][N] = {}, sum_s[NP][N] = {};
+    // (whole: rows' threads take groups side by side; else the rows of one group)
+    const int64_t walkers = WHOLE ? int64_t(gridDim.x) * subs : a.go.slots;
+    const int64_t jstep = WHOLE ? 1 : a.go.parts * subs;
+    const int64_t j0 = WHOLE ? 0 : blockIdx.x % a.go.parts * subs;
+    const int64_t g0 = WHOLE ? int64_t(blockIdx.x) * subs : blockIdx.x / a.go.parts;
+    // mul = scale post gate: of the group, or with a row's own gate of the row
+    P post[NP], pre[NP];
+    float mul[NP][N], sum_pre[NP][N] = {}, sum_s[NP][N] = {};
     float sum_post[WHOLE ? NP : 1][N] = {};
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-        load_any<T, N>(a.par.post, a.par.wide, at[k].c, 1.f, post[k]);
-        load_any<T, N>(a.par.pre, a.par.wide, at[k].c, 1.f, pre[k]);
+        post[k].load(a.par.post, a.par.wide, at[k].c, 1.f);
+        pre[k].load(a.par.pre, a.par.wide, at[k].c, 1.f);
     }
-    for (int64_t gi = g0; gi < a.go.groups; gi += walkers) {
-        if (!a.gate.own)
+    for (int64_t g1 = g0; g1 < a.go.groups; g1 += walkers) {
+        const int64_t gi = WHOLE && !ONE ? min(g1 + sub, a.go.groups - 1) : g1;
+        const bool mine_too = !WHOLE || ONE || g1 + sub < a.go.groups;
+        if constexpr (!OWN)
 #pragma unroll
-            for (int k = 0; k < NP; ++k)
-                load_any<T, N>(a.gate.p, a.gate.wide, gi * a.gate.ld + at[k].c, 1.f, g[k]);
-        for (int64_t j = j0; j < a.go.per; j += jstep, turn ^= 1) {
-            const int64_t r = row_of(gi, j);
-            const Row q = AHEAD ? next : load(r);
-            if (AHEAD) {
-                // (the next one of this group, or the first of the next group)
-                if (j + jstep < a.go.per)
-                    next = load(row_of(gi, j + jstep));
-                else if (gi + walkers < a.go.groups)
-                    next = load(row_of(gi + walkers, j0));
+            for (int k = 0; k < NP; ++k) {
+                load_any<T, N>(a.gate.p, a.gate.wide, gi * a.gate.ld + at[k].c, 1.f, mul[k]);
+#pragma unroll
+                for (int i = 0; i < N; ++i) mul[k][i] *= a.scale * post[k].get(i);
             }
+        for (int64_t j1 = j0; j1 < a.go.per; j1 += jstep, turn ^= 1) {
+            const int64_t j = WHOLE || ONE ? j1 : j1 + sub;
+            const bool active = ONE || (mine_too && j < a.go.per);
+            const int64_t r = gi * a.go.per + (active ? j : a.go.per - 1);
+            Row q = load(r);
+            auto keep = [&] {
+                if constexpr (sizeof(T) == 2 && N > 1)
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+                        post[k].keep();
+                        pre[k].keep();
+                        keep_packed<T>(q.dh[k]);
+                        keep_packed<T>(q.y[k]);
+                        keep_packed<T>(q.b[k]);
+                    }
+            };
+            const float r1 = normed ? q.r1 : 1.f;
             float s = 0.f;
 #pragma unroll
-            for (int k = 0; k < NP; ++k)
+            for (int k = 0; k < NP; ++k) {
+                if constexpr (OWN)
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float w = float(q.dh[k][i]), n2 = float(q.y[k][i]) * q.r2;
-                    sum_pre[k][i] = fmaf(w, n2, sum_pre[k][i]);
-                    s = fmaf(own(at, k, i) ? w * pre[k][i] : 0.f, n2, s);
-                }
-            const float m2 = row_sum<L>(s, buf[turn][0]) / float(d);
+                    for (int i = 0; i < N; ++i) mul[k][i] = a.scale * q.gate[k].get(i) * post[k].get(i);
+                if (active)
+                    each_own<N>(at, k, [&](int i, bool mine) {
+                        const float t = float(q.dh[k][i]) * float(q.y[k][i]);
+                        sum_pre[k][i] = fmaf(t, q.r2, sum_pre[k][i]);
+                        s = fmaf(mine ? t : 0.f, pre[k].get(i), s);
+                    });
+            }
+            // Y = dy + r2 dh pre + y A, A = -r2^2 sum(a n2) / d
+            const float A = -q.r2 * q.r2 * (q.r2 * rows_sum<L>(s, buf[turn][0], first, waves) / float(d));
+            keep();
             float v[NP][N];
             s = 0.f;
 #pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                if (a.gate.own) q.gate[k].get(a.gate.wide, g[k]);
-                float dg[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float n2 = float(q.y[k][i]) * q.r2, n1 = float(q.b[k][i]) * q.r1;
-                    const float Y = fmaf(q.r2, fmaf(float(q.dh[k][i]), pre[k][i], -n2 * m2),
-                                         a.dy ? float(q.dy[k][i]) : 0.f);
-                    const float sy = a.scale * Y, t = sy * n1;
-                    dg[i] = t * post[k][i];
-                    sum_s[k][i] = fmaf(t, a.gate.own ? g[k][i] : 1.f, sum_s[k][i]);
-                    const float c = sy * g[k][i] * post[k][i];
-                    s = fmaf(own(at, k, i) ? c : 0.f, n1, s);
+            for (int k = 0; k < NP; ++k)
+                each_own<N>(at, k, [&](int i, bool mine) {
+                    const float Y = fmaf(float(q.dh[k][i]) * q.r2, pre[k].get(i),
+                                         fmaf(float(q.y[k][i]), A, a.dy ? float(q.dy[k][i]) : 0.f));
                     v[k][i] = Y;
-                }
-                if (a.gate.own && at[k].shift < N)
-                    store_any<T, N>(a.dgate, a.gate.wide, r * a.lddg + at[k].c, dg);
-            }
-            const float m1 = normed ? row_sum<L>(s, buf[turn][1]) / float(d) : 0.f;
+                    s = fmaf(mine ? Y * mul[k][i] : 0.f, float(q.b[k][i]), s);
+                });
+            // db = r1 c + b B, B = -r1^2 sum(c n1) / d
+            const float B = normed ? -r1 * r1 * (r1 * rows_sum<L>(s, buf[turn][1], first, waves) / float(d)) : 0.f;
+            keep();
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
-                if (at[k].shift >= N) break;
+                if (!active) break;
                 Vec<T, N> ox, ob;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float c = a.scale * v[k][i] * g[k][i] * post[k][i], n1 = float(q.b[k][i]) * q.r1;
+                    const float e = v[k][i] * r1, f = float(q.b[k][i]);
+                    sum_s[k][i] = fmaf(OWN ? e * q.gate[OWN ? k : 0].get(i) : e, f, sum_s[k][i]);
                     ox[i] = T(v[k][i]);
-                    ob[i] = T(q.r1 * fmaf(-n1, m1, c));
+                    ob[i] = T(fmaf(f, B, e * mul[k][i]));
                 }
-                store_vec_nt<T, N>(a.dx + r * a.lddx + at[k].c, ox);
-                store_vec_nt<T, N>(a.db + r * a.lddb + at[k].c, ob);
+                if (at[k].shift >= N) break;
+                store_vec_nt<T, N>(column(a.dx + r * a.lddx, at[k].c), ox);
+                store_vec_nt<T, N>(column(a.db + r * a.lddb, at[k].c), ob);
+                if constexpr (OWN) {
+                    float dg[N];
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        dg[i] = v[k][i] * r1 * a.scale * float(q.b[k][i]) * post[k].get(i);
+                    store_any<T, N>(a.dgate, a.gate.wide, r * a.lddg + at[k].c, dg);
+                }
             }
         }
         if constexpr (WHOLE) {
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
-                float dg[N];
+                float dg[N], g[N];
+                load_any<T, N>(a.gate.p, a.gate.wide, gi * a.gate.ld + at[k].c, 1.f, g);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    dg[i] = sum_s[k][i] * post[k][i];
-                    sum_post[k][i] = fmaf(sum_s[k][i], g[k][i], sum_post[k][i]);
+                    dg[i] = a.scale * sum_s[k][i] * post[k].get(i);
+                    sum_post[k][i] = fmaf(sum_s[k][i], g[i], sum_post[k][i]);
                     sum_s[k][i] = 0.f;
                 }
-                if (at[k].shift < N) store_any<T, N>(a.dgate, a.gate.wide, gi * a.lddg + at[k].c, dg);
+                if (mine_too && at[k].shift < N)
+                    store_any<T, N>(a.dgate, a.gate.wide, gi * a.lddg + at[k].c, dg);
             }
         } else {
-            if constexpr (ROWS > 1) add_rows<L, WAVES>(sum_s, lds);
-            if (ROWS == 1 || int(threadIdx.x) < L) {
+            add_rows<L, MOST>(sum_s, lds, threads, subs);
+            if (sub == 0) {
                 float* p = a.sums.s + (gi * a.go.parts + blockIdx.x % a.go.parts) * d;
 #pragma unroll
                 for (int k = 0; k < NP; ++k)
@@ -436,11 +548,9 @@ __global__ __launch_bounds__(MOST) void after_block_grad(GradArgs<T> a) {
                 for (int i = 0; i < N; ++i) sum_s[k][i] = 0.f;
         }
     }
-    if constexpr (ROWS > 1) {
-        add_rows<L, WAVES>(sum_pre, lds);
-        if constexpr (WHOLE) add_rows<L, WAVES>(sum_post, lds);
-        if (int(threadIdx.x) >= L) return;
-    }
+    add_rows<L, MOST>(sum_pre, lds, threads, subs);
+    if constexpr (WHOLE) add_rows<L, MOST>(sum_post, lds, threads, subs);
+    if (sub > 0) return;
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
         if (at[k].shift >= N) break;
@@ -554,7 +664,7 @@ __global__ __launch_bounds__(kBlock) void after_block_sums_long(GradArgs<T> a, c
                 const float n2 = float(y[i]) * r2;
                 const float Y = fmaf(r2, fmaf(float(dh[i]), pre[i], -n2 * m2), dy[i]);
                 sum_pre[i] = fmaf(float(dh[i]), n2, sum_pre[i]);
-                sum_s[i] = fmaf(a.scale * Y * float(b[i]) * r1, k[i], sum_s[i]);
+                sum_s[i] = fmaf(Y * float(b[i]) * r1, k[i], sum_s[i]);
             }
         }
         add(sum_s);
@@ -563,7 +673,7 @@ __global__ __launch_bounds__(kBlock) void after_block_sums_long(GradArgs<T> a, c
                 float dg[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    dg[i] = sum_s[i] * post[i];
+                    dg[i] = a.scale * sum_s[i] * post[i];
                     sum_post[i] = fmaf(sum_s[i], g[i], sum_post[i]);
                 }
                 store_any<T, N>(a.dgate, a.gate.wide, gi * a.lddg + at.c, dg);
@@ -578,16 +688,17 @@ __global__ __launch_bounds__(kBlock) void after_block_sums_long(GradArgs<T> a, c
     if constexpr (WHOLE) store_any<float, N>(a.sums.s + int64_t(blockIdx.y) * a.d, true, at.c, sum_post);
 }
 
-// The parts added up: dpre (item 0), dpost (1) and the gate's rows (2 and on),
-// parts in their order within a wavefront, the wavefronts in theirs.
+// The parts added up: dpre (item 0), dpost (1) and the gate's rows (2 and on):
+// every kJoinBlock / COLUMNS-th part in its order, those sums pairwise.  Narrow
+// workgroups where few columns would leave most of the chip idle.
 constexpr int kJoinBlock = 1024;
-template <typename T>
+template <typename T, int COLUMNS>
 __global__ __launch_bounds__(kJoinBlock) void join_sums(Sums sums, Spread go, int64_t items, int64_t d, BlockGate gate,
-                                                        BlockParams par, void* dpre, void* dpost, void* dgate,
+                                                        BlockParams par, float scale, void* dpre, void* dpost, void* dgate,
                                                         int64_t lddg) {
-    constexpr int W = kJoinBlock / kWave;
-    __shared__ float lds[W][kWave];
-    const int w = threadIdx.x / kWave, l = lane_id();
+    constexpr int W = kJoinBlock / COLUMNS;  // parts under way
+    __shared__ float lds[W][COLUMNS];
+    const int w = threadIdx.x / COLUMNS, l = threadIdx.x % COLUMNS;
     for (int64_t item = blockIdx.y; item < items; item += gridDim.y) {
         if (item == 0 ? !dpre : item == 1 && !dpost) continue;
         const int64_t gi = item - 2;
@@ -597,10 +708,11 @@ __global__ __launch_bounds__(kJoinBlock) void join_sums(Sums sums, Spread go, in
                                                                    : go.parts;
         // (S of a part of a group, times that group's gate, is its share of dpost)
         const bool weighted = item == 1 && !go.whole && gate.p && !gate.own;
-        for (int64_t c0 = int64_t(blockIdx.x) * kWave; c0 < d; c0 += int64_t(gridDim.x) * kWave) {
+        for (int64_t c0 = int64_t(blockIdx.x) * COLUMNS; c0 < d; c0 += int64_t(gridDim.x) * COLUMNS) {
             const int64_t c = c0 + l;
             float s = 0.f;
             if (c < d && weighted) {
+#pragma unroll 4
                 for (int64_t q = w; q < count; q += W) {
                     float k[1];
                     load_any<T, 1>(gate.p, gate.wide, q / go.parts * gate.ld + c, 1.f, k);
@@ -612,16 +724,20 @@ __global__ __launch_bounds__(kJoinBlock) void join_sums(Sums sums, Spread go, in
             }
             lds[w][l] = s;
             __syncthreads();
-            if (w == 0 && c < d) {
-                float v[1] = {0.f};
 #pragma unroll
-                for (int i = 0; i < W; ++i) v[0] += lds[i][l];
+            for (int half = W / 2; half > 0; half /= 2) {
+                if (w < half) lds[w][l] += lds[w + half][l];
+                __syncthreads();
+            }
+            if (w == 0 && c < d) {
+                float v[1] = {lds[0][l]};
                 if (item > 1) {
                     float k[1];
                     load_any<T, 1>(par.post, par.wide, c, 1.f, k);
-                    v[0] *= k[0];
+                    v[0] *= scale * k[0];
                     store_any<T, 1>(dgate, gate.wide, gi * lddg + c, v);
                 } else {
+                    if (item) v[0] *= scale;
                     store_any<T, 1>(item ? dpost : dpre, par.wide, c, v);
                 }
             }
@@ -668,25 +784,37 @@ inline void by_block_shape(const RowShape& s, F f) {
     }
 }
 
-// Workgroups of the gradient: as many as a compute unit holds at two wavefronts
-// a SIMD, over the groups.
+// Rows that a workgroup of the gradient has under way, and workgroups: 16
+// wavefronts on a compute unit, as few workgroups as that takes, since each
+// leaves two sums of d floats.
+inline int grad_rows(const RowShape& s) {
+    return s.lanes ? kGradBlock / s.lanes : s.threads && s.threads <= kGradBlock ? kGradBlock / s.threads : 1;
+}
 constexpr int64_t kLongParts = 64;
 Spread spread_of(int64_t m, int64_t groups, const RowShape& s) {
     Spread go;
     go.groups = groups;
     go.per = m / groups;
-    const int rows = s.lanes ? kGradBlock / s.lanes : 1;
-    const int64_t room = !s.np ? kLongParts : kCus * std::max(1, 512 / (s.lanes ? kGradBlock : s.threads));
-    // (as many groups as walkers: each takes whole ones)
-    if (m > 0 && groups > 1 && groups >= (s.np ? room * rows : room) / 2) {
+    const int rows = s.np ? grad_rows(s) : 1;
+    const int64_t room = !s.np ? kLongParts : s.threads > kGradBlock ? kCus : 2 * kCus;
+    // (as many groups as rows under way: each takes whole ones)
+    if (m > 0 && groups > 1 && groups >= room * rows / 2) {
         go.whole = true;
-        go.slots = std::min(room, ceil_div(groups, s.np ? rows : 1));
+        go.slots = std::min(room, ceil_div(groups, rows));
         return go;
     }
     go.slots = std::min(groups, room);
     const int64_t most = std::max<int64_t>(1, ceil_div(go.per, s.np ? rows : kWavesPerBlock));
     go.parts = std::min(most, std::max<int64_t>(1, room / go.slots));
     return go;
+}
+
+// f(whether a parameter or the gate is of another type than the rows)
+template <typename T, typename F>
+inline void by_types(const BlockGate& gate, const BlockParams& par, F f) {
+    if constexpr (sizeof(T) == 2)
+        if (((par.post || par.pre) && par.wide) || (gate.p && gate.wide)) return f(std::integral_constant<bool, true>());
+    f(std::integral_constant<bool, false>());
 }
 
 int64_t groups_of(const BlockGate& gate) { return gate.p && !gate.own ? gate.rows : 1; }
@@ -714,8 +842,17 @@ void block_norm(const DenseRows& X, const DenseRows& B, const BlockGate& gate, f
             const int threads = L ? MOST : shape.threads;
             const int64_t blocks = L ? ceil_div(m, MOST / (L ? L : 1)) : m;
             const unsigned grid = unsigned(std::min<int64_t>(blocks, kCus * std::max(1, 1024 / threads)));
-            after_block<T, N, L, MOST, NP><<<grid, threads, 0, s>>>(x, X.ld, b, B.ld, m, d, gate, scale, par, normed,
-                                                                    eps, y, Y.ld, h, H.ld, rstd_post, rstd_pre);
+            by_types<T>(gate, par, [&](auto any) {
+                auto launch = [&](auto own_gate) {
+                    after_block<T, N, L, MOST, NP, decltype(any)::value, decltype(own_gate)::value>
+                        <<<grid, threads, 0, s>>>(x, X.ld, b, B.ld, m, d, gate, scale, par, normed, eps, y, Y.ld, h,
+                                                  H.ld, rstd_post, rstd_pre);
+                };
+                if (gate.own)
+                    launch(std::integral_constant<bool, true>());
+                else
+                    launch(std::integral_constant<bool, false>());
+            });
         });
     });
 }
@@ -753,6 +890,7 @@ void block_norm_grad(const DenseRows& DY, const DenseRows& DH, const DenseRows& 
         a.ldb = B.ld;
         a.m = m;
         a.d = d;
+        a.threads = shape.threads;
         a.rstd_post = rstd_post;
         a.rstd_pre = rstd_pre;
         a.gate = gate;
@@ -776,9 +914,17 @@ void block_norm_grad(const DenseRows& DY, const DenseRows& DH, const DenseRows& 
         if (m > 0 && shape.np) {
             by_block_shape<T, N, kGradBlock>(shape, [&](auto lanes, auto most, auto np) {
                 constexpr int L = decltype(lanes)::value, MOST = decltype(most)::value, NP = decltype(np)::value;
-                by_whole([&](auto whole) {
-                    after_block_grad<T, N, L, MOST, NP, decltype(whole)::value>
-                        <<<unsigned(go.grid()), L ? MOST : shape.threads, 0, s>>>(a);
+                by_types<T>(gate, par, [&](auto any) {
+                    auto launch = [&](auto how) {
+                        after_block_grad<T, N, L, MOST, NP, decltype(any)::value, decltype(how)::value>
+                            <<<unsigned(go.grid()), L ? MOST : shape.threads * grad_rows(shape), 0, s>>>(a);
+                    };
+                    if (gate.p && gate.own)
+                        launch(integral_constant<int, kOwn>());
+                    else if (go.whole)
+                        launch(integral_constant<int, kWhole>());
+                    else
+                        launch(integral_constant<int, kSplit>());
                 });
             });
         } else if (m > 0) {
@@ -795,8 +941,16 @@ void block_norm_grad(const DenseRows& DY, const DenseRows& DH, const DenseRows& 
         const int64_t items = shared ? 2 + go.groups : 2;
         Spread add = go;
         if (m == 0) add.parts = 0;  // (of no rows: zeros)
-        join_sums<T><<<dim3(row_grid(ceil_div(d, kWave)), unsigned(std::min<int64_t>(items, 1 << 15))), kJoinBlock, 0,
-                       s>>>(sums, add, items, d, gate, par, dpre, dpost, dgate, lddg);
+        auto join = [&](auto columns) {
+            constexpr int COLUMNS = decltype(columns)::value;
+            join_sums<T, COLUMNS>
+                <<<dim3(row_grid(ceil_div(d, COLUMNS)), unsigned(std::min<int64_t>(items, 1 << 15))), kJoinBlock, 0,
+                   s>>>(sums, add, items, d, gate, par, scale, dpre, dpost, dgate, lddg);
+        };
+        if (ceil_div(d, 64) * items >= kCus / 2)
+            join(integral_constant<int, 64>());
+        else
+            join(integral_constant<int, 16>());
     });
 }
 
