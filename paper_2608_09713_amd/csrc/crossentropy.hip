@@ -10,9 +10,9 @@
 // some rows at a time and keeps their exponentials, each relative to its tile's
 // largest, in the inputs' type: a rounding of at most half a step of each
 // probability, where a rounded logit would cost several.  `fold` makes G of
-// them, the target's entry from its 32-bit logit (its difference to 1 would
-// lose all digits of a row that is nearly sure), and lays down G and G^T for
-// the two products that follow.
+// them in place, the target's entry from its 32-bit logit (its difference to 1
+// would lose all digits of a row that is nearly sure).  The products that follow
+// take W, G and x turned as they lie, with no copies but of x's rows that count.
 //
 // Exponentials are powers of two of differences times log2(e), so that logits
 // up to the floats' ends keep theirs.  A tile's base is at least the lowest
@@ -124,19 +124,23 @@ __global__ __launch_bounds__(WM* WN* kWave) void logits_kernel(Operand W, Operan
     }
     if constexpr (KEEP) {
         const float raise = __builtin_amdgcn_exp2f(kRaise<T>);
+        if constexpr (sizeof(T) == 2) {
+            __builtin_amdgcn_sched_barrier(0);
+            store_rows<T, FM, FN, WM * WN>(acc, buf0, buf1, w, raise, [&](int n1, int m1, Vec<T, 8> v) {
+                const int64_t n = n0 + wn * FN * 16 + n1, m = m0 + wm * FM * 16 + m1;
+                if (n < X.rows && m < lde) store_vec<T, 8>(E + n * lde + m, v);  // (lde is a multiple of eight)
+            });
+        } else {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            __builtin_amdgcn_sched_barrier(0);  // (addresses of all packs at once would spill)
-            const int64_t n = n0 + col + j * 16;
-            if (n >= X.rows) continue;
+            for (int j = 0; j < FN; ++j) {
+                __builtin_amdgcn_sched_barrier(0);  // (addresses of all packs at once would spill)
+                const int64_t n = n0 + col + j * 16;
+                if (n >= X.rows) continue;
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const int64_t m = mw + i * 16;
-                if (m >= lde) continue;  // (lde is a multiple of four, so a pack fits or stays out)
-                Vec<T, 4> o;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = T(acc[i][j][r] * raise);
-                store_vec<T, 4>(E + n * lde + m, o);
+                for (int i = 0; i < FM; ++i) {
+                    const int64_t m = mw + i * 16;
+                    if (m < lde) *reinterpret_cast<F4*>(E + n * lde + m) = acc[i][j];
+                }
             }
         }
     }
@@ -187,18 +191,21 @@ __global__ __launch_bounds__(1024) void weight_unit(Targets t, const float* __re
 
 // ---- layouts for the products
 
-constexpr int kSide = 64;  // of the tiles that are transposed
-
-// dst: rows of `cols` elements, zeros up to ldd
-template <typename T>
+// dst: rows of `cols` elements, zeros up to ldd, and (MASK) rows of zeros for those
+// without weight
+template <typename T, bool MASK>
 __global__ __launch_bounds__(kBlock) void pack_rows(const T* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
-                                                    T* __restrict__ dst, int64_t ldd) {
+                                                    T* __restrict__ dst, int64_t ldd, Targets t,
+                                                    const float* __restrict__ weight, int64_t V) {
     constexpr int N = 16 / int(sizeof(T));
     const int64_t packs = ldd / N;
     for (int64_t q = int64_t(blockIdx.x) * kBlock + threadIdx.x; q < rows * packs; q += int64_t(gridDim.x) * kBlock) {
         const int64_t r = q / packs, c = q % packs * N;
         Vec<T, N> v;
-        if (c + N <= cols) {
+        if (MASK && row_weight(t, weight, V, r) == 0.f) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = T(0.f);
+        } else if (c + N <= cols) {
             v = load_vec<T, N>(src + r * ld + c);
         } else {
 #pragma unroll
@@ -208,79 +215,53 @@ __global__ __launch_bounds__(kBlock) void pack_rows(const T* __restrict__ src, i
     }
 }
 
-// dst[c][r] = src[r][c], zeros for r from rows to ldd, and for rows without weight
-template <typename T, bool MASK>
-__global__ __launch_bounds__(kBlock) void pack_transposed(const T* __restrict__ src, int64_t ld, int64_t rows,
-                                                          int64_t cols, T* __restrict__ dst, int64_t ldd, Targets t,
-                                                          const float* __restrict__ weight, int64_t V) {
-    __shared__ T tile[kSide][kSide + 8 / sizeof(T)];
-    const int64_t across = (cols + kSide - 1) / kSide;
-    const int64_t r0 = blockIdx.x / across * kSide, c0 = blockIdx.x % across * kSide;
-    const int x = threadIdx.x % kSide;
-    for (int y = threadIdx.x / kSide; y < kSide; y += kBlock / kSide) {
-        const int64_t r = r0 + y, c = c0 + x;
-        bool there = r < rows && c < cols;
-        if constexpr (MASK) there = there && row_weight(t, weight, V, r) != 0.f;
-        tile[y][x] = there ? src[r * ld + c] : T(0.f);
-    }
-    __syncthreads();
-    for (int y = threadIdx.x / kSide; y < kSide; y += kBlock / kSide) {
-        const int64_t c = c0 + y, r = r0 + x;
-        if (c < cols && r < ldd) dst[c * ldd + r] = tile[x][y];
-    }
-}
-
-// G (in E's place, zeros from V to lde) and G^T (zeros from the rows to ldt) of
-// a tile of kSide rows and columns; piece: columns that share a base.
+// G in E's place, zeros from V to lde.  piece: columns that share a base.  A
+// workgroup takes kFoldColumns of some rows.
+constexpr int kFoldPacks = 4;  // of a thread, a workgroup's width apart
 template <typename T>
 __global__ __launch_bounds__(kBlock) void fold(T* __restrict__ E, int64_t lde, int64_t rows, int64_t V,
                                                const Piece* __restrict__ pieces, int64_t tm, int piece,
                                                const float* __restrict__ lse, const float* __restrict__ loss,
                                                Targets t, const float* __restrict__ weight,
-                                               const float* __restrict__ unit, T* __restrict__ GT, int64_t ldt) {
-    constexpr int N = 16 / int(sizeof(T)), PER = kSide / N;
-    __shared__ T tile[kSide][kSide + 8 / sizeof(T)];
-    const int64_t r0 = int64_t(blockIdx.y) * kSide, c0 = int64_t(blockIdx.x) * kSide;
-    for (int q = threadIdx.x; q < kSide * PER; q += kBlock) {
-        const int y = q / PER, x = q % PER * N;
-        const int64_t r = r0 + y, c = c0 + x;
-        Vec<T, N> o;
+                                               const float* __restrict__ unit) {
+    constexpr int N = 16 / int(sizeof(T)), SPAN = kBlock * kFoldPacks * N;
+    const int64_t across = (lde + SPAN - 1) / SPAN;
+    const int64_t r = blockIdx.x / across, c0 = blockIdx.x % across * SPAN + threadIdx.x * N;
+    const float w = row_weight(t, weight, V, r) / (unit ? unit[0] : 1.f);
+    T* row = E + r * lde;
+    Vec<T, N> e[kFoldPacks];
+    float f[kFoldPacks];
+    if (w != 0.f) {
+        const float l = lse[r];
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = T(0.f);
-        if (r < rows && c < lde) {
-            const float w = row_weight(t, weight, V, r) / (unit ? unit[0] : 1.f);
-            if (w != 0.f) {
-                const int64_t target = target_of(t, r);
-                const float f = w * __builtin_amdgcn_exp2f(
-                                        (pieces[r * tm + min(c, V - 1) / piece].top - lse[r]) * kLog2e - kRaise<T>);
-                const Vec<T, N> e = load_vec<T, N>(E + r * lde + c);
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    float g = float(e[i]) * f;
-                    if (c + i == target) g = w * expm1f(-loss[r]);
-                    o[i] = c + i < V ? T(g) : T(0.f);
-                }
-            }
-            store_vec<T, N>(E + r * lde + c, o);
+        for (int q = 0; q < kFoldPacks; ++q) {
+            const int64_t c = c0 + q * kBlock * N;
+            if (c >= lde) break;
+            e[q] = load_vec<T, N>(row + c);
+            f[q] = w * __builtin_amdgcn_exp2f((pieces[r * tm + min(c, V - 1) / piece].top - l) * kLog2e - kRaise<T>);
         }
-#pragma unroll
-        for (int i = 0; i < N; ++i) tile[y][x + i] = o[i];
     }
-    __syncthreads();
-    for (int q = threadIdx.x; q < kSide * PER; q += kBlock) {
-        const int y = q / PER, x = q % PER * N;
-        const int64_t c = c0 + y, r = r0 + x;
-        if (c >= V || r >= ldt) continue;
+    const int64_t target = w != 0.f ? target_of(t, r) : -1;
+#pragma unroll
+    for (int q = 0; q < kFoldPacks; ++q) {
+        const int64_t c = c0 + q * kBlock * N;
+        if (c >= lde) break;
         Vec<T, N> o;
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = tile[x + i][y];
-        store_vec<T, N>(GT + c * ldt + r, o);
+        for (int i = 0; i < N; ++i) o[i] = w != 0.f && c + i < V ? T(float(e[q][i]) * f[q]) : T(0.f);
+        if (target >= c && target < c + N) {
+            const T g = T(w * expm1f(-loss[r]));
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = c + i == target ? g : o[i];
+        }
+        store_vec<T, N>(row + c, o);
     }
 }
 
 // ---- plain products
 
-// What becomes of out[n][m]: rounded to T (kStore), a part of k as 32-bit
+// Products of a turned A (W, or the rows of x that count) with B in rows of k (G) or
+// turned too.  What becomes of out[n][m]: rounded to T (kStore), a part of k as 32-bit
 // floats (kPart, part z behind rows x ldo each), or added to 32-bit floats
 // (kAdd; the first addition writes), the last time rounded to T as well.
 enum Into { kStore, kPart, kAdd };
@@ -311,10 +292,10 @@ __device__ inline void store_four(const Product& o, int64_t n, int64_t m, int64_
     }
 }
 
-template <typename T, int FM, int FN, int WM, int WN, int INTO>
+template <typename T, int FM, int FN, int WM, int WN, bool TB, int INTO>
 __global__ __launch_bounds__(WM* WN* kWave) void product_kernel(Operand A, Operand B, int64_t steps, int64_t per,
                                                                 int64_t tm, int64_t tn, Product o) {
-    using P = TileProduct<T, FM, FN, WM, WN>;
+    using P = TileProduct<T, FM, FN, WM, WN, true, TB>;
     __shared__ __align__(1024) unsigned char buf0[P::BUFFER], buf1[P::BUFFER];
     const TileAt at = tile_at(blockIdx.x, tm, tn);
     const int64_t m0 = int64_t(at.m) * P::BM, n0 = int64_t(at.n) * P::BN;
@@ -324,6 +305,25 @@ __global__ __launch_bounds__(WM* WN* kWave) void product_kernel(Operand A, Opera
 
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / WN, wn = w % WN;
     const float alpha = o.unit ? o.alpha * o.unit[0] : o.alpha;
+    if constexpr (INTO == kStore && sizeof(T) == 2) {
+        __syncthreads();  // (the buffers are free)
+        store_rows<T, FM, FN, WM * WN>(acc, buf0, buf1, w, alpha, [&](int n1, int m1, Vec<T, 8> v) {
+            const int64_t n = n0 + wn * FN * 16 + n1, m = m0 + wm * FM * 16 + m1;
+            if (n >= B.rows || m >= A.rows) return;
+            if (o.t.p && row_weight(o.t, o.weight, o.V, n) == 0.f)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = T(0.f);
+            T* p = static_cast<T*>(o.out) + n * o.ldo + m;
+            if (m + 8 <= A.rows) {
+                store_vec<T, 8>(p, v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (m + i < A.rows) p[i] = v[i];
+            }
+        });
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         __builtin_amdgcn_sched_barrier(0);  // (addresses of all packs at once would spill)
@@ -390,7 +390,7 @@ void by_tile(int side, F f) {
           integral_constant<int, 2>());
 }
 
-template <typename T, int INTO>
+template <typename T, bool TB, int INTO>
 void launch_product(const Operand& A, const Operand& B, int64_t steps, int64_t parts, const Product& o,
                     hipStream_t s) {
     const int side = side_of(A.rows, B.rows);
@@ -398,7 +398,7 @@ void launch_product(const Operand& A, const Operand& B, int64_t steps, int64_t p
         constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
                       WN = decltype(wn)::value;
         const int64_t tm = ceil_div(A.rows, side), tn = ceil_div(B.rows, side);
-        product_kernel<T, FM, FN, WM, WN, INTO><<<dim3(unsigned(tm * tn), unsigned(parts)), WM * WN * kWave, 0, s>>>(
+        product_kernel<T, FM, FN, WM, WN, TB, INTO><<<dim3(unsigned(tm * tn), unsigned(parts)), WM * WN * kWave, 0, s>>>(
             A, B, steps, ceil_div(steps, parts), tm, tn, o);
     });
 }
@@ -425,29 +425,29 @@ inline Targets from_row(Targets t, int64_t row) {
 
 constexpr int64_t kKeptBytes = int64_t(2) << 30;  // exponentials of the rows taken at a time, at most
 
-// rows of k as an operand: as they are, or packed
+// rows as an operand: as they are, or packed to whole steps
 template <typename T>
 bool as_operand(const DenseRows& x) {
-    return on_boundaries(x.p, x.ld, x.dt) && x.n % (kStepBytes / int(sizeof(T))) == 0;
+    return on_boundaries(x.p, x.ld, x.dt) && x.n % (kStepBytes / int(sizeof(T))) == 0 &&
+           x.ld * int64_t(sizeof(T)) < kMostStride;
+}
+template <typename T, bool MASK>
+Operand packed(const DenseRows& x, T* p, int64_t ld, const Targets& t, const float* weight, int64_t V, hipStream_t s) {
+    if (x.m > 0)
+        pack_rows<T, MASK><<<grid_of(x.m * ld * int64_t(sizeof(T)) / 16), kBlock, 0, s>>>(
+            static_cast<const T*>(x.p), x.ld, x.m, x.n, p, ld, t, weight, V);
+    return {p, ld, x.m, 0};
 }
 template <typename T>
 Operand operand_rows(const DenseRows& x, Carver& c, hipStream_t s) {
-    if (as_operand<T>(x)) return {x.p, x.ld, x.m};
+    if (as_operand<T>(x)) return {x.p, x.ld, x.m, 0};
     const int64_t ld = round_up(x.n, kStepBytes / int(sizeof(T)));
     T* p = c.get<T>(x.m * ld);
-    if (c.base && x.m > 0)
-        pack_rows<T><<<grid_of(x.m * ld * int64_t(sizeof(T)) / 16), kBlock, 0, s>>>(static_cast<const T*>(x.p), x.ld,
-                                                                                 x.m, x.n, p, ld);
-    return {p, ld, x.m};
+    if (!c.base) return {nullptr, ld, x.m, 0};
+    return packed<T, false>(x, p, ld, Targets(), nullptr, 0, s);
 }
-template <typename T, bool MASK>
-Operand operand_columns(const DenseRows& x, const Targets& t, const float* weight, int64_t V, T* p, hipStream_t s) {
-    const int64_t ld = round_up(x.m, kStepBytes / int(sizeof(T)));
-    if (ld > 0)
-        pack_transposed<T, MASK><<<unsigned(ceil_div(x.n, kSide) * ceil_div(ld, kSide)), kBlock, 0, s>>>(
-            static_cast<const T*>(x.p), x.ld, x.m, x.n, p, ld, t, weight, V);
-    return {p, ld, x.n};
-}
+// the same memory with its rows as the depth of a product
+inline Operand turned(const Operand& o, int64_t columns) { return {o.p, o.ld, columns, o.rows}; }
 
 template <typename T>
 size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, float scale, float* loss, float* lse,
@@ -464,7 +464,7 @@ size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, f
     const int64_t steps = ceil_div(X.n, kStepBytes / int(sizeof(T)));
     for (int64_t r0 = 0; r0 < X.m; r0 += chunk) {
         const int64_t n = std::min(chunk, X.m - r0);
-        const Operand xr{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n};
+        const Operand xr{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n, 0};
         const Targets tr = from_row(t, r0);
         const int side = side_of(W.m, n);
         const int64_t tm = ceil_div(W.m, side), tn = ceil_div(n, side);
@@ -485,7 +485,7 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
                           float* loss, const DenseRows& dX, const DenseRows& dW, char* tmp, hipStream_t s) {
     constexpr int64_t STEP = kStepBytes / int(sizeof(T));
     const int64_t V = W.m, D = W.n, Vp = round_up(V, STEP);
-    // rows at a time: a whole number of steps (of dW's product) and of tiles
+    // rows at a time: whole tiles
     const int64_t chunk =
         std::max<int64_t>(kWide, std::min({round_up(X.m, kWide), kKeptBytes / int64_t(sizeof(T)) / Vp / kWide * kWide,
                                            int64_t(1) << 17}));
@@ -495,8 +495,8 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
     Piece* pieces = c.get<Piece>(most * ceil_div(V, kNarrow));
     float *hit = c.get<float>(most), *lse = c.get<float>(most), *unit = c.get<float>(1);
     T* E = c.get<T>(most * Vp);
-    const int64_t mostp = round_up(most, STEP);
-    T *GT = c.get<T>(V * mostp), *WT = c.get<T>(D * Vp), *XT = c.get<T>(D * mostp);
+    const int64_t xld = round_up(D, 16 / int64_t(sizeof(T)));
+    T* XM = c.get<T>(most * xld);
     const int64_t sumld = round_up(D, 4);
     float* sums = chunks > 1 ? c.get<float>(V * sumld) : nullptr;
     const int64_t steps_v = Vp / STEP, parts = parts_of(D, most, steps_v);
@@ -506,19 +506,18 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
     constexpr bool HALF = sizeof(T) == 2;
     if (HALF)
         weight_unit<<<1, 1024, 0, s>>>(t, weight, V, X.m, std::is_same<T, _Float16>::value ? 0x1p-14f : 1.f, unit);
-    const Operand wt = X.m ? operand_columns<T, false>(W, Targets(), nullptr, 0, WT, s) : Operand();
     Product out;
     out.alpha = scale;
     out.unit = HALF ? unit : nullptr;
     for (int64_t r0 = 0; r0 < X.m || r0 == 0; r0 += chunk) {
-        const int64_t n = std::min(chunk, X.m - r0), np = round_up(n, STEP);
+        const int64_t n = std::min(chunk, X.m - r0);
         const Targets tr = from_row(t, r0);
         const float* wr = weight ? weight + r0 : nullptr;
         DenseRows xr = X;
         xr.m = n;
         xr.p = static_cast<char*>(X.p) + r0 * X.ld * int64_t(sizeof(T));
         if (n > 0) {
-            const Operand xo{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n};
+            const Operand xo{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n, 0};
             const int here = side_of(V, n);
             const int64_t tm = ceil_div(V, here), tn = ceil_div(n, here);
             by_tile<T>(here, [&](auto fm, auto fn, auto wm, auto wn) {
@@ -528,8 +527,9 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
                     w, xo, ceil_div(D, STEP), scale, tr, tm, tn, pieces, hit, E, Vp);
             });
             join_pieces<<<grid_of(n * kWave), kBlock, 0, s>>>(pieces, tm, n, hit, tr, V, loss + r0, lse);
-            fold<T><<<dim3(unsigned(ceil_div(Vp, kSide)), unsigned(ceil_div(np, kSide))), kBlock, 0, s>>>(
-                E, Vp, n, V, pieces, tm, here, lse, loss + r0, tr, wr, out.unit, GT, np);
+            const int64_t span = kBlock * kFoldPacks * 16 / int64_t(sizeof(T));
+            fold<T><<<unsigned(n * ceil_div(Vp, span)), kBlock, 0, s>>>(E, Vp, n, V, pieces, tm, here, lse, loss + r0,
+                                                                       tr, wr, out.unit);
             // dx = G W
             Product dx = out;
             dx.out = static_cast<T*>(dX.p) + r0 * dX.ld;
@@ -537,16 +537,16 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
             dx.t = tr;
             dx.weight = wr;
             dx.V = V;
-            const Operand g{E, Vp, n};
+            const Operand g{E, Vp, n, 0}, wt = turned(w, D);
             const int64_t p = std::min(parts, parts_of(D, n, steps_v));
             if (p > 1) {
                 dx.sums = dxparts;
                 dx.lds = sumld;
                 dx.plane = n * sumld;
-                launch_product<T, kPart>(wt, g, steps_v, p, dx, s);
+                launch_product<T, false, kPart>(wt, g, steps_v, p, dx, s);
                 join_parts<T><<<grid_of(n * sumld / 4), kBlock, 0, s>>>(dx, p, n, D);
             } else {
-                launch_product<T, kStore>(wt, g, steps_v, 1, dx, s);
+                launch_product<T, false, kStore>(wt, g, steps_v, 1, dx, s);
             }
         }
         // dW = G^T x
@@ -557,12 +557,11 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
         dw.lds = sumld;
         dw.first = r0 == 0;
         dw.last = r0 + chunk >= X.m;
-        const Operand xt = operand_columns<T, true>(xr, tr, wr, V, XT, s);
-        const Operand gt{GT, np, V};
+        const Operand xt = turned(packed<T, true>(xr, XM, xld, tr, wr, V, s), D), gt{E, Vp, V, n};
         if (sums)
-            launch_product<T, kAdd>(xt, gt, np / STEP, 1, dw, s);
+            launch_product<T, true, kAdd>(xt, gt, ceil_div(n, STEP), 1, dw, s);
         else
-            launch_product<T, kStore>(xt, gt, np / STEP, 1, dw, s);
+            launch_product<T, true, kStore>(xt, gt, ceil_div(n, STEP), 1, dw, s);
     }
     return 0;
 }
