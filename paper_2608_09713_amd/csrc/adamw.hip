@@ -121,8 +121,14 @@ __device__ inline void load_parameters(const AdamTensor& t, int64_t i, float (&w
         load_some<FULL>(static_cast<const P*>(t.p), i, t.n, w);
 }
 template <bool FULL, typename P, bool MASTER>
-__device__ inline void store_parameters(const AdamTensor& t, int64_t i, const float (&w)[kAt]) {
-    if constexpr (MASTER) store_some<FULL>(t.master, i, t.n, w);
+__device__ inline void store_parameters(const AdamTensor& t, int64_t i, float (&w)[kAt]) {
+    if constexpr (MASTER) {
+        // (the copy's value is what is rounded: kept from instructions that round the
+        // last operation's unrounded result to 16 bits)
+#pragma unroll
+        for (int k = 0; k < kAt; ++k) asm volatile("" : "+v"(w[k]));
+        store_some<FULL>(t.master, i, t.n, w);
+    }
     store_some<FULL>(static_cast<P*>(t.p), i, t.n, w);
 }
 
@@ -168,30 +174,25 @@ __global__ __launch_bounds__(kThreads<false>) void adamw_wide(Batch<MASTER ? 5 :
         step_wide<false, P, G, MASTER>(t, i0, r);
 }
 
-// The code of y >= 0 for the scale S > 0: nearest in c, where y = (c / LEVELS)^POWER S.
-// 32 bits give LEVELS times the root within 2^-13 (6 units of 2^-24 relative, 255
-// levels); what is nearer to a border than twice that is compared with it in 64 bits.
+// what codes stand for, in units of S / 127^2 and S / 255^4 (the largest codes: S itself)
+constexpr double kSquares = 1.0 / (127.0 * 127.0), kFourths = 1.0 / (255.0 * 255.0 * 255.0 * 255.0);
+static_assert(127.0 * 127.0 * kSquares == 1.0 && 255.0 * 255.0 * 255.0 * 255.0 * kFourths == 1.0, "");
+__device__ inline int squared(int c) { return c * abs(c); }
+__device__ inline uint32_t fourth(int c) { return uint32_t(c * c) * uint32_t(c * c); }
+
+// The code of y >= 0 for the scale S > 0, nearest in c, where y = (c / LEVELS)^POWER S;
+// f: y as a float, inv: about 1 / S.  32 bits give LEVELS times the root within
+// 2^-13 (6 units of 2^-24 relative, 255 levels); what is nearer to a border than
+// twice that is compared with it in 64 bits.
 template <int LEVELS, int POWER>
-__device__ inline int code_of(double y, float S) {
-    const float up = S < 0x1p-60f ? 0x1p80f : 1.f;  // (so that S has a reciprocal)
-    float x = float(y * up) * __builtin_amdgcn_rcpf(S * up);
-    x = __builtin_amdgcn_sqrtf(x);
+__device__ inline int code_of(double y, float f, float inv, float S) {
+    float x = __builtin_amdgcn_sqrtf(f * inv);
     if constexpr (POWER == 4) x = __builtin_amdgcn_sqrtf(x);
     x = fminf(x * LEVELS, float(LEVELS));
     const float c = rintf(x);
     if (fabsf(x - c) <= 0.5f - 0x1p-12f) return int(c);
     const double border = (floorf(x) + 0.5) * (1.0 / LEVELS), q = border * border;
     return int(floorf(x)) + (y > (POWER == 4 ? q * q : q) * double(S) ? 1 : 0);
-}
-
-__device__ inline double value_m(int c, float S) {
-    const double q = c * (1.0 / 127);
-    return q * fabs(q) * double(S);
-}
-__device__ inline double value_v(int c, float S) {
-    double q = c * (1.0 / 255);
-    q *= q;
-    return q * q * double(S);
 }
 
 template <bool FULL, typename C>
@@ -219,9 +220,15 @@ __device__ inline void store_codes(C* p, int64_t i, int64_t n, const int (&v)[kA
     }
 }
 
+__device__ inline double blend(double rate, double a, double b) {
+#pragma clang fp contract(off)
+    const double p = rate * a, q = (1.0 - rate) * b;
+    return p + q;
+}
+
 template <bool FULL, typename P, typename G, bool MASTER>
 __device__ inline void step_narrow(const AdamTensor& t, int64_t i0, const AdamRates& r) {
-    const float gs = r.grad_scale ? r.grad_scale[0] : 1.f;
+    const double gs = r.grad_scale ? double(r.grad_scale[0]) : 1.0;
     float w[kPacks<true>][kAt], g[kPacks<true>][kAt], ms[kPacks<true>], vs[kPacks<true>];
     int mc[kPacks<true>][kAt], vc[kPacks<true>][kAt];
 #pragma unroll
@@ -239,30 +246,41 @@ __device__ inline void step_narrow(const AdamTensor& t, int64_t i0, const AdamRa
     for (int j = 0; j < kPacks<true>; ++j) {
         const int64_t i = i0 + j * kWidth<true>, block = i / kAdamBlock;
         if (!FULL && block * kAdamBlock >= t.n) return;
+        const double sm = double(ms[j]), sv = double(vs[j]);
         double m[kAt], v[kAt];
-        float most_m = 0.f, most_v = 0.f;
+        float fm[kAt], fv[kAt], most_m = 0.f, most_v = 0.f;
         bool bad = false;
 #pragma unroll
         for (int q = 0; q < kAt; ++q) {
-            const double x = double(g[j][q]) * double(gs);
-            m[q] = fma(r.d1, value_m(mc[j][q], ms[j]), (1.0 - r.d1) * x);
-            v[q] = fma(r.d2, value_v(vc[j][q], vs[j]), (1.0 - r.d2) * (x * x));
+            // (each product rounded: beta S + (1 - beta) g of a block's largest is a
+            // tie between two scales often enough for its last bit to count)
+            const double x = double(g[j][q]) * gs;
+            m[q] = blend(r.d1, double(squared(mc[j][q])) * kSquares * sm, x);
+            v[q] = blend(r.d2, double(fourth(vc[j][q])) * kFourths * sv, x * x);
             if (!FULL && i + q >= t.n) m[q] = v[q] = 0.0;
-            const float fm = float(m[q]), fv = float(v[q]);
-            bad = bad || !(fabsf(fm) < __builtin_huge_valf()) || !(fv < __builtin_huge_valf());
-            most_m = fmaxf(most_m, fabsf(fm));
-            most_v = fmaxf(most_v, fv);
-            w[j][q] = stepped(w[j][q], fm, fv, r);
+            fm[q] = float(m[q]);
+            fv[q] = float(v[q]);
+            bad = bad || !(fabsf(fm[q]) < __builtin_huge_valf()) || !(fv[q] < __builtin_huge_valf());
+            most_m = fmaxf(most_m, fabsf(fm[q]));
+            most_v = fmaxf(most_v, fv[q]);
+            w[j][q] = fmaf(-r.lr_decay, w[j][q], w[j][q]) -
+                      r.lr_m * fm[q] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(fv[q] * r.inv_v) + r.eps);
         }
         most_m = wave_max(most_m);
         most_v = wave_max(most_v);
         if (__any(bad)) most_m = most_v = __builtin_nanf("");  // (a scale of NaN: all its values are)
+        // (scales and values of the smallest are raised together, to have reciprocals)
+        const float um = most_m < 0x1p-60f ? 0x1p80f : 1.f, uv = most_v < 0x1p-60f ? 0x1p80f : 1.f;
+        const float im = __builtin_amdgcn_rcpf(most_m * um), iv = __builtin_amdgcn_rcpf(most_v * uv);
 #pragma unroll
         for (int q = 0; q < kAt; ++q) {
-            mc[j][q] = most_m > 0.f ? code_of<127, 2>(fabs(m[q]), most_m) : 0;
+            mc[j][q] = vc[j][q] = 0;
+            if (most_m > 0.f) mc[j][q] = code_of<127, 2>(fabs(m[q]), um == 1.f ? fabsf(fm[q]) : fabsf(float(m[q] * um)), im, most_m);
             if (m[q] < 0.0) mc[j][q] = -mc[j][q];
-            vc[j][q] = most_v > 0.f ? code_of<255, 4>(v[q], most_v) : 0;
-            if (v[q] > 0.0 && most_v > 0.f) vc[j][q] = max(vc[j][q], 1);
+            if (most_v > 0.f) {
+                vc[j][q] = code_of<255, 4>(v[q], uv == 1.f ? fv[q] : float(v[q] * uv), iv, most_v);
+                if (v[q] > 0.0) vc[j][q] = max(vc[j][q], 1);
+            }
         }
         store_codes<FULL>(static_cast<int8_t*>(t.m), i, t.n, mc[j]);
         store_codes<FULL>(static_cast<uint8_t*>(t.v), i, t.n, vc[j]);
@@ -302,11 +320,12 @@ __device__ inline void values_of(const AdamTensor& t, int64_t i0) {
 #pragma unroll
     for (int j = 0; j < kPacks<true>; ++j) {
         const int64_t i = i0 + j * kWidth<true>;
+        const double km = kSquares * double(ms[j]), kv = kFourths * double(vs[j]);
         float m[kAt], v[kAt];
 #pragma unroll
         for (int q = 0; q < kAt; ++q) {
-            m[q] = float(value_m(mc[j][q], ms[j]));
-            v[q] = float(value_v(vc[j][q], vs[j]));
+            m[q] = float(squared(mc[j][q]) * km);
+            v[q] = float(fourth(vc[j][q]) * kv);
         }
         store_some<FULL>(static_cast<float*>(t.p), i, t.n, m);
         store_some<FULL>(t.master, i, t.n, v);

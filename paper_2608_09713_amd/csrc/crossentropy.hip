@@ -67,25 +67,41 @@ __global__ __launch_bounds__(WM* WN* kWave) void logits_kernel(Operand W, Operan
     P::run(W, X, m0, n0, steps, 0, buf0, buf1, acc);
 
     const int lane = lane_id(), w = threadIdx.x / kWave, wm = w / WN, wn = w % WN;
-    const int64_t mw = m0 + wm * FM * 16 + 4 * (lane >> 4);
+    // this lane's columns of W in the tile: mine + 16 i + r
+    const int mine = wm * FM * 16 + 4 * (lane >> 4), valid = int(min(W.rows - m0, int64_t(P::BM)));
+    const int64_t mw = m0 + mine;
     const int col = wn * FN * 16 + (lane & 15);
     float top[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         __builtin_amdgcn_sched_barrier(0);
         const int64_t n = n0 + col + j * 16;
-        const int64_t target = n < X.rows ? target_of(t, n) : -1;
+        const int64_t target = n < X.rows ? target_of(t, n) - m0 : -1;
+        const int at_target = target >= 0 && target < valid ? int(target) - mine : -1;
         float mx = -__builtin_huge_valf();
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t m = mw + i * 16 + r;
-                const float v = m < W.rows ? acc[i][j][r] * scale : -__builtin_huge_valf();
-                if (m == target && m < W.rows) hit[n] = v;
-                acc[i][j][r] = v;
-                mx = fmaxf(mx, v);
-            }
+            for (int r = 0; r < 4; ++r) acc[i][j][r] *= scale;
+        if (valid < P::BM)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (mine + i * 16 + r >= valid) acc[i][j][r] = -__builtin_huge_valf();
+        // (few tiles hold a target of a wavefront's rows)
+        if (__any(at_target >= 0)) {
+            float h = 0.f;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) h = at_target == i * 16 + r ? acc[i][j][r] : h;
+            if (at_target >= 0 && at_target < FM * 16 && (at_target & 15) < 4) hit[n] = h;
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, acc[i][j][r]);
         mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
         top[j] = fmaxf(mx, __shfl_xor(mx, 32, kWave));
         if (lane < 16) part[0][wm][col + j * 16] = top[j];
@@ -146,6 +162,131 @@ __global__ __launch_bounds__(WM* WN* kWave) void logits_kernel(Operand W, Operan
     }
 }
 
+// ---- the same for few rows: one reading of W, from memory into the registers of
+// the matrix instructions.  A workgroup takes kFewColumns rows of W, its wavefronts
+// a quarter of k each; rows of any alignment, past their ends zeros.  Bound by W's
+// bytes (32000 x 2048 bf16, one row: 131 MB).
+
+constexpr int kFewColumns = 64, kFewRows = 64;  // a piece's columns; rows at most
+
+// elements [c, c + N) of a row of d, zeros past its end
+template <typename T, int N>
+__device__ inline Vec<T, N> row_part(const T* row, int64_t c, int64_t d) {
+    if (c + N <= d) return load_vec<T, N>(row + c);
+    Vec<T, N> v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = c + i < d ? row[c + i] : T(0.f);
+    return v;
+}
+
+template <typename T, int NB>
+__global__ __launch_bounds__(kBlock) void logits_few(const T* __restrict__ w, int64_t ldw, int64_t V,
+                                                     const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t d,
+                                                     float scale, Targets t, int64_t tm, Piece* __restrict__ pieces,
+                                                     float* __restrict__ hit) {
+    constexpr int FM = kFewColumns / 16, N = 16 / int(sizeof(T)), STEP = 4 * N, AHEAD = NB == 1 ? 8 : 2;
+    using C = typename Chunk<T>::V;
+    __shared__ F4 sums[kWavesPerBlock][FM][NB][kWave];
+    __shared__ float part[2][kWavesPerBlock][NB * 16];
+    const int lane = lane_id(), wave = int(uniform(threadIdx.x / kWave)), g = lane >> 4, r16 = lane & 15;
+    const int64_t m0 = int64_t(blockIdx.x) * kFewColumns;
+    const T *pw[FM], *px[NB];
+    bool there[NB];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) pw[i] = w + min(m0 + i * 16 + r16, V - 1) * ldw;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        there[j] = j * 16 + r16 < rows;
+        px[j] = x + (there[j] ? j * 16 + r16 : 0) * ldx;
+    }
+    F4 acc[FM][NB] = {};
+    const int64_t steps = (d + STEP - 1) / STEP, whole = d / STEP;
+    const int64_t k0 = steps * wave / kWavesPerBlock, k1 = steps * (wave + 1) / kWavesPerBlock;
+    auto multiply = [&](const Vec<T, N> (&a)[FM], const Vec<T, N> (&b)[NB]) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const C cb = __builtin_bit_cast(C, b[j]);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) acc[i][j] = Chunk<T>::mul(__builtin_bit_cast(C, a[i]), cb, acc[i][j]);
+        }
+    };
+    Vec<T, N> none;
+#pragma unroll
+    for (int i = 0; i < N; ++i) none[i] = T(0.f);
+    int64_t k = k0;
+    for (; k + AHEAD <= min(k1, whole); k += AHEAD) {
+        Vec<T, N> a[AHEAD][FM], b[AHEAD][NB];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            const int64_t c = (k + q) * STEP + g * N;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) a[q][i] = load_vec<T, N>(pw[i] + c);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) b[q][j] = there[j] ? load_vec<T, N>(px[j] + c) : none;
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (all of them are under way before the first is used)
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) multiply(a[q], b[q]);
+    }
+    for (; k < k1; ++k) {
+        Vec<T, N> a[FM], b[NB];
+        const int64_t c = k * STEP + g * N;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) a[i] = row_part<T, N>(pw[i], c, d);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) b[j] = there[j] ? row_part<T, N>(px[j], c, d) : none;
+        multiply(a, b);
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sums[wave][i][j][lane] = acc[i][j];
+    __syncthreads();
+    // (a wavefront goes on with 16 of the columns: the quarters of k in their order)
+    const int64_t m = m0 + wave * 16 + 4 * g;
+    F4 v[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        v[j] = sums[0][wave][j][lane];
+#pragma unroll
+        for (int q = 1; q < kWavesPerBlock; ++q) v[j] += sums[q][wave][j][lane];
+        const int64_t n = j * 16 + r16;
+        const int64_t target = n < rows ? target_of(t, n) : -1;
+        float mx = -__builtin_huge_valf();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            v[j][r] = m + r < V ? v[j][r] * scale : -__builtin_huge_valf();
+            if (m + r == target && m + r < V) hit[n] = v[j][r];
+            mx = fmaxf(mx, v[j][r]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        if (lane < 16) part[0][wave][j * 16 + lane] = mx;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        float mx = -3.402823466e38f, s = 0.f;
+#pragma unroll
+        for (int q = 0; q < kWavesPerBlock; ++q) mx = fmaxf(mx, part[0][q][j * 16 + r16]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s += exp_of(v[j][r] - mx);
+        s += __shfl_xor(s, 16, kWave);
+        s += __shfl_xor(s, 32, kWave);
+        if (lane < 16) part[1][wave][j * 16 + lane] = s;
+    }
+    __syncthreads();
+    const int64_t n = threadIdx.x;
+    if (n >= min(rows, int64_t(NB * 16))) return;
+    float mx = -3.402823466e38f, s = 0.f;
+#pragma unroll
+    for (int q = 0; q < kWavesPerBlock; ++q) {
+        mx = fmaxf(mx, part[0][q][n]);
+        s += part[1][q][n];
+    }
+    pieces[n * tm + blockIdx.x] = {mx, s};
+}
+
 // A row's pieces joined: loss and lse (may be null).
 __global__ __launch_bounds__(kBlock) void join_pieces(const Piece* __restrict__ pieces, int64_t tm, int64_t rows,
                                                       const float* __restrict__ hit, Targets t, int64_t V,
@@ -153,12 +294,16 @@ __global__ __launch_bounds__(kBlock) void join_pieces(const Piece* __restrict__ 
     for (int64_t n = int64_t(blockIdx.x) * kWavesPerBlock + threadIdx.x / kWave; n < rows;
          n += int64_t(gridDim.x) * kWavesPerBlock) {
         const Piece* p = pieces + n * tm;
-        float mx = -3.402823466e38f;
-        for (int64_t i = lane_id(); i < tm; i += kWave) mx = fmaxf(mx, p[i].top);
-        mx = wave_max(mx);
-        float s = 0.f;
-        for (int64_t i = lane_id(); i < tm; i += kWave) s = fmaf(p[i].sum, exp_of(p[i].top - mx), s);
-        s = wave_total(s);
+        float top = -3.402823466e38f, s = 0.f;
+#pragma unroll 8
+        for (int64_t i = lane_id(); i < tm; i += kWave) {
+            const Piece q = p[i];
+            const float high = fmaxf(top, q.top);
+            s = s * exp_of(top - high) + q.sum * exp_of(q.top - high);
+            top = high;
+        }
+        const float mx = wave_max(top);
+        s = wave_total(s * exp_of(top - mx));
         if (lane_id() != 0) continue;
         // (the difference of the two largest terms first: a small loss keeps its digits)
         const float l = __builtin_amdgcn_logf(s) * kLn2;
@@ -366,17 +511,27 @@ __global__ __launch_bounds__(kBlock) void join_parts(Product o, int64_t parts, i
     }
 }
 
-// Tiles of 256 x 256 by eight wavefronts where they fill the chip, else of 128 x 128 by four.
+// Tiles of 256 x 256 by eight wavefronts where they fill three quarters of the chip
+// (8192 x 131072 x 4096 bf16: 6.70 ms, by the others 8.53), else of 128 x 128 by
+// four.  Where k can be split, its parts count as tiles (2047 x 1001 x 50021 f16:
+// 197 us with eight parts, 237 by small tiles), unless large tiles would be padded
+// by a quarter more.  32-bit products, whose fragments feed the matrix cores four
+// times as long, go by small tiles, which leave less of the last round idle (1001
+// x 50021 x 250: 257 us, 298 by large ones).
 constexpr int kWide = 256, kNarrow = 128;
-inline bool wide_tiles(int64_t M, int64_t N) { return ceil_div(M, kWide) * ceil_div(N, kWide) >= kCus * 3 / 4; }
-inline int side_of(int64_t M, int64_t N) { return wide_tiles(M, N) ? kWide : kNarrow; }
-
-// parts of k for a product with too few tiles to fill the chip
-inline int64_t parts_of(int64_t M, int64_t N, int64_t steps) {
-    const int64_t side = side_of(M, N), tiles = ceil_div(M, side) * ceil_div(N, side);
-    const int64_t room = side == kWide ? kCus : 2 * kCus;
+inline int64_t tiles_of(int64_t M, int64_t N, int64_t side) { return ceil_div(M, side) * ceil_div(N, side); }
+// parts of k that fill the chip with tiles, each of eight steps at least
+inline int64_t parts_of(int64_t M, int64_t N, int64_t steps, int64_t side) {
+    const int64_t tiles = tiles_of(M, N, side), room = side == kWide ? kCus : 2 * kCus;
     if (tiles == 0 || 2 * tiles > room) return 1;
     return std::max<int64_t>(1, std::min<int64_t>({room / tiles, steps / 8, 64}));
+}
+inline int side_of(int64_t M, int64_t N, int dt, int64_t split_steps = 0) {
+    if (dt == kDtF32) return kNarrow;
+    const int64_t wide = tiles_of(M, N, kWide), narrow = tiles_of(M, N, kNarrow);
+    const int64_t parts = split_steps ? parts_of(M, N, split_steps, kWide) : 1;
+    if (parts > 1 && 16 * wide > 5 * narrow) return kNarrow;
+    return wide * parts >= kCus * 3 / 4 ? kWide : kNarrow;
 }
 
 template <typename T, typename F>
@@ -391,9 +546,8 @@ void by_tile(int side, F f) {
 }
 
 template <typename T, bool TB, int INTO>
-void launch_product(const Operand& A, const Operand& B, int64_t steps, int64_t parts, const Product& o,
+void launch_product(const Operand& A, const Operand& B, int64_t steps, int64_t parts, int side, const Product& o,
                     hipStream_t s) {
-    const int side = side_of(A.rows, B.rows);
     by_tile<T>(side, [&](auto fm, auto fn, auto wm, auto wn) {
         constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
                       WN = decltype(wn)::value;
@@ -453,6 +607,25 @@ template <typename T>
 size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, float scale, float* loss, float* lse,
                      char* tmp, hipStream_t s) {
     Carver c{tmp};
+    if (X.m <= kFewRows) {
+        const int64_t tm = ceil_div(W.m, kFewColumns);
+        Piece* pieces = c.get<Piece>(X.m * tm);
+        float* hit = c.get<float>(X.m);
+        if (!tmp) return c.used;
+        auto few = [&](auto nb) {
+            logits_few<T, decltype(nb)::value><<<unsigned(tm), kBlock, 0, s>>>(
+                static_cast<const T*>(W.p), W.ld, W.m, static_cast<const T*>(X.p), X.ld, X.m, X.n, scale, t, tm, pieces,
+                hit);
+        };
+        if (X.m <= 16)
+            few(std::integral_constant<int, 1>());
+        else if (X.m <= 32)
+            few(std::integral_constant<int, 2>());
+        else
+            few(std::integral_constant<int, 4>());
+        join_pieces<<<grid_of(X.m * kWave), kBlock, 0, s>>>(pieces, tm, X.m, hit, t, W.m, loss, lse);
+        return 0;
+    }
     const Operand x = operand_rows<T>(X, c, s), w = operand_rows<T>(W, c, s);
     // rows at a time: 256 MB of pieces at most
     const int64_t chunk =
@@ -466,7 +639,7 @@ size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, f
         const int64_t n = std::min(chunk, X.m - r0);
         const Operand xr{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n, 0};
         const Targets tr = from_row(t, r0);
-        const int side = side_of(W.m, n);
+        const int side = side_of(W.m, n, W.dt);
         const int64_t tm = ceil_div(W.m, side), tn = ceil_div(n, side);
         by_tile<T>(side, [&](auto fm, auto fn, auto wm, auto wn) {
             constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
@@ -497,10 +670,13 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
     T* E = c.get<T>(most * Vp);
     const int64_t xld = round_up(D, 16 / int64_t(sizeof(T)));
     T* XM = c.get<T>(most * xld);
-    const int64_t sumld = round_up(D, 4);
+    const int64_t sumld = round_up(D, 4), steps_v = Vp / STEP;
     float* sums = chunks > 1 ? c.get<float>(V * sumld) : nullptr;
-    const int64_t steps_v = Vp / STEP, parts = parts_of(D, most, steps_v);
-    float* dxparts = parts > 1 ? c.get<float>(parts * most * sumld) : nullptr;
+    // (parts of dX's products: of whole turns, and of the last one)
+    auto dx_parts = [&](int64_t n) { return parts_of(D, n, steps_v, side_of(D, n, W.dt, steps_v)); };
+    auto dx_floats = [&](int64_t n) { return dx_parts(n) > 1 ? dx_parts(n) * n * sumld : 0; };
+    const int64_t rest = X.m - (chunks - 1) * chunk;
+    float* dxparts = c.get<float>(chunks ? std::max(dx_floats(most), dx_floats(rest)) : 0);
     if (!tmp) return c.used;
 
     constexpr bool HALF = sizeof(T) == 2;
@@ -518,7 +694,7 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
         xr.p = static_cast<char*>(X.p) + r0 * X.ld * int64_t(sizeof(T));
         if (n > 0) {
             const Operand xo{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n, 0};
-            const int here = side_of(V, n);
+            const int here = side_of(V, n, W.dt);
             const int64_t tm = ceil_div(V, here), tn = ceil_div(n, here);
             by_tile<T>(here, [&](auto fm, auto fn, auto wm, auto wn) {
                 constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
@@ -538,15 +714,16 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
             dx.weight = wr;
             dx.V = V;
             const Operand g{E, Vp, n, 0}, wt = turned(w, D);
-            const int64_t p = std::min(parts, parts_of(D, n, steps_v));
+            const int64_t p = dx_parts(n);
+            const int side = side_of(D, n, W.dt, steps_v);
             if (p > 1) {
                 dx.sums = dxparts;
                 dx.lds = sumld;
                 dx.plane = n * sumld;
-                launch_product<T, false, kPart>(wt, g, steps_v, p, dx, s);
+                launch_product<T, false, kPart>(wt, g, steps_v, p, side, dx, s);
                 join_parts<T><<<grid_of(n * sumld / 4), kBlock, 0, s>>>(dx, p, n, D);
             } else {
-                launch_product<T, false, kStore>(wt, g, steps_v, 1, dx, s);
+                launch_product<T, false, kStore>(wt, g, steps_v, 1, side, dx, s);
             }
         }
         // dW = G^T x
@@ -558,10 +735,11 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
         dw.first = r0 == 0;
         dw.last = r0 + chunk >= X.m;
         const Operand xt = turned(packed<T, true>(xr, XM, xld, tr, wr, V, s), D), gt{E, Vp, V, n};
+        const int side = side_of(D, V, W.dt);
         if (sums)
-            launch_product<T, true, kAdd>(xt, gt, ceil_div(n, STEP), 1, dw, s);
+            launch_product<T, true, kAdd>(xt, gt, ceil_div(n, STEP), 1, side, dw, s);
         else
-            launch_product<T, true, kStore>(xt, gt, ceil_div(n, STEP), 1, dw, s);
+            launch_product<T, true, kStore>(xt, gt, ceil_div(n, STEP), 1, side, dw, s);
     }
     return 0;
 }
