@@ -180,16 +180,25 @@ static_assert(127.0 * 127.0 * kSquares == 1.0 && 255.0 * 255.0 * 255.0 * 255.0 *
 __device__ inline int squared(int c) { return c * abs(c); }
 __device__ inline uint32_t fourth(int c) { return uint32_t(c * c) * uint32_t(c * c); }
 
-// The code of y >= 0 for the scale S > 0, nearest in c, where y = (c / LEVELS)^POWER S;
-// f: y as a float, inv: about 1 / S.  32 bits give LEVELS times the root within
-// 2^-13 (6 units of 2^-24 relative, 255 levels); what is nearer to a border than
-// twice that is compared with it in 64 bits.
+// The code of y >= 0 for the scale S > 0, nearest in c, where y = (c / LEVELS)^POWER S.
+// code_near: from y as a float and about 1 / S.  32 bits give LEVELS times the root
+// within 2^-13 (6 units of 2^-24 relative, 255 levels); *near: it is within twice
+// that of a border, and code_at has to compare it with the border, in 64 bits.
 template <int LEVELS, int POWER>
-__device__ inline int code_of(double y, float f, float inv, float S) {
+__device__ inline float code_root(float f, float inv) {
     float x = __builtin_amdgcn_sqrtf(f * inv);
     if constexpr (POWER == 4) x = __builtin_amdgcn_sqrtf(x);
-    x = fminf(x * LEVELS, float(LEVELS));
-    const float c = rintf(x);
+    return fminf(x * LEVELS, float(LEVELS));
+}
+template <int LEVELS, int POWER>
+__device__ inline int code_near(float f, float inv, bool* near) {
+    const float x = code_root<LEVELS, POWER>(f, inv), c = rintf(x);
+    *near = *near || fabsf(x - c) > 0.5f - 0x1p-12f;
+    return int(c);
+}
+template <int LEVELS, int POWER>
+__device__ inline int code_at(double y, float f, float inv, float S) {
+    const float x = code_root<LEVELS, POWER>(f, inv), c = rintf(x);
     if (fabsf(x - c) <= 0.5f - 0x1p-12f) return int(c);
     const double border = (floorf(x) + 0.5) * (1.0 / LEVELS), q = border * border;
     return int(floorf(x)) + (y > (POWER == 4 ? q * q : q) * double(S) ? 1 : 0);
@@ -272,15 +281,36 @@ __device__ inline void step_narrow(const AdamTensor& t, int64_t i0, const AdamRa
         // (scales and values of the smallest are raised together, to have reciprocals)
         const float um = most_m < 0x1p-60f ? 0x1p80f : 1.f, uv = most_v < 0x1p-60f ? 0x1p80f : 1.f;
         const float im = __builtin_amdgcn_rcpf(most_m * um), iv = __builtin_amdgcn_rcpf(most_v * uv);
+        if (um != 1.f || uv != 1.f)
+#pragma unroll
+            for (int q = 0; q < kAt; ++q) {
+                fm[q] = float(m[q] * um);
+                fv[q] = float(v[q] * uv);
+            }
+        if (most_m > 0.f && most_v > 0.f) {
+            bool near = false;
+#pragma unroll
+            for (int q = 0; q < kAt; ++q) {
+                mc[j][q] = code_near<127, 2>(fabsf(fm[q]), im, &near);
+                vc[j][q] = code_near<255, 4>(fv[q], iv, &near);
+            }
+            if (__any(near))
+#pragma unroll
+                for (int q = 0; q < kAt; ++q) {
+                    mc[j][q] = code_at<127, 2>(fabs(m[q]), fabsf(fm[q]), im, most_m);
+                    vc[j][q] = code_at<255, 4>(v[q], fv[q], iv, most_v);
+                }
+        } else {
+#pragma unroll
+            for (int q = 0; q < kAt; ++q) {
+                mc[j][q] = most_m > 0.f ? code_at<127, 2>(fabs(m[q]), fabsf(fm[q]), im, most_m) : 0;
+                vc[j][q] = most_v > 0.f ? code_at<255, 4>(v[q], fv[q], iv, most_v) : 0;
+            }
+        }
 #pragma unroll
         for (int q = 0; q < kAt; ++q) {
-            mc[j][q] = vc[j][q] = 0;
-            if (most_m > 0.f) mc[j][q] = code_of<127, 2>(fabs(m[q]), um == 1.f ? fabsf(fm[q]) : fabsf(float(m[q] * um)), im, most_m);
             if (m[q] < 0.0) mc[j][q] = -mc[j][q];
-            if (most_v > 0.f) {
-                vc[j][q] = code_of<255, 4>(v[q], uv == 1.f ? fv[q] : float(v[q] * uv), iv, most_v);
-                if (v[q] > 0.0) vc[j][q] = max(vc[j][q], 1);
-            }
+            if (most_v > 0.f && v[q] > 0.0) vc[j][q] = max(vc[j][q], 1);
         }
         store_codes<FULL>(static_cast<int8_t*>(t.m), i, t.n, mc[j]);
         store_codes<FULL>(static_cast<uint8_t*>(t.v), i, t.n, vc[j]);
