@@ -360,8 +360,7 @@ __global__ __launch_bounds__(kBlock) void pack_rows(const T* __restrict__ src, i
     }
 }
 
-// G in E's place, zeros from V to lde.  piece: columns that share a base.  A
-// workgroup takes kFoldColumns of some rows.
+// G in E's place, zeros from V to lde.  piece: columns that share a base.
 constexpr int kFoldPacks = 4;  // of a thread, a workgroup's width apart
 template <typename T>
 __global__ __launch_bounds__(kBlock) void fold(T* __restrict__ E, int64_t lde, int64_t rows, int64_t V,
@@ -511,47 +510,73 @@ __global__ __launch_bounds__(kBlock) void join_parts(Product o, int64_t parts, i
     }
 }
 
-// Tiles of 256 x 256 by eight wavefronts where they fill three quarters of the chip
-// (8192 x 131072 x 4096 bf16: 6.70 ms, by the others 8.53), else of 128 x 128 by
-// four.  Where k can be split, its parts count as tiles (2047 x 1001 x 50021 f16:
-// 197 us with eight parts, 237 by small tiles), unless large tiles would be padded
-// by a quarter more.  32-bit products, whose fragments feed the matrix cores four
-// times as long, go by small tiles, which leave less of the last round idle (1001
-// x 50021 x 250: 257 us, 298 by large ones).
-constexpr int kWide = 256, kNarrow = 128;
-inline int64_t tiles_of(int64_t M, int64_t N, int64_t side) { return ceil_div(M, side) * ceil_div(N, side); }
+// Tiles of m by n.  16-bit products go by 256 x 256 and eight wavefronts where such
+// tiles fill three quarters of the chip (8192 x 131072 x 4096 bf16: 6.70 ms, by the
+// others 8.53), else by 128 x 128 and four.  Where k can be split, its parts count
+// as tiles (2047 x 1001 x 50021 f16: 197 us with eight parts, 237 by small tiles),
+// unless large tiles would be padded by a quarter more.  32-bit products, whose
+// fragments feed the matrix cores four times as long, go by small tiles, which leave
+// less of the last round idle (1001 x 50021 x 250: 257 us, 298 by large ones), or
+// by 128 x 64 where the busiest compute unit has less to do by those (217 x 36096 x
+// 1472: 229 us, 272 by 128 x 128; 25 x 44003 x 257 with its gradient: 123 and 169).
+struct Tile {
+    int m, n;
+};
+constexpr Tile kLarge{256, 256}, kSmall{128, 128}, kSlim{128, 64};
+inline int64_t tiles_of(int64_t M, int64_t N, Tile t) { return ceil_div(M, t.m) * ceil_div(N, t.n); }
 // parts of k that fill the chip with tiles, each of eight steps at least
-inline int64_t parts_of(int64_t M, int64_t N, int64_t steps, int64_t side) {
-    const int64_t tiles = tiles_of(M, N, side), room = side == kWide ? kCus : 2 * kCus;
+inline int64_t parts_of(int64_t M, int64_t N, int64_t steps, Tile t) {
+    const int64_t tiles = tiles_of(M, N, t), room = t.m == kLarge.m ? kCus : 2 * kCus;
     if (tiles == 0 || 2 * tiles > room) return 1;
     return std::max<int64_t>(1, std::min<int64_t>({room / tiles, steps / 8, 64}));
 }
-inline int side_of(int64_t M, int64_t N, int dt, int64_t split_steps = 0) {
-    if (dt == kDtF32) return kNarrow;
-    const int64_t wide = tiles_of(M, N, kWide), narrow = tiles_of(M, N, kNarrow);
-    const int64_t parts = split_steps ? parts_of(M, N, split_steps, kWide) : 1;
-    if (parts > 1 && 16 * wide > 5 * narrow) return kNarrow;
-    return wide * parts >= kCus * 3 / 4 ? kWide : kNarrow;
+inline Tile tile_of(int64_t M, int64_t N, int dt, int64_t split_steps = 0) {
+    if (dt == kDtF32) {
+        auto busiest = [&](Tile t) {
+            const int64_t parts = split_steps ? parts_of(M, N, split_steps, t) : 1;
+            return ceil_div(tiles_of(M, N, t) * parts, kCus) * ceil_div(std::max<int64_t>(split_steps, 1), parts) * t.n;
+        };
+        return busiest(kSlim) < busiest(kSmall) ? kSlim : kSmall;
+    }
+    const int64_t large = tiles_of(M, N, kLarge), small = tiles_of(M, N, kSmall);
+    const int64_t parts = split_steps ? parts_of(M, N, split_steps, kLarge) : 1;
+    if (parts > 1 && 16 * large > 5 * small) return kSmall;
+    return large * parts >= kCus * 3 / 4 ? kLarge : kSmall;
 }
 
+// f(fragments of A and of B, wavefronts along A and along B) of a tile
 template <typename T, typename F>
-void by_tile(int side, F f) {
+void by_tile(Tile t, F f) {
     using std::integral_constant;
-    if (side == kWide)
-        f(integral_constant<int, 8>(), integral_constant<int, 4>(), integral_constant<int, 2>(),
-          integral_constant<int, 4>());
-    else
-        f(integral_constant<int, 4>(), integral_constant<int, 4>(), integral_constant<int, 2>(),
-          integral_constant<int, 2>());
+    using Two = integral_constant<int, 2>;
+    using Four = integral_constant<int, 4>;
+    if constexpr (sizeof(T) == 2) {
+        if (t.m == kLarge.m) return f(integral_constant<int, 8>(), Four(), Two(), Four());
+    } else {
+        if (t.n == kSlim.n) return f(Four(), Two(), Two(), Two());
+    }
+    f(Four(), Four(), Two(), Two());
+}
+
+template <typename T, bool KEEP>
+void launch_logits(const Operand& W, const Operand& X, int64_t steps, float scale, const Targets& t, Tile tile,
+                   Piece* pieces, float* hit, T* E, int64_t lde, hipStream_t s) {
+    by_tile<T>(tile, [&](auto fm, auto fn, auto wm, auto wn) {
+        constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
+                      WN = decltype(wn)::value;
+        const int64_t tm = ceil_div(W.rows, tile.m), tn = ceil_div(X.rows, tile.n);
+        logits_kernel<T, FM, FN, WM, WN, KEEP><<<unsigned(tm * tn), WM * WN * kWave, 0, s>>>(
+            W, X, steps, scale, t, tm, tn, pieces, hit, E, lde);
+    });
 }
 
 template <typename T, bool TB, int INTO>
-void launch_product(const Operand& A, const Operand& B, int64_t steps, int64_t parts, int side, const Product& o,
+void launch_product(const Operand& A, const Operand& B, int64_t steps, int64_t parts, Tile tile, const Product& o,
                     hipStream_t s) {
-    by_tile<T>(side, [&](auto fm, auto fn, auto wm, auto wn) {
+    by_tile<T>(tile, [&](auto fm, auto fn, auto wm, auto wn) {
         constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
                       WN = decltype(wn)::value;
-        const int64_t tm = ceil_div(A.rows, side), tn = ceil_div(B.rows, side);
+        const int64_t tm = ceil_div(A.rows, tile.m), tn = ceil_div(B.rows, tile.n);
         product_kernel<T, FM, FN, WM, WN, TB, INTO><<<dim3(unsigned(tm * tn), unsigned(parts)), WM * WN * kWave, 0, s>>>(
             A, B, steps, ceil_div(steps, parts), tm, tn, o);
     });
@@ -579,12 +604,6 @@ inline Targets from_row(Targets t, int64_t row) {
 
 constexpr int64_t kKeptBytes = int64_t(2) << 30;  // exponentials of the rows taken at a time, at most
 
-// rows as an operand: as they are, or packed to whole steps
-template <typename T>
-bool as_operand(const DenseRows& x) {
-    return on_boundaries(x.p, x.ld, x.dt) && x.n % (kStepBytes / int(sizeof(T))) == 0 &&
-           x.ld * int64_t(sizeof(T)) < kMostStride;
-}
 template <typename T, bool MASK>
 Operand packed(const DenseRows& x, T* p, int64_t ld, const Targets& t, const float* weight, int64_t V, hipStream_t s) {
     if (x.m > 0)
@@ -592,10 +611,13 @@ Operand packed(const DenseRows& x, T* p, int64_t ld, const Targets& t, const flo
             static_cast<const T*>(x.p), x.ld, x.m, x.n, p, ld, t, weight, V);
     return {p, ld, x.m, 0};
 }
+// rows as an operand: as they are, or packed to whole steps
 template <typename T>
 Operand operand_rows(const DenseRows& x, Carver& c, hipStream_t s) {
-    if (as_operand<T>(x)) return {x.p, x.ld, x.m, 0};
-    const int64_t ld = round_up(x.n, kStepBytes / int(sizeof(T)));
+    const int64_t step = kStepBytes / int64_t(sizeof(T));
+    if (on_boundaries(x.p, x.ld, x.dt) && x.n % step == 0 && x.ld * int64_t(sizeof(T)) < kMostStride)
+        return {x.p, x.ld, x.m, 0};
+    const int64_t ld = round_up(x.n, step);
     T* p = c.get<T>(x.m * ld);
     if (!c.base) return {nullptr, ld, x.m, 0};
     return packed<T, false>(x, p, ld, Targets(), nullptr, 0, s);
@@ -629,9 +651,9 @@ size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, f
     const Operand x = operand_rows<T>(X, c, s), w = operand_rows<T>(W, c, s);
     // rows at a time: 256 MB of pieces at most
     const int64_t chunk =
-        std::max<int64_t>(kWide, std::min(X.m, (int64_t(1) << 25) / ceil_div(W.m, kNarrow) / kWide * kWide));
+        std::max<int64_t>(kLarge.m, std::min(X.m, (int64_t(1) << 25) / ceil_div(W.m, kSmall.m) / kLarge.m * kLarge.m));
     const int64_t most = std::min(X.m, chunk);
-    Piece* pieces = c.get<Piece>(most * ceil_div(W.m, kNarrow));
+    Piece* pieces = c.get<Piece>(most * ceil_div(W.m, kSmall.m));
     float* hit = c.get<float>(most);
     if (!tmp) return c.used;
     const int64_t steps = ceil_div(X.n, kStepBytes / int(sizeof(T)));
@@ -639,15 +661,9 @@ size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, f
         const int64_t n = std::min(chunk, X.m - r0);
         const Operand xr{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n, 0};
         const Targets tr = from_row(t, r0);
-        const int side = side_of(W.m, n, W.dt);
-        const int64_t tm = ceil_div(W.m, side), tn = ceil_div(n, side);
-        by_tile<T>(side, [&](auto fm, auto fn, auto wm, auto wn) {
-            constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
-                          WN = decltype(wn)::value;
-            logits_kernel<T, FM, FN, WM, WN, false><<<unsigned(tm * tn), WM * WN * kWave, 0, s>>>(
-                w, xr, steps, scale, tr, tm, tn, pieces, hit, static_cast<T*>(nullptr), 0);
-        });
-        join_pieces<<<grid_of(n * kWave), kBlock, 0, s>>>(pieces, tm, n, hit, tr, W.m, loss + r0,
+        const Tile tile = tile_of(W.m, n, W.dt);
+        launch_logits<T, false>(w, xr, steps, scale, tr, tile, pieces, hit, nullptr, 0, s);
+        join_pieces<<<grid_of(n * kWave), kBlock, 0, s>>>(pieces, ceil_div(W.m, tile.m), n, hit, tr, W.m, loss + r0,
                                                          lse ? lse + r0 : nullptr);
     }
     return 0;
@@ -660,12 +676,12 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
     const int64_t V = W.m, D = W.n, Vp = round_up(V, STEP);
     // rows at a time: whole tiles
     const int64_t chunk =
-        std::max<int64_t>(kWide, std::min({round_up(X.m, kWide), kKeptBytes / int64_t(sizeof(T)) / Vp / kWide * kWide,
+        std::max<int64_t>(kLarge.m, std::min({round_up(X.m, kLarge.m), kKeptBytes / int64_t(sizeof(T)) / Vp / kLarge.m * kLarge.m,
                                            int64_t(1) << 17}));
     const int64_t chunks = ceil_div(X.m, chunk), most = std::min(X.m, chunk);
     Carver c{tmp};
     const Operand x = operand_rows<T>(X, c, s), w = operand_rows<T>(W, c, s);
-    Piece* pieces = c.get<Piece>(most * ceil_div(V, kNarrow));
+    Piece* pieces = c.get<Piece>(most * ceil_div(V, kSmall.m));
     float *hit = c.get<float>(most), *lse = c.get<float>(most), *unit = c.get<float>(1);
     T* E = c.get<T>(most * Vp);
     const int64_t xld = round_up(D, 16 / int64_t(sizeof(T)));
@@ -673,7 +689,7 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
     const int64_t sumld = round_up(D, 4), steps_v = Vp / STEP;
     float* sums = chunks > 1 ? c.get<float>(V * sumld) : nullptr;
     // (parts of dX's products: of whole turns, and of the last one)
-    auto dx_parts = [&](int64_t n) { return parts_of(D, n, steps_v, side_of(D, n, W.dt, steps_v)); };
+    auto dx_parts = [&](int64_t n) { return parts_of(D, n, steps_v, tile_of(D, n, W.dt, steps_v)); };
     auto dx_floats = [&](int64_t n) { return dx_parts(n) > 1 ? dx_parts(n) * n * sumld : 0; };
     const int64_t rest = X.m - (chunks - 1) * chunk;
     float* dxparts = c.get<float>(chunks ? std::max(dx_floats(most), dx_floats(rest)) : 0);
@@ -694,17 +710,12 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
         xr.p = static_cast<char*>(X.p) + r0 * X.ld * int64_t(sizeof(T));
         if (n > 0) {
             const Operand xo{static_cast<const T*>(x.p) + r0 * x.ld, x.ld, n, 0};
-            const int here = side_of(V, n, W.dt);
-            const int64_t tm = ceil_div(V, here), tn = ceil_div(n, here);
-            by_tile<T>(here, [&](auto fm, auto fn, auto wm, auto wn) {
-                constexpr int FM = decltype(fm)::value, FN = decltype(fn)::value, WM = decltype(wm)::value,
-                              WN = decltype(wn)::value;
-                logits_kernel<T, FM, FN, WM, WN, true><<<unsigned(tm * tn), WM * WN * kWave, 0, s>>>(
-                    w, xo, ceil_div(D, STEP), scale, tr, tm, tn, pieces, hit, E, Vp);
-            });
+            const Tile here = tile_of(V, n, W.dt);
+            const int64_t tm = ceil_div(V, here.m);
+            launch_logits<T, true>(w, xo, ceil_div(D, STEP), scale, tr, here, pieces, hit, E, Vp, s);
             join_pieces<<<grid_of(n * kWave), kBlock, 0, s>>>(pieces, tm, n, hit, tr, V, loss + r0, lse);
             const int64_t span = kBlock * kFoldPacks * 16 / int64_t(sizeof(T));
-            fold<T><<<unsigned(n * ceil_div(Vp, span)), kBlock, 0, s>>>(E, Vp, n, V, pieces, tm, here, lse, loss + r0,
+            fold<T><<<unsigned(n * ceil_div(Vp, span)), kBlock, 0, s>>>(E, Vp, n, V, pieces, tm, here.m, lse, loss + r0,
                                                                        tr, wr, out.unit);
             // dx = G W
             Product dx = out;
@@ -715,15 +726,15 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
             dx.V = V;
             const Operand g{E, Vp, n, 0}, wt = turned(w, D);
             const int64_t p = dx_parts(n);
-            const int side = side_of(D, n, W.dt, steps_v);
+            const Tile tile = tile_of(D, n, W.dt, steps_v);
             if (p > 1) {
                 dx.sums = dxparts;
                 dx.lds = sumld;
                 dx.plane = n * sumld;
-                launch_product<T, false, kPart>(wt, g, steps_v, p, side, dx, s);
+                launch_product<T, false, kPart>(wt, g, steps_v, p, tile, dx, s);
                 join_parts<T><<<grid_of(n * sumld / 4), kBlock, 0, s>>>(dx, p, n, D);
             } else {
-                launch_product<T, false, kStore>(wt, g, steps_v, 1, side, dx, s);
+                launch_product<T, false, kStore>(wt, g, steps_v, 1, tile, dx, s);
             }
         }
         // dW = G^T x
@@ -735,11 +746,11 @@ size_t cross_entropy_grad(const DenseRows& X, const DenseRows& W, const Targets&
         dw.first = r0 == 0;
         dw.last = r0 + chunk >= X.m;
         const Operand xt = turned(packed<T, true>(xr, XM, xld, tr, wr, V, s), D), gt{E, Vp, V, n};
-        const int side = side_of(D, V, W.dt);
+        const Tile tile = tile_of(D, V, W.dt);
         if (sums)
-            launch_product<T, true, kAdd>(xt, gt, ceil_div(n, STEP), 1, side, dw, s);
+            launch_product<T, true, kAdd>(xt, gt, ceil_div(n, STEP), 1, tile, dw, s);
         else
-            launch_product<T, true, kStore>(xt, gt, ceil_div(n, STEP), 1, side, dw, s);
+            launch_product<T, true, kStore>(xt, gt, ceil_div(n, STEP), 1, tile, dw, s);
     }
     return 0;
 }

@@ -128,6 +128,19 @@ def test_gradient_against_differences():
     assert abs(got - slope) <= 1e-5 * (dx.abs().cpu().double() * ux.abs()).sum() + 1e-5 * (dw.abs().cpu().double() * uw.abs()).sum()
 
 
+# (tiles of 128 x 128, others than the ones above: of the logits, of both products of
+# which dX's is split, and of dX's whole; rows that are whole steps, and odd ones)
+@pytest.mark.parametrize("N,V,D", [(128, 32700, 33), (130, 32760, 64), (300, 9000, 128), (300, 9000, 129),
+                                   (4090, 40, 2045), (4096, 50, 2048)])
+def test_larger_tiles_of_32_bits(N, V, D):
+    x, w, t, wt = problem(N, V, D, torch.float32)
+    want = ref.cross_entropy(x.double(), w.double(), t, 1.0, wt.double())
+    loss, dx, dw = sp.linear_cross_entropy_grad(x.to(DEV), w.to(DEV), t.to(DEV), 1.0, wt.to(DEV))
+    check_loss((loss,), want, V, D)
+    check_grad(dx, dw, want, wt, N, V, D, torch.float32)
+    assert torch.equal(sp.linear_cross_entropy(x.to(DEV), w.to(DEV), t.to(DEV))[0], loss)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_strides_and_leading_dimensions(dtype):
     N, V, D = 36, 77, 64
