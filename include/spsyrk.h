@@ -460,7 +460,10 @@ spsyrk_status spsyrk_distill_grad(const spsyrk_dense* S, const spsyrk_entries* t
  * rows of one entry and no values; a row whose target lies outside [0, v) is
  * padding and has loss 0.  The logits are formed in 32 bits, piece by piece,
  * and not kept.  Logits that are NaN or infinite make their row's loss NaN or
- * infinite.  loss: m floats; lse: m floats, or NULL.
+ * infinite.  loss: m floats; lse: m floats, or NULL.  d of 2^22 or more,
+ * v of 2^28 or more: SPSYRK_ERR_SHAPE.  Workspace: 8 bytes for every 64 columns of
+ * each of up to 64 rows; of more rows about 256 MB at most, and copies of X and W if their
+ * rows are not on 16-byte boundaries or not a multiple of 128 bytes long.
  */
 spsyrk_status spsyrk_linear_cross_entropy(const spsyrk_dense* X, const spsyrk_dense* W, const spsyrk_entries* targets,
                                           float scale, const spsyrk_allocator* al, void* hip_stream, float* loss,
@@ -473,9 +476,11 @@ spsyrk_status spsyrk_linear_cross_entropy(const spsyrk_dense* X, const spsyrk_de
  * weight: m floats, NULL for ones.  Rows of weight 0 and padding take no part:
  * their dX is zero and dW has nothing of them, whatever X holds there.  For
  * 16-bit types G is rounded to X's type before the products (exponentials as
- * well), the target's entry from its 32-bit logit.  Workspace: up to about
- * 4 GB for the exponentials of some rows at a time and their transpose, a
- * transposed copy of W, and 4 v d bytes where the rows take several turns.
+ * well), the target's entry from its 32-bit logit.  v of 2^22 or more:
+ * SPSYRK_ERR_SHAPE.  Workspace besides the loss's: the exponentials of as many
+ * rows as go into 2 GB (256 at least, 2^17 at most) and those rows of X; 4 v d
+ * bytes where the rows take several turns; for few rows or columns up to 64
+ * parts of dX in 32 bits.
  */
 spsyrk_status spsyrk_linear_cross_entropy_grad(const spsyrk_dense* X, const spsyrk_dense* W,
                                                const spsyrk_entries* targets, float scale, const float* weight,
@@ -525,13 +530,13 @@ spsyrk_status spsyrk_block_norm_grad(const spsyrk_dense* dY, const spsyrk_dense*
  * unsigned for v, and a float for every SPSYRK_ADAM_BLOCK elements of the tensor
  * (and for what is left) in m_scale and v_scale, S below:
  *     m = sign(c) (c / 127)^2 S,  v = (c / 255)^4 S,
- * S the largest magnitude among them after the step, rounded to a float, and c
- * the nearest code (by 127 sqrt(|m| / S), 255 (v / S)^(1/4)), at least 1 for v > 0.
+ * S the largest magnitude among them after the step (formed in 64 bits, each
+ * product rounded), rounded to a float, and c the nearest code (by 127 sqrt(|m| / S), 255 (v / S)^(1/4)), at least 1 for v > 0.
  * The update is that of the values before they are coded.  All zeros is a state
  * to begin with.  A value that is not a finite float makes S NaN for its block.
- * Tensors must not overlap each other; their arrays are as large as n says, and
- * the call needs no workspace.  The rates are the host's: a captured call repeats
- * them.  grad_scale is read on the device.
+ * Tensors must not overlap each other; their arrays are as large as n says (2^33 or
+ * more: SPSYRK_ERR_SHAPE), and the call needs no workspace.  The rates are the
+ * host's: a captured call repeats them.  grad_scale is read on the device.
  */
 #define SPSYRK_ADAM_BLOCK 256
 typedef struct spsyrk_adam_tensor {

@@ -494,7 +494,8 @@ __global__ __launch_bounds__(WM* WN* kWave) void product_kernel(Operand A, Opera
     }
 }
 
-// the parts of k added in their order
+// the parts of k added in their order (64 parts of 25 x 257: 18 us with one load under
+// way at a time, 7 with eight)
 template <typename T>
 __global__ __launch_bounds__(kBlock) void join_parts(Product o, int64_t parts, int64_t N, int64_t M) {
     const float alpha = o.unit ? o.alpha * o.unit[0] : o.alpha;
@@ -504,6 +505,7 @@ __global__ __launch_bounds__(kBlock) void join_parts(Product o, int64_t parts, i
         if (m >= M) continue;
         const float* p = o.sums + n * o.lds + m;
         F4 v = *reinterpret_cast<const F4*>(p);
+#pragma unroll 8
         for (int64_t i = 1; i < parts; ++i) v += *reinterpret_cast<const F4*>(p + i * o.plane);
         const bool keep = !o.t.p || row_weight(o.t, o.weight, o.V, n) != 0.f;
         store_four<T>(o, n, m, M, alpha, keep, v);

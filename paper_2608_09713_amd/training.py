@@ -210,9 +210,11 @@ _ptr = torch.Tensor.data_ptr
 
 
 class AdamWPlan:
-    """AdamW steps over the same tensors: their sizes and types are checked once.
-    The plan keeps the tensors; their addresses are read again at every step, so
-    it follows tensors whose storage was exchanged (``.data = ...``)."""
+    """AdamW steps over the same tensors.  The plan keeps the tensors; their
+    addresses are read again at every step, so it follows tensors whose storage was
+    exchanged (``.data = ...``) for one of the same type and size.  Parameters that
+    require gradients count a step as a change in place, so that autograd refuses a
+    backward pass that saved them before."""
 
     def __init__(self, params, grads, states, masters=None):
         params, grads = list(params), list(grads)
@@ -224,9 +226,29 @@ class AdamWPlan:
         self._device = params[0].get_device() if params else -1
         if params and not params[0].is_cuda:
             raise TypeError("params must be device tensors")
+        self._recorded = [p for p in params if p.requires_grad]
+        self._kinds = self._checked()
         groups = {}
-        for k, (p, g, s) in enumerate(zip(params, grads, states)):
-            w = None if masters is None else masters[k]
+        for k, (_, *kind) in enumerate(self._kinds):
+            groups.setdefault(tuple(kind), []).append(k)
+        # (one call for each kind of tensor)
+        self._calls = []
+        for (pt, gt, bits, wide), index in groups.items():
+            how = _sp._AdamStep(_DTYPE[pt], _DTYPE[gt], bits)
+            columns = [[params[k] for k in index], [grads[k] for k in index], [masters[k] for k in index] if wide else None]
+            columns += [[states[k][c] for k in index] for c in range(4 if bits == 8 else 2)]
+            table = (_sp._AdamTensor * len(index))()
+            for row, k in zip(table, index):
+                row.n = params[k].numel()
+            self._calls.append((how, table, columns))
+        self._at = None
+        self._follow()
+
+    def _checked(self):
+        """(size, parameter's type, gradient's type, state's bits, with a master copy) of every tensor."""
+        kinds = []
+        for k, (p, g, s) in enumerate(zip(self.params, self.grads, self.states)):
+            w = None if self.masters is None else self.masters[k]
             if p.dtype not in _DTYPE:
                 raise TypeError(f"params must be float32, float16 or bfloat16, not {p.dtype}")
             if g.dtype not in (torch.float32, p.dtype):
@@ -246,36 +268,25 @@ class AdamWPlan:
                         raise ValueError("all tensors must be on one device")
                     if not t.is_contiguous():
                         raise ValueError("all tensors must be contiguous")
-            groups.setdefault((p.dtype, g.dtype, bits, w is not None), []).append(k)
-        # (one call for each kind of tensor)
-        self._calls = []
-        for (pt, gt, bits, wide), index in groups.items():
-            how = _sp._AdamStep(_DTYPE[pt], _DTYPE[gt], bits)
-            columns = [[params[k] for k in index], [grads[k] for k in index], [masters[k] for k in index] if wide else None]
-            columns += [[states[k][c] for k in index] for c in range(4 if bits == 8 else 2)]
-            table = (_sp._AdamTensor * len(index))()
-            for row, k in zip(table, index):
-                row.n = params[k].numel()
-            self._calls.append((how, table, columns, []))
-        self._follow()
+                    if n and not t.data_ptr():
+                        raise ValueError("a tensor of the plan has no storage")
+            kinds.append((n, p.dtype, g.dtype, bits, w is not None))
+        return kinds
 
     def _follow(self):
         """The tensors' present addresses into the tables."""
-        moved = False
-        for _, table, columns, last in self._calls:
-            now = [None if c is None else list(map(_ptr, c)) for c in columns]
-            if now == last:
-                continue
-            for name, column in zip(("param", "grad", "master", "m", "v", "m_scale", "v_scale"), now):
+        at = [[None if c is None else list(map(_ptr, c)) for c in columns] for _, _, columns in self._calls]
+        if at == self._at:
+            return
+        if self._at is not None and self._checked() != self._kinds:
+            raise ValueError("a tensor of the plan has changed its type or size")
+        self._distinct()
+        for (_, table, _), columns in zip(self._calls, at):
+            for name, column in zip(("param", "grad", "master", "m", "v", "m_scale", "v_scale"), columns):
                 if column is not None:
                     for row, p in zip(table, column):
-                        if row.n and not p:
-                            raise ValueError("a tensor of the plan has lost its storage")
                         setattr(row, name, p)
-            last[:] = now
-            moved = True
-        if moved:
-            self._distinct()
+        self._at = at
 
     def _distinct(self):
         """Refuses tensors that are written twice in a step."""
@@ -298,10 +309,12 @@ class AdamWPlan:
         lib = _sp._lib or _sp.library()
         self._follow()
         with torch.cuda.device(self._device):
-            for how, table, _, _ in self._calls:
+            for how, table, _ in self._calls:
                 how.step, how.lr, how.eps, how.weight_decay, how.grad_scale = step, lr, eps, weight_decay, scale
                 how.beta1, how.beta2 = betas
                 _check(lib.spsyrk_adamw(table, len(table), _byref(how), _raw_stream(self._device)))
+        if self._recorded:
+            torch.autograd.graph.increment_version(self._recorded)
 
 
 def adamw_plan(params, grads, states, masters=None):

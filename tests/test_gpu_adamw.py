@@ -202,3 +202,27 @@ def test_overlapping_tensors_are_refused():
         sp.adamw([w], [g], [sp.AdamState(s.m, s.m)], LR, 1)
     with pytest.raises(ValueError, match="overlap"):
         sp.adamw([w[:60], w[50:]], [g[:60], g[50:]], [sp.adam_state(w[:60]), sp.adam_state(w[50:])], LR, 1)
+
+
+def test_exchanged_storage_of_another_size_or_type_is_refused():
+    w, g = torch.zeros(100, device=DEV), torch.ones(100, device=DEV)
+    plan = sp.adamw_plan([w], [g], [sp.adam_state(w)])
+    before = g.data
+    for other in (torch.ones(60, device=DEV), torch.ones(100, device=DEV, dtype=torch.bfloat16),
+                  torch.ones(200, device=DEV)[::2]):
+        g.data = other
+        for _ in range(2):
+            with pytest.raises((ValueError, TypeError)):
+                plan.step(LR, 1)
+    g.data = before
+    plan.step(LR, 1, eps=0.0, weight_decay=0.0)
+    assert (w + LR).abs().max() <= 2 ** -20 * LR  # (one step from zero: -lr)
+
+
+def test_autograd_sees_the_change():
+    w = torch.ones(8, device=DEV, requires_grad=True)
+    loss = (w * w).sum()
+    plan = sp.adamw_plan([w], [torch.ones(8, device=DEV)], [sp.adam_state(w)])
+    plan.step(LR, 1)
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()

@@ -151,3 +151,19 @@ def test_binding_of_the_others():
     assert sp.adam_state(torch.zeros(257), 8).m_scale.numel() == 2
     with pytest.raises(TypeError):
         sp.adam_values([sp.AdamState(s.m, s.v.double())])
+
+
+def test_sizes_past_the_limits(lib):  # noqa: F811
+    # (columns of X, rows of W; fewer of those for the gradient, whose exponentials are rows of them)
+    def calls(v, d):
+        x, w, t = dense(4, d), dense(v, d), tokens(n=v)
+        return (lib.spsyrk_linear_cross_entropy(ref(x), ref(w), ref(t), 1.0, None, None, P, P),
+                lib.spsyrk_linear_cross_entropy_grad(ref(x), ref(w), ref(t), 1.0, None, None, None, P, ref(x), ref(w)))
+
+    assert calls(16, 1 << 22) == (SHAPE, SHAPE)
+    assert calls(1 << 28, 1) == (SHAPE, SHAPE)
+    assert calls(1 << 22, 1)[1] == SHAPE
+    big = (sp._AdamTensor * 1)()
+    big[0].n, big[0].param, big[0].grad, big[0].m, big[0].v = 1 << 33, P, P, P, P
+    how = sp._AdamStep(0, 0, 32, 1, 1e-3, 0.9, 0.999, 1e-8, 0.0)
+    assert lib.spsyrk_adamw(big, 1, ref(how), None) == SHAPE
