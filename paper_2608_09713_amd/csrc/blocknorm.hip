@@ -293,18 +293,23 @@ struct Spread {
     int64_t slots = 1, parts = 1;
     bool whole = false;
     __host__ __device__ int64_t grid() const { return slots * parts; }
+    // whether the workgroups finish the gate's gradient
+    __host__ __device__ bool direct() const { return groups > 1 && parts == 1; }
 };
 
-// How the gate's rows go with the rows: split over workgroups, whole groups a
-// row's threads, or a row each.
-enum { kSplit, kWhole, kOwn };
+// How the gate's rows go with the rows: one group, split over workgroups; several
+// groups, each split; whole groups a row's threads; or a row each.
+enum { kOne, kSplit, kWhole, kOwn };
 
-// workspace: the workgroups' sums of dh n2, then of S (split groups: one of each
-// part of a group; whole groups: a workgroup's sums of gate S)
+// workspace: the workgroups' sums of dh n2, of several groups those of gate S, and
+// S of the groups' parts that are still to be added up
 struct Sums {
     float* pre = nullptr;
+    float* post = nullptr;
     float* s = nullptr;
 };
+inline int64_t post_rows(const Spread& go) { return go.groups > 1 ? go.grid() : 0; }
+inline int64_t s_rows(const Spread& go) { return go.direct() ? 0 : go.groups * go.parts; }
 
 template <typename T>
 struct GradArgs {
@@ -385,9 +390,14 @@ __device__ inline void add_rows(float (&v)[NP][N], float* lds, int threads, int 
     }
 }
 
+// Four wavefronts a SIMD, two workgroups of 512 threads on a compute unit, even
+// where sums are spilled for it (16384 x 4096, 64 groups: 160 us, 209 without the
+// limit; 262144 x 128, 4096 groups: 75 and 87), but for rows of a wavefront's lanes
+// whose groups are not split (262144 x 128, a gate for each: 86, with it 92).
 template <typename T, int N, int L, int MOST, int NP, bool ANY, int GATE>
-__global__ __launch_bounds__(MOST) void after_block_grad(GradArgs<T> a) {
-    constexpr bool WHOLE = GATE == kWhole, OWN = GATE == kOwn;
+__global__ __launch_bounds__(MOST) __attribute__((amdgpu_waves_per_eu(L && GATE != kSplit ? 2 : 4))) void
+after_block_grad(GradArgs<T> a) {
+    constexpr bool WHOLE = GATE == kWhole, OWN = GATE == kOwn, POST = GATE == kWhole || GATE == kSplit;
     __shared__ float buf[2][2][kMostWaves];
     __shared__ float lds[L ? MOST / 2 * NP * N : MOST < kRowBlock ? MOST * NP * N : 1];
     // rows under way in the workgroup (all of them take every step of the loops
@@ -435,7 +445,7 @@ __global__ __launch_bounds__(MOST) void after_block_grad(GradArgs<T> a) {
     // mul = scale post gate: of the group, or with a row's own gate of the row
     P post[NP], pre[NP];
     float mul[NP][N], sum_pre[NP][N] = {}, sum_s[NP][N] = {};
-    float sum_post[WHOLE ? NP : 1][N] = {};
+    float sum_post[POST ? NP : 1][N] = {};
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
         post[k].load(a.par.post, a.par.wide, at[k].c, 1.f);
@@ -520,32 +530,29 @@ __global__ __launch_bounds__(MOST) void after_block_grad(GradArgs<T> a) {
                 }
             }
         }
-        if constexpr (WHOLE) {
+        if constexpr (!WHOLE) add_rows<L, MOST>(sum_s, lds, threads, subs);
+        const bool write = WHOLE ? mine_too : sub == 0;
 #pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                float dg[N], g[N];
+        for (int k = 0; k < NP; ++k) {
+            if (POST && write) {
+                float g[N];
                 load_any<T, N>(a.gate.p, a.gate.wide, gi * a.gate.ld + at[k].c, 1.f, g);
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    dg[i] = a.scale * sum_s[k][i] * post[k].get(i);
-                    sum_post[k][i] = fmaf(sum_s[k][i], g[i], sum_post[k][i]);
-                    sum_s[k][i] = 0.f;
-                }
-                if (mine_too && at[k].shift < N)
+                for (int i = 0; i < N; ++i) sum_post[POST ? k : 0][i] = fmaf(sum_s[k][i], g[i], sum_post[POST ? k : 0][i]);
+            }
+            if (write && at[k].shift < N) {
+                if (WHOLE || (POST && a.go.direct())) {
+                    float dg[N];
+#pragma unroll
+                    for (int i = 0; i < N; ++i) dg[i] = a.scale * sum_s[k][i] * post[k].get(i);
                     store_any<T, N>(a.dgate, a.gate.wide, gi * a.lddg + at[k].c, dg);
-            }
-        } else {
-            add_rows<L, MOST>(sum_s, lds, threads, subs);
-            if (sub == 0) {
-                float* p = a.sums.s + (gi * a.go.parts + blockIdx.x % a.go.parts) * d;
-#pragma unroll
-                for (int k = 0; k < NP; ++k)
-                    if (at[k].shift < N) store_any<float, N>(p, true, at[k].c, sum_s[k]);
+                } else {
+                    store_any<float, N>(a.sums.s + (gi * a.go.parts + blockIdx.x % a.go.parts) * d, true, at[k].c,
+                                        sum_s[k]);
+                }
             }
 #pragma unroll
-            for (int k = 0; k < NP; ++k)
-#pragma unroll
-                for (int i = 0; i < N; ++i) sum_s[k][i] = 0.f;
+            for (int i = 0; i < N; ++i) sum_s[k][i] = 0.f;
         }
     }
     add_rows<L, MOST>(sum_pre, lds, threads, subs);
@@ -555,7 +562,7 @@ __global__ __launch_bounds__(MOST) void after_block_grad(GradArgs<T> a) {
     for (int k = 0; k < NP; ++k) {
         if (at[k].shift >= N) break;
         store_any<float, N>(a.sums.pre + int64_t(blockIdx.x) * d, true, at[k].c, sum_pre[k]);
-        if constexpr (WHOLE) store_any<float, N>(a.sums.s + int64_t(blockIdx.x) * d, true, at[k].c, sum_post[k]);
+        if constexpr (POST) store_any<float, N>(a.sums.post + int64_t(blockIdx.x) * d, true, at[k].c, sum_post[k]);
     }
 }
 
@@ -626,7 +633,7 @@ __global__ __launch_bounds__(kRowBlock) void after_block_grad_long(GradArgs<T> a
 
 // The sums of long rows: workgroup (x, y) takes a pack of columns per lane of
 // the groups and parts that y stands for, its wavefronts in turn.
-template <typename T, bool WHOLE>
+template <typename T, bool SEVERAL>
 __global__ __launch_bounds__(kBlock) void after_block_sums_long(GradArgs<T> a, const float* __restrict__ means) {
     constexpr int N = 16 / int(sizeof(T));
     __shared__ float lds[kWavesPerBlock][kWave][N];
@@ -669,13 +676,13 @@ __global__ __launch_bounds__(kBlock) void after_block_sums_long(GradArgs<T> a, c
         }
         add(sum_s);
         if (w == 0 && at.shift < N) {
-            if constexpr (WHOLE) {
+            if constexpr (SEVERAL)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum_post[i] = fmaf(sum_s[i], g[i], sum_post[i]);
+            if (SEVERAL && a.go.direct()) {
                 float dg[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    dg[i] = a.scale * sum_s[i] * post[i];
-                    sum_post[i] = fmaf(sum_s[i], g[i], sum_post[i]);
-                }
+                for (int i = 0; i < N; ++i) dg[i] = a.scale * sum_s[i] * post[i];
                 store_any<T, N>(a.dgate, a.gate.wide, gi * a.lddg + at.c, dg);
             } else {
                 store_any<float, N>(a.sums.s + (gi * a.go.parts + part) * a.d, true, at.c, sum_s);
@@ -685,63 +692,79 @@ __global__ __launch_bounds__(kBlock) void after_block_sums_long(GradArgs<T> a, c
     add(sum_pre);
     if (w > 0 || at.shift >= N) return;
     store_any<float, N>(a.sums.pre + int64_t(blockIdx.y) * a.d, true, at.c, sum_pre);
-    if constexpr (WHOLE) store_any<float, N>(a.sums.s + int64_t(blockIdx.y) * a.d, true, at.c, sum_post);
+    if constexpr (SEVERAL) store_any<float, N>(a.sums.post + int64_t(blockIdx.y) * a.d, true, at.c, sum_post);
 }
 
-// The parts added up: dpre (item 0), dpost (1) and the gate's rows (2 and on):
-// every kJoinBlock / COLUMNS-th part in its order, those sums pairwise.  Narrow
-// workgroups where few columns would leave most of the chip idle.
-constexpr int kJoinBlock = 1024;
-template <typename T, int COLUMNS>
-__global__ __launch_bounds__(kJoinBlock) void join_sums(Sums sums, Spread go, int64_t items, int64_t d, BlockGate gate,
-                                                        BlockParams par, float scale, void* dpre, void* dpost, void* dgate,
-                                                        int64_t lddg) {
+// The parts added up.  A workgroup takes some columns of dpre, of dpost (and of the
+// gate, if that is one row) or of a row of the gate, many parts of them side by
+// side: each in its order, then those sums pairwise.  16 columns instead of 64 where
+// few would leave most of the chip idle (512 parts of 1001 columns: 4 us and 6, of
+// 8192: 15 and 5); kGateColumns of a gate's row that has few parts (64 rows of 4096
+// columns, 8 parts each: 13 us less than by 64 columns).
+constexpr int kJoinBlock = 1024, kGateColumns = 256;
+inline __host__ __device__ int gate_columns(int64_t parts, int columns) { return parts < 16 ? kGateColumns : columns; }
+
+// the sum of `count` rows of d at column c0 + threadIdx.x % COLUMNS, for the first COLUMNS threads
+template <int COLUMNS>
+__device__ inline float join_columns(const float* from, int64_t count, int64_t d, int64_t c0, float* lds) {
     constexpr int W = kJoinBlock / COLUMNS;  // parts under way
-    __shared__ float lds[W][COLUMNS];
-    const int w = threadIdx.x / COLUMNS, l = threadIdx.x % COLUMNS;
-    for (int64_t item = blockIdx.y; item < items; item += gridDim.y) {
-        if (item == 0 ? !dpre : item == 1 && !dpost) continue;
-        const int64_t gi = item - 2;
-        const float* from = item == 0 ? sums.pre : item == 1 ? sums.s : sums.s + gi * go.parts * d;
-        const int64_t count = item == 0 || (item == 1 && go.whole) ? go.grid()
-                              : item == 1                          ? go.groups * go.parts
-                                                                   : go.parts;
-        // (S of a part of a group, times that group's gate, is its share of dpost)
-        const bool weighted = item == 1 && !go.whole && gate.p && !gate.own;
-        for (int64_t c0 = int64_t(blockIdx.x) * COLUMNS; c0 < d; c0 += int64_t(gridDim.x) * COLUMNS) {
-            const int64_t c = c0 + l;
-            float s = 0.f;
-            if (c < d && weighted) {
-#pragma unroll 4
-                for (int64_t q = w; q < count; q += W) {
-                    float k[1];
-                    load_any<T, 1>(gate.p, gate.wide, q / go.parts * gate.ld + c, 1.f, k);
-                    s = fmaf(from[q * d + c], k[0], s);
-                }
-            } else if (c < d) {
+    const int w = threadIdx.x / COLUMNS;
+    const int64_t c = c0 + threadIdx.x % COLUMNS;
+    float s = 0.f;
+    if (c < d)
 #pragma unroll 8
-                for (int64_t q = w; q < count; q += W) s += from[q * d + c];
-            }
-            lds[w][l] = s;
-            __syncthreads();
+        for (int64_t q = w; q < count; q += W) s += from[q * d + c];
+    lds[threadIdx.x] = s;
+    __syncthreads();
 #pragma unroll
-            for (int half = W / 2; half > 0; half /= 2) {
-                if (w < half) lds[w][l] += lds[w + half][l];
-                __syncthreads();
+    for (int half = W / 2; half > 0; half /= 2) {
+        if (w < half) lds[threadIdx.x] += lds[threadIdx.x + half * COLUMNS];
+        __syncthreads();
+    }
+    s = lds[threadIdx.x % COLUMNS];
+    __syncthreads();
+    return s;
+}
+
+template <typename T, int COLUMNS>
+__global__ __launch_bounds__(kJoinBlock) void join_sums(Sums sums, Spread go, int64_t gate_rows, int64_t d,
+                                                        BlockGate gate, BlockParams par, float scale, void* dpre,
+                                                        void* dpost, void* dgate, int64_t lddg) {
+    __shared__ float lds[kJoinBlock];
+    const bool one = go.groups == 1;
+    const int64_t across = (d + COLUMNS - 1) / COLUMNS, wide = gate_columns(go.parts, COLUMNS),
+                  gate_across = (d + wide - 1) / wide;
+    for (int64_t b = blockIdx.x; b < 2 * across + gate_rows * gate_across; b += gridDim.x) {
+        float v[1], k[1];
+        if (b < across) {
+            if (!dpre) continue;
+            const int64_t c0 = b * COLUMNS, c = c0 + threadIdx.x;
+            v[0] = join_columns<COLUMNS>(sums.pre, go.grid(), d, c0, lds);
+            if (threadIdx.x < COLUMNS && c < d) store_any<T, 1>(dpre, par.wide, c, v);
+        } else if (b < 2 * across) {
+            const bool gated = one && gate.p && !gate.own;
+            if (!dpost && !gated) continue;
+            const int64_t c0 = (b - across) * COLUMNS, c = c0 + threadIdx.x;
+            const float S = scale * join_columns<COLUMNS>(one ? sums.s : sums.post, one ? go.parts : go.grid(), d, c0, lds);
+            if (threadIdx.x < COLUMNS && c < d) {
+                load_any<T, 1>(gated ? gate.p : nullptr, gate.wide, c, 1.f, k);
+                v[0] = S * k[0];
+                if (dpost) store_any<T, 1>(dpost, par.wide, c, v);
+                load_any<T, 1>(par.post, par.wide, c, 1.f, k);
+                v[0] = S * k[0];
+                if (gated) store_any<T, 1>(dgate, gate.wide, c, v);
             }
-            if (w == 0 && c < d) {
-                float v[1] = {lds[0][l]};
-                if (item > 1) {
-                    float k[1];
-                    load_any<T, 1>(par.post, par.wide, c, 1.f, k);
-                    v[0] *= scale * k[0];
-                    store_any<T, 1>(dgate, gate.wide, gi * lddg + c, v);
-                } else {
-                    if (item) v[0] *= scale;
-                    store_any<T, 1>(item ? dpost : dpre, par.wide, c, v);
-                }
+        } else {
+            const int64_t gi = (b - 2 * across) / gate_across;
+            const int64_t c0 = (b - 2 * across) % gate_across * wide, c = c0 + threadIdx.x;
+            const float* from = sums.s + gi * go.parts * d;
+            v[0] = wide == COLUMNS ? join_columns<COLUMNS>(from, go.parts, d, c0, lds)
+                                   : join_columns<kGateColumns>(from, go.parts, d, c0, lds);
+            if (threadIdx.x < wide && c < d) {
+                load_any<T, 1>(par.post, par.wide, c, 1.f, k);
+                v[0] *= scale * k[0];
+                store_any<T, 1>(dgate, gate.wide, gi * lddg + c, v);
             }
-            __syncthreads();
         }
     }
 }
@@ -785,8 +808,9 @@ inline void by_block_shape(const RowShape& s, F f) {
 }
 
 // Rows that a workgroup of the gradient has under way, and workgroups: 16
-// wavefronts on a compute unit, as few workgroups as that takes, since each
-// leaves two sums of d floats.
+// wavefronts on a compute unit, as few workgroups as that takes, since each leaves
+// sums of d floats (8191 x 1001: 31 us, with half as many workgroups 37, with twice
+// as many 41; 8192 x 4096: 88, 107 and 100).
 inline int grad_rows(const RowShape& s) {
     return s.lanes ? kGradBlock / s.lanes : s.threads && s.threads <= kGradBlock ? kGradBlock / s.threads : 1;
 }
@@ -797,8 +821,11 @@ Spread spread_of(int64_t m, int64_t groups, const RowShape& s) {
     go.per = m / groups;
     const int rows = s.np ? grad_rows(s) : 1;
     const int64_t room = !s.np ? kLongParts : s.threads > kGradBlock ? kCus : 2 * kCus;
-    // (as many groups as rows under way: each takes whole ones)
-    if (m > 0 && groups > 1 && groups >= room * rows / 2) {
+    // Groups of fewer rows than a workgroup takes side by side go whole to a row's
+    // threads each, if they are so many that the workgroups would take longer by
+    // turns (262144 x 128: of 16 rows 86 us, split 124; of 2 rows 79 and 725; of 32
+    // rows, which fill a workgroup, 79 split and 92 whole).
+    if (rows > 1 && m > 0 && go.per < rows && go.per * room < 2 * groups) {
         go.whole = true;
         go.slots = std::min(room, ceil_div(groups, rows));
         return go;
@@ -860,8 +887,7 @@ void block_norm(const DenseRows& X, const DenseRows& B, const BlockGate& gate, f
 size_t block_norm_grad_tmp_bytes(int64_t m, int64_t d, int dt, const BlockGate& gate) {
     const RowShape shape = block_shape(d, dt);
     const Spread go = spread_of(m, groups_of(gate), shape);
-    const int64_t rows = go.grid() + (go.whole ? go.grid() : go.groups * go.parts);
-    return size_t(rows * d + (shape.np ? 0 : m)) * sizeof(float);
+    return size_t((go.grid() + post_rows(go) + s_rows(go)) * d + (shape.np ? 0 : m)) * sizeof(float);
 }
 
 void block_norm_grad(const DenseRows& DY, const DenseRows& DH, const DenseRows& Y, const DenseRows& B,
@@ -873,8 +899,9 @@ void block_norm_grad(const DenseRows& DY, const DenseRows& DH, const DenseRows& 
     const Spread go = spread_of(m, groups_of(gate), shape);
     Sums sums;
     sums.pre = static_cast<float*>(tmp);
-    sums.s = sums.pre + go.grid() * d;
-    float* means = sums.s + (go.whole ? go.grid() : go.groups * go.parts) * d;
+    sums.post = sums.pre + go.grid() * d;
+    sums.s = sums.post + post_rows(go) * d;
+    float* means = sums.s + s_rows(go) * d;
     by_width(Y.dt, d, [&](auto e, auto n) {
         using T = decltype(e);
         constexpr int N = decltype(n)::value;
@@ -905,12 +932,6 @@ void block_norm_grad(const DenseRows& DY, const DenseRows& DH, const DenseRows& 
         a.sums = sums;
         a.go = go;
         using std::integral_constant;
-        auto by_whole = [&](auto f) {
-            if (go.whole)
-                f(integral_constant<bool, true>());
-            else
-                f(integral_constant<bool, false>());
-        };
         if (m > 0 && shape.np) {
             by_block_shape<T, N, kGradBlock>(shape, [&](auto lanes, auto most, auto np) {
                 constexpr int L = decltype(lanes)::value, MOST = decltype(most)::value, NP = decltype(np)::value;
@@ -923,31 +944,36 @@ void block_norm_grad(const DenseRows& DY, const DenseRows& DH, const DenseRows& 
                         launch(integral_constant<int, kOwn>());
                     else if (go.whole)
                         launch(integral_constant<int, kWhole>());
-                    else
+                    else if (go.groups > 1)
                         launch(integral_constant<int, kSplit>());
+                    else
+                        launch(integral_constant<int, kOne>());
                 });
             });
         } else if (m > 0) {
             if constexpr (N > 1) {
                 after_block_grad_long<T><<<row_grid(m), kRowBlock, 0, s>>>(a, means);
-                by_whole([&](auto whole) {
-                    after_block_sums_long<T, decltype(whole)::value>
+                auto launch = [&](auto several) {
+                    after_block_sums_long<T, decltype(several)::value>
                         <<<dim3(unsigned(ceil_div(packs_of(d, Y.dt), kWave)), unsigned(go.grid())), kBlock, 0, s>>>(
                             a, means);
-                });
+                };
+                if (go.groups > 1)
+                    launch(integral_constant<bool, true>());
+                else
+                    launch(integral_constant<bool, false>());
             }
         }
-        const bool shared = gate.p && !gate.own && !go.whole;
-        const int64_t items = shared ? 2 + go.groups : 2;
+        const int64_t gate_rows = go.groups > 1 && !(m > 0 && go.direct()) ? go.groups : 0;
         Spread add = go;
         if (m == 0) add.parts = 0;  // (of no rows: zeros)
         auto join = [&](auto columns) {
             constexpr int COLUMNS = decltype(columns)::value;
-            join_sums<T, COLUMNS>
-                <<<dim3(row_grid(ceil_div(d, COLUMNS)), unsigned(std::min<int64_t>(items, 1 << 15))), kJoinBlock, 0,
-                   s>>>(sums, add, items, d, gate, par, scale, dpre, dpost, dgate, lddg);
+            const int64_t blocks = 2 * ceil_div(d, COLUMNS) + gate_rows * ceil_div(d, gate_columns(add.parts, COLUMNS));
+            join_sums<T, COLUMNS><<<row_grid(blocks), kJoinBlock, 0, s>>>(sums, add, gate_rows, d, gate, par, scale, dpre,
+                                                                         dpost, dgate, lddg);
         };
-        if (ceil_div(d, 64) * items >= kCus / 2)
+        if (ceil_div(d, 64) >= kCus / 4)
             join(integral_constant<int, 64>());
         else
             join(integral_constant<int, 16>());

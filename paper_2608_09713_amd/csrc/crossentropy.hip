@@ -614,12 +614,14 @@ Operand packed(const DenseRows& x, T* p, int64_t ld, const Targets& t, const flo
     return {p, ld, x.m, 0};
 }
 // rows as an operand: as they are, or packed to whole steps
+inline bool as_they_are(const DenseRows& x) {
+    return on_boundaries(x.p, x.ld, x.dt) && x.n % step_elements(x.dt) == 0 &&
+           x.ld * dtype_bytes(x.dt) < kMostStride;
+}
 template <typename T>
 Operand operand_rows(const DenseRows& x, Carver& c, hipStream_t s) {
-    const int64_t step = kStepBytes / int64_t(sizeof(T));
-    if (on_boundaries(x.p, x.ld, x.dt) && x.n % step == 0 && x.ld * int64_t(sizeof(T)) < kMostStride)
-        return {x.p, x.ld, x.m, 0};
-    const int64_t ld = round_up(x.n, step);
+    if (as_they_are(x)) return {x.p, x.ld, x.m, 0};
+    const int64_t ld = round_up(x.n, kStepBytes / int64_t(sizeof(T)));
     T* p = c.get<T>(x.m * ld);
     if (!c.base) return {nullptr, ld, x.m, 0};
     return packed<T, false>(x, p, ld, Targets(), nullptr, 0, s);
@@ -627,11 +629,21 @@ Operand operand_rows(const DenseRows& x, Carver& c, hipStream_t s) {
 // the same memory with its rows as the depth of a product
 inline Operand turned(const Operand& o, int64_t columns) { return {o.p, o.ld, columns, o.rows}; }
 
+// Whether the loss of some rows goes by one reading of W (kernel above): up to 16;
+// up to 64 where W would have to be packed for the tiles, or makes too few of them
+// (32 rows of 2000 x 2048 bf16: 16 us, tiles 22; 24 of 50021 x 1001 f16: 53 and 67;
+// but 64 of 131072 x 4096 bf16: 303 and 222, 32 of 32000 x 2048: 32.4 and 30.6; in
+// 32 bits 24 of 50021 x 1024: 69 and 71, 64: 117 and 73).
+inline bool few_rows(const DenseRows& X, const DenseRows& W) {
+    if (X.m <= (X.dt == kDtF32 ? 32 : 16)) return true;
+    return X.m <= kFewRows && (!as_they_are(W) || 4 * ceil_div(W.m, kSmall.m) < 3 * kCus);
+}
+
 template <typename T>
 size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, float scale, float* loss, float* lse,
                      char* tmp, hipStream_t s) {
     Carver c{tmp};
-    if (X.m <= kFewRows) {
+    if (few_rows(X, W)) {
         const int64_t tm = ceil_div(W.m, kFewColumns);
         Piece* pieces = c.get<Piece>(X.m * tm);
         float* hit = c.get<float>(X.m);

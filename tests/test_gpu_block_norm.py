@@ -115,6 +115,17 @@ def test_gates(dtype, m, d, g_rows):
     run(m, d, dtype, torch.float32, g_rows, torch.float32, False, no_dy=True)
 
 
+# (more groups than workgroups, of fewer and of more rows than a workgroup takes side
+# by side; groups that several workgroups take, and rows of several kinds of threads)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,d,g_rows", [(8192, 64, 4096), (1800, 128, 600), (1200, 1001, 600), (3000, 1001, 600),
+                                        (64, 4096, 16), (1100, 4096, 550), (300, 8192, 150), (140, 9000, 70),
+                                        (24, 9000, 3), (520, 8200, 260)])
+def test_many_groups(dtype, m, d, g_rows):
+    run(m, d, dtype, dtype, g_rows, dtype, True)
+    run(m, d, dtype, torch.float32, g_rows, torch.float32, False, no_dy=True)
+
+
 @pytest.mark.parametrize("dtype", DTYPES[1:])
 @pytest.mark.parametrize("pdtype", [0, 1])
 @pytest.mark.parametrize("gdtype", [0, 1])

@@ -128,6 +128,15 @@ def test_gradient_against_differences():
     assert abs(got - slope) <= 1e-5 * (dx.abs().cpu().double() * ux.abs()).sum() + 1e-5 * (dw.abs().cpu().double() * uw.abs()).sum()
 
 
+# (few rows by tiles: many columns in whole steps; beside them, by one reading of W)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,V,D", [(17, 25000, 64), (33, 25000, 64), (64, 24577, 128), (64, 24577, 130), (64, 20000, 64)])
+def test_few_rows_of_many_columns(dtype, N, V, D):
+    x, w, t, _ = problem(N, V, D, dtype)
+    want = ref.cross_entropy(x.double(), w.double(), t, 1.0)
+    check_loss(sp.linear_cross_entropy(x.to(DEV), w.to(DEV), t.to(DEV)), want, V, D)
+
+
 # (tiles of 128 x 128, others than the ones above: of the logits, of both products of
 # which dX's is split, and of dX's whole; rows that are whole steps, and odd ones)
 @pytest.mark.parametrize("N,V,D", [(128, 32700, 33), (130, 32760, 64), (300, 9000, 128), (300, 9000, 129),

@@ -4,10 +4,10 @@ report for gfx950 (no GPU needed).
 The products of 256 x 256 tiles hold 128 sums and two half steps' fragments a lane
 and have 256 registers (two wavefronts per SIMD): spills there would wait for the
 loads that are under way.  Their two buffers leave room on a compute unit for one
-workgroup.  Of the gradient of the norms
-around a block, whose rows of more than 512 threads leave 128 registers, at most
-32 bytes a lane spill.  AdamW's kernels do not spill, and keep eight wavefronts a
-SIMD with states of 32 bits.
+workgroup.  Of the gradient of the norms around a block, which has 128 registers
+where two workgroups of 512 threads are to share a compute unit, at most 48 bytes a
+lane spill.  AdamW's kernels do not spill, and keep eight wavefronts a SIMD with
+states of 32 bits.
 """
 from tests.test_kernel_resources import _report, pytestmark  # noqa: F401
 
@@ -27,7 +27,9 @@ def test_block_norm_budgets():
     grads = {k: v for k, v in ks.items() if "after_block_grad" in k and "long" not in k}
     assert len(grads) > 50
     for name, r in ks.items():
-        assert r["ScratchSize"] <= (32 if name in grads and "Li1024E" in name else 0), (name, r)
+        assert r["ScratchSize"] <= (48 if name in grads and "Li512E" in name else 0), (name, r)
+        if name in grads and "Li0ELi512E" in name:
+            assert r["Occupancy"] >= 4, (name, r)
 
 
 def test_adamw_budgets():
