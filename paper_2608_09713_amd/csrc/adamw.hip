@@ -6,7 +6,10 @@
 // Bound by bytes: parameter, gradient and states are read once, parameter and
 // states written once.  The tensors' addresses travel in the launch's arguments,
 // so a call needs no memory of its own and can be captured; a workgroup finds
-// its tensor among them by its number.
+// its tensor among them by its number.  160 M elements of bf16 with copies and
+// states in 32 bits: 880 us, 5.1 TB/s; 64 M with states in 8: 172 us, 3.7 TB/s
+// (each pack's scale is known only when all of it is summed, and the codes' roots
+// and comparisons follow before its stores).
 //
 // States in 8 bits: kAdamBlock elements of a tensor share a scale S, their
 // largest magnitude after the step; m = sign (c / 127)^2 S with c from -127 to
@@ -29,7 +32,8 @@ constexpr int kAt = 4;  // elements of a pack: 16 bytes of 32-bit floats
 // of 32 bits: the widest chunks are read and written fastest (160 M elements of
 // bf16 with copies: 980 us by 128 threads, 902 by 256, 888 by 1024; two packs a
 // thread 967).  Of 8 bits, where a wavefront's arithmetic counts, two packs by
-// 256 threads (64 M: 280 us with the values, one pack 290, by 1024 threads 296).
+// 256 threads (64 M, with the values: one pack 290 us, by 1024 threads 296, these 280,
+// and 259 with one comparison for values next to a border).
 template <bool NARROW>
 constexpr int kPacks = NARROW ? 2 : 1;
 template <bool NARROW>

@@ -13,8 +13,14 @@
 // between as in the layer norm.  The rows that share a row of the gate share S,
 // so its gradient and that of post are one sum, told apart when the workgroups'
 // parts are added up, in their order, by a second launch.  A gate of a row's own
-// has its gradient written with the row.  y is rounded when it is stored; h and
-// r2 come from the sum before that.
+// has its gradient written with the row.  Several rows of the gate: a workgroup
+// keeps the sum of gate S over its groups, which is dpost's share.  y is rounded
+// when it is stored; h and r2 come from the sum before that.
+//
+// 32768 x 4096 bf16, forward: 197 us, 5.4 TB/s; 16384 x 8192 with a gate of each
+// row's own, gradient: 432 us, 5.0 TB/s; with one gate 8192 x 8192: 178 us, 4.5.  The
+// gradient's loads of a row stand before its two sums and its stores behind them;
+// loading a row ahead took the registers of other wavefronts (432 us: 564).
 #include "internal.h"
 #include "row_shape.h"
 #include "training.h"
