@@ -705,8 +705,8 @@ __global__ __launch_bounds__(kBlock) void after_block_sums_long(GradArgs<T> a, c
 // gate, if that is one row) or of a row of the gate, many parts of them side by
 // side: each in its order, then those sums pairwise.  16 columns instead of 64 where
 // few would leave most of the chip idle (512 parts of 1001 columns: 4 us and 6, of
-// 8192: 15 and 5); kGateColumns of a gate's row that has few parts (64 rows of 4096
-// columns, 8 parts each: 13 us less than by 64 columns).
+// 8192: 15 and 5); kGateColumns of a gate's row that has few parts (16384 x 4096, 64
+// rows of the gate, 8 parts each: 209 us in all, 224 by 64 columns).
 constexpr int kJoinBlock = 1024, kGateColumns = 256;
 inline __host__ __device__ int gate_columns(int64_t parts, int columns) { return parts < 16 ? kGateColumns : columns; }
 
@@ -946,10 +946,10 @@ void block_norm_grad(const DenseRows& DY, const DenseRows& DH, const DenseRows& 
                         after_block_grad<T, N, L, MOST, NP, decltype(any)::value, decltype(how)::value>
                             <<<unsigned(go.grid()), L ? MOST : shape.threads * grad_rows(shape), 0, s>>>(a);
                     };
+                    if constexpr (MOST == kGradBlock)  // (past it no rows side by side)
+                        if (go.whole) return launch(integral_constant<int, kWhole>());
                     if (gate.p && gate.own)
                         launch(integral_constant<int, kOwn>());
-                    else if (go.whole)
-                        launch(integral_constant<int, kWhole>());
                     else if (go.groups > 1)
                         launch(integral_constant<int, kSplit>());
                     else
