@@ -1,13 +1,15 @@
-"""Build libspsyrk.so (hipcc, gfx950) in-tree.
+"""Build libspsyrk.so (hipcc, gfx950) and the binding's _tensors.so (g++) in-tree.
 
 Usage: python -m paper_2608_09713_amd.build
 """
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -15,6 +17,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libspsyrk.so")
 # the same sources with the kernels' invariant checks compiled in (SPSYRK_DEBUG)
 DEBUG_LIB = os.path.join(PKG, "libspsyrk_debug.so")
+# host code of the Python binding, which reads torch's tensors (the library itself knows no torch)
+TENSORS = os.path.join(PKG, "_tensors.so")
 ARCH = os.environ.get("SPSYRK_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [
@@ -61,5 +65,19 @@ def build(verbose: bool = False, debug: bool = False) -> str:
     return target
 
 
+def build_tensors() -> str:
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    include = [sysconfig.get_paths()["include"], os.path.join(torch, "include"),
+               os.path.join(torch, "include", "torch", "csrc", "api", "include")]
+    tmp = TENSORS + f".tmp{os.getpid()}"
+    # (the directories are torch's: their warnings are not this source's)
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                           *[f for d in include for f in ("-isystem", d)], os.path.join(CSRC, "tensors.cpp"), "-o", tmp,
+                           "-L", os.path.join(torch, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"])
+    os.replace(tmp, TENSORS)
+    return TENSORS
+
+
 if __name__ == "__main__":
     print(build(verbose=True))
+    print(build_tensors())

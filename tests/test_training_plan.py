@@ -1,0 +1,85 @@
+"""What an AdamW plan sees of its tensors before a step, on the host: tensors of
+the host stand in for a device's, and no step is enqueued."""
+import os
+
+import pytest
+import torch
+
+import paper_2608_09713_amd as sp
+from paper_2608_09713_amd import build
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _tensors():
+    if not os.path.exists(build.TENSORS):
+        build.build_tensors()
+
+
+class OnDevice(torch.Tensor):
+    is_cuda = True
+
+
+def host(t):
+    return t.as_subclass(OnDevice)
+
+
+def plan_of(*shapes, bits=32, dtype=torch.float32):
+    params = [host(torch.zeros(s, dtype=dtype)) for s in shapes]
+    grads = [torch.ones(s, dtype=dtype) for s in shapes]
+    return sp.adamw_plan(params, grads, [sp.adam_state(p, bits) for p in params]), params, grads
+
+
+@pytest.mark.parametrize("which", ["param", "grad", "m", "v"])
+@pytest.mark.parametrize("change", [lambda t: t[:32], lambda t: t.t(), lambda t: t.view(torch.int32), lambda t: t[:0],
+                                    lambda t: t[:, :1]], ids=["half", "turned", "type", "empty", "column"])
+def test_a_change_at_the_same_address_is_refused(which, change):
+    plan, params, grads = plan_of((64, 64), (5,))
+    t = dict(param=params[0], grad=grads[0], m=plan.states[0].m, v=plan.states[0].v)[which]
+    whole, at = t.data, t.data_ptr()
+    t.data = change(whole)
+    assert t.data_ptr() in (at, 0)
+    for _ in range(2):  # (and stays refused)
+        with pytest.raises((ValueError, TypeError)):
+            plan._follow()
+    t.data = whole
+    plan._follow()
+
+
+def test_a_scale_that_lost_elements_is_refused():
+    plan, _, _ = plan_of((600,), bits=8)
+    s = plan.states[0].m_scale
+    s.data = s.data[:1]
+    with pytest.raises(ValueError, match="m_scale"):
+        plan._follow()
+
+
+def test_another_shape_of_the_same_elements_is_followed():
+    plan, params, grads = plan_of((6, 4), (3,))
+    params[0].data = params[0].data.view(24)
+    grads[0].data = torch.full((24,), 2.0)
+    plan._follow()
+    table = plan._calls[0][1]
+    assert table[0].n == 24 and table[0].param == params[0].data_ptr() and table[0].grad == grads[0].data_ptr()
+    assert table[1].grad == grads[1].data_ptr()
+
+
+def test_the_binding_says_what_is_not_built(monkeypatch):
+    import sys
+
+    from paper_2608_09713_amd import training
+    monkeypatch.setattr(training, "_note", None)
+    monkeypatch.setitem(sys.modules, "paper_2608_09713_amd._tensors", None)
+    monkeypatch.delattr(sp, "_tensors", raising=False)
+    with pytest.raises(ImportError, match="build"):
+        plan_of((4,))
+
+
+def test_notes_are_of_tensors():
+    from paper_2608_09713_amd import training
+    note = training._tensor_notes()
+    t = torch.zeros(6)
+    assert note((t, t[1:])) == note((t, t[1:])) != note((t, t[2:]))
+    assert note(()) == b"" and len(note((t,))) * 2 == len(note((t, t)))
+    for bad in ([t], (t, None), (3,)):
+        with pytest.raises(TypeError):
+            note(bad)
