@@ -309,8 +309,8 @@ class AdamWPlan:
     def _distinct(self):
         """Refuses tensors that are written twice in a step."""
         spans = []
-        for t in (*self.params, *(self.masters or ()), *(x for s in self.states for x in s if x is not None)):
-            if t.numel():
+        for t in (*self.params, *(self.masters or ()), *(x for s in self.states for x in s)):
+            if t is not None and t.numel():
                 spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
         spans.sort()
         for (_, end), (start, _) in zip(spans, spans[1:]):
@@ -347,8 +347,8 @@ def adamw(params, grads, states, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_
     ``adam_state``, one for each parameter; ``step`` counts from 1; ``grads`` of
     float32 or the parameters' type, times ``grad_scale`` (a float32 device tensor
     of one element) if given; ``masters``: float32 copies of 16-bit parameters,
-    which are stepped and rounded into them.  The rates are taken at the call: a
-    captured call repeats them."""
+    which are stepped and rounded into them (None for a parameter without one).
+    The rates are taken at the call: a captured call repeats them."""
     AdamWPlan(params, grads, states, masters).step(lr, step, betas, eps, weight_decay, grad_scale)
 
 

@@ -83,3 +83,20 @@ def test_notes_are_of_tensors():
     for bad in ([t], (t, None), (3,)):
         with pytest.raises(TypeError):
             note(bad)
+
+
+@pytest.mark.parametrize("order", [1, -1])
+def test_copies_of_some_parameters(order):
+    # (32-bit parameters have no copy: None beside the others')
+    shapes, types = [(300,), (7,), (40,)], [torch.bfloat16, torch.float32, torch.float16]
+    params = [host(torch.zeros(s, dtype=t)) for s, t in zip(shapes, types)][::order]
+    masters = [None if p.dtype == torch.float32 else p.float() for p in params]
+    plan = sp.adamw_plan(params, [torch.ones_like(p) for p in params], [sp.adam_state(p) for p in params], masters)
+    assert len(plan._calls) == 3
+    for how, table, _ in plan._calls:
+        row, k = table[0], next(k for k, p in enumerate(params) if p.numel() == table[0].n)
+        assert row.master == (None if masters[k] is None else masters[k].data_ptr())
+    twice = [params[0], params[0]]
+    with pytest.raises(ValueError, match="overlap"):
+        sp.adamw_plan(params[:1] + [host(torch.zeros_like(params[0]))], twice, [sp.adam_state(p) for p in twice],
+                      [masters[0], masters[0]])
