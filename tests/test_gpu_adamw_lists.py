@@ -43,3 +43,10 @@ def same_as_alone(kinds, bits):
 def test_copies_of_some_parameters(bits, order):
     kinds = [(300, torch.bfloat16, True), (77, torch.float32, False), (4100, torch.float16, True), (9, torch.bfloat16, False)]
     same_as_alone(kinds[::order], bits)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("copy", [False, True])
+def test_an_empty_tensor_in_front(bits, copy):
+    same_as_alone([(0, torch.bfloat16, copy), (500, torch.bfloat16, copy), (0, torch.bfloat16, copy), (33, torch.bfloat16, copy)],
+                  bits)

@@ -1,5 +1,6 @@
 """What an AdamW plan sees of its tensors before a step, on the host: tensors of
 the host stand in for a device's, and no step is enqueued."""
+import ctypes
 import os
 
 import pytest
@@ -7,6 +8,8 @@ import torch
 
 import paper_2608_09713_amd as sp
 from paper_2608_09713_amd import build
+from tests.test_rows_refusals import INVALID, P, lib  # noqa: F401
+from tests.test_training_refusals import adam
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -100,3 +103,21 @@ def test_copies_of_some_parameters(order):
     with pytest.raises(ValueError, match="overlap"):
         sp.adamw_plan(params[:1] + [host(torch.zeros_like(params[0]))], twice, [sp.adam_state(p) for p in twice],
                       [masters[0], masters[0]])
+
+
+def test_an_empty_tensor_in_front(lib):  # noqa: F811
+    # (its address, and its copy's, may be null: the others decide whether copies are given)
+    def step(*tensors, pt=2):
+        table = (sp._AdamTensor * len(tensors))(*tensors)
+        how = sp._AdamStep(pt, pt, 32, 1, 1e-3, 0.9, 0.99, 1e-8, 0.1, None)
+        return lib.spsyrk_adamw(table, len(tensors), ctypes.byref(how), None)
+
+    empty = adam(n=0, param=None, grad=None, m=None, v=None)
+    mixed = (adam(master=P), adam())
+    assert step(empty, *mixed) == step(*mixed) == step(*mixed[::-1]) == INVALID
+    assert b"all tensors or for none" in lib.spsyrk_last_error_detail()
+    # (an address off its boundary is refused behind that check, before any device call)
+    assert step(empty, adam(master=P + 2)) == step(empty, adam(master=P), adam(master=P + 2)) == INVALID
+    assert b"master is not aligned" in lib.spsyrk_last_error_detail()
+    assert step(empty, adam(master=P), pt=0) == INVALID
+    assert b"no master copy" in lib.spsyrk_last_error_detail()
