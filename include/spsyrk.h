@@ -534,8 +534,9 @@ spsyrk_status spsyrk_block_norm_grad(const spsyrk_dense* dY, const spsyrk_dense*
  * product rounded), rounded to a float, and c the nearest code (by 127 sqrt(|m| / S), 255 (v / S)^(1/4)), at least 1 for v > 0.
  * The update is that of the values before they are coded.  All zeros is a state
  * to begin with.  A value that is not a finite float makes S NaN for its block.
- * Tensors must not overlap each other; their arrays are as large as n says (2^33 or
- * more: SPSYRK_ERR_SHAPE), and the call needs no workspace.  The rates are the
+ * Arrays that are written must not overlap each other, nor a gradient (but a param may
+ * be its own); they are as large as n says (2^33 or more: SPSYRK_ERR_SHAPE), and the
+ * call needs no workspace.  The rates are the
  * host's: a captured call repeats them.  grad_scale is read on the device.
  */
 #define SPSYRK_ADAM_BLOCK 256

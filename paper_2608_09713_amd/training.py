@@ -307,15 +307,23 @@ class AdamWPlan:
         self._seen = seen
 
     def _distinct(self):
-        """Refuses tensors that are written twice in a step."""
+        """Refuses tensors that are written twice in a step, or read as a gradient
+        while they are written (but for a parameter that is its own gradient, each
+        element of which is read and written by one thread)."""
+        written = [*self.params, *(self.masters or ()), *(x for s in self.states for x in s)]
+        read = [g for p, g in zip(self.params, self.grads) if g.data_ptr() != p.data_ptr() or g.dtype != p.dtype]
         spans = []
-        for t in (*self.params, *(self.masters or ()), *(x for s in self.states for x in s)):
-            if t is not None and t.numel():
-                spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
+        for ts, write in ((written, True), (read, False)):
+            for t in ts:
+                if t is not None and t.numel():
+                    spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), write))
         spans.sort()
-        for (_, end), (start, _) in zip(spans, spans[1:]):
-            if start < end:
-                raise ValueError("tensors that a step writes must not overlap (the same one twice?)")
+        last = {True: 0, False: 0}  # where what was written (read) so far ends
+        for start, end, write in spans:
+            if start < last[True] or (write and start < last[False]):
+                raise ValueError("tensors that a step writes must not overlap, nor be the gradients of others (the same "
+                                 "one twice?)")
+            last[write] = max(last[write], end)
 
     def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None):
         """One step, in place (``adamw``)."""

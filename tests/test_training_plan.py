@@ -121,3 +121,30 @@ def test_an_empty_tensor_in_front(lib):  # noqa: F811
     assert b"master is not aligned" in lib.spsyrk_last_error_detail()
     assert step(empty, adam(master=P), pt=0) == INVALID
     assert b"no master copy" in lib.spsyrk_last_error_detail()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_that_a_step_writes_are_refused(bits):
+    # (a gradient is read while other tensors, or other elements of the same one, are written)
+    a, b, g = host(torch.zeros(512)), host(torch.zeros(512)), torch.ones(512)
+    s, r = sp.adam_state(a, bits), sp.adam_state(b, bits)
+    buffer = torch.zeros(1024)
+    for params, grads in (([a, b], [g, a]), ([a, b], [b, g]), ([host(buffer[:512])], [buffer[100:612]]),
+                          ([host(buffer[512:])], [buffer[1:513]])):
+        with pytest.raises(ValueError, match="overlap"):
+            sp.adamw_plan(params, grads, [s, r][:len(params)])
+    if bits == 32:
+        with pytest.raises(ValueError, match="overlap"):
+            sp.adamw_plan([a], [s.m], [s])
+    sp.adamw_plan([a, b], [g, g], [s, r])  # (one gradient of two parameters is read twice)
+    sp.adamw_plan([a], [a], [s])           # (each element is its own)
+    sp.adamw_plan([host(buffer[:512])], [buffer[512:]], [s])
+    sp.adamw_plan([host(buffer[:0]), a], [buffer[:0], g], [sp.adam_state(buffer[:0], bits), r])
+
+
+def test_a_gradient_exchanged_for_a_parameter_is_refused():
+    plan, params, grads = plan_of((8, 8), (64,))
+    grads[0].data = params[1].data
+    for _ in range(2):
+        with pytest.raises(ValueError, match="overlap"):
+            plan._follow()
