@@ -227,7 +227,8 @@ class AdamWPlan:
     """AdamW steps over the same tensors.  The plan keeps the tensors; their
     addresses, sizes, types and layouts are read again at every step, so it follows
     tensors whose storage was exchanged (``.data = ...``) for one of the same type and
-    size, and refuses others.  Parameters that require gradients count a step as a
+    size, and refuses others.  A gradient that was its parameter's ``grad`` has to stay
+    that (``zero_grad(set_to_none=False)``).  Parameters that require gradients count a step as a
     change in place, so that autograd refuses a backward pass that saved them
     before."""
 
@@ -242,6 +243,7 @@ class AdamWPlan:
         if params and not params[0].is_cuda:
             raise TypeError("params must be device tensors")
         self._recorded = [p for p in params if p.requires_grad]
+        self._of_autograd = [(p, g) for p, g in zip(params, grads) if p.is_leaf and p.grad is g]
         self._kinds = self._checked()
         self._all = tuple(t for t in (*params, *grads, *(masters or ()), *(t for s in states for t in s)) if t is not None)
         groups = {}
@@ -293,6 +295,10 @@ class AdamWPlan:
         """The tensors' present addresses into the tables.  What a step relies on is
         compared whole: a tensor that has changed its size, type or order may still
         have its old address."""
+        for p, g in self._of_autograd:
+            if p.grad is not g:
+                raise ValueError("a parameter's grad is no longer the tensor that the plan was given (set to None and made "
+                                 "anew?): keep it, or make a plan of the new ones")
         seen = _tensor_notes()(self._all)
         if seen == self._seen:
             return

@@ -148,3 +148,25 @@ def test_a_gradient_exchanged_for_a_parameter_is_refused():
     for _ in range(2):
         with pytest.raises(ValueError, match="overlap"):
             plan._follow()
+
+
+def test_a_gradient_that_autograd_replaced_is_refused():
+    # (a plan over p.grad: set to None and made anew, the plan's tensor is the old gradient)
+    params = [host(torch.zeros(6)).requires_grad_() for _ in range(2)]
+    for p in params:
+        p.grad = torch.ones(6)
+    plan = sp.adamw_plan(params, [p.grad for p in params], [sp.adam_state(p) for p in params])
+    plan._follow()
+    old = params[1].grad
+    for new in (None, torch.ones(6)):
+        params[1].grad = new
+        with pytest.raises(ValueError, match="grad"):
+            plan._follow()
+    params[1].grad = old
+    params[1].grad.data = torch.full((6,), 2.0)
+    plan._follow()
+    assert plan._calls[0][1][1].grad == old.data_ptr()
+    # (tensors of its own: what autograd holds beside them is another's)
+    other = sp.adamw_plan(params, [torch.ones(6) for _ in params], [sp.adam_state(p) for p in params])
+    params[0].grad = None
+    other._follow()
