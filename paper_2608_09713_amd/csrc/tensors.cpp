@@ -22,23 +22,23 @@ struct Seen {
 };
 static_assert(sizeof(Seen) == 24, "no bytes between the members");
 
+// whether it is a tuple of tensors; sets the error if not
+bool are_tensors(PyObject* tensors) {
+    bool ok = PyTuple_Check(tensors);
+    for (Py_ssize_t i = 0; ok && i < PyTuple_GET_SIZE(tensors); ++i) ok = THPVariable_Check(PyTuple_GET_ITEM(tensors, i));
+    if (!ok) PyErr_SetString(PyExc_TypeError, "a tuple of tensors is needed");
+    return ok;
+}
+
 PyObject* note(PyObject*, PyObject* tensors) {
     HANDLE_TH_ERRORS
-    if (!PyTuple_Check(tensors)) {
-        PyErr_SetString(PyExc_TypeError, "a tuple of tensors is needed");
-        return nullptr;
-    }
+    if (!are_tensors(tensors)) return nullptr;
     const Py_ssize_t n = PyTuple_GET_SIZE(tensors);
     THPObjectPtr out(PyBytes_FromStringAndSize(nullptr, n * Py_ssize_t(sizeof(Seen))));
     if (!out) return nullptr;
     char* to = PyBytes_AsString(out.get());
     for (Py_ssize_t i = 0; i < n; ++i, to += sizeof(Seen)) {
-        PyObject* o = PyTuple_GET_ITEM(tensors, i);
-        if (!THPVariable_Check(o)) {
-            PyErr_SetString(PyExc_TypeError, "a tuple of tensors is needed");
-            return nullptr;
-        }
-        const at::Tensor& t = THPVariable_Unpack(o);
+        const at::Tensor& t = THPVariable_Unpack(PyTuple_GET_ITEM(tensors, i));
         Seen s;
         s.address = int64_t(reinterpret_cast<intptr_t>(t.data_ptr()));
         s.size = t.numel();
@@ -51,7 +51,21 @@ PyObject* note(PyObject*, PyObject* tensors) {
     END_HANDLE_TH_ERRORS
 }
 
+// changed(tensors): counts a change in place of each, so that autograd refuses a
+// backward pass that saved one before.  (Tensors of inference mode have no count.)
+PyObject* changed(PyObject*, PyObject* tensors) {
+    HANDLE_TH_ERRORS
+    if (!are_tensors(tensors)) return nullptr;
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(tensors); ++i) {
+        const at::Tensor& t = THPVariable_Unpack(PyTuple_GET_ITEM(tensors, i));
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    }
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {{"note", note, METH_O, "Addresses, sizes, types, devices and layouts of a tuple of tensors."},
+                         {"changed", changed, METH_O, "Counts a change in place of each tensor of a tuple."},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -207,20 +207,20 @@ def _state_bits(state, numel):
 
 
 _ptr = torch.Tensor.data_ptr
-_note = None
+_tensors = None
 
 
-def _tensor_notes():
-    """``note`` of csrc/tensors.cpp; raises if that has not been built."""
-    global _note
-    if _note is None:
+def _native():
+    """The module of csrc/tensors.cpp; raises if that has not been built."""
+    global _tensors
+    if _tensors is None:
         try:
-            from . import _tensors
+            from . import _tensors as module
         except ImportError as e:
             raise ImportError("_tensors.so is missing or of another torch: run `python -m paper_2608_09713_amd.build` "
                               "(or __graft_entry__.build()) first") from e
-        _note = _tensors.note
-    return _note
+        _tensors = module
+    return _tensors
 
 
 class AdamWPlan:
@@ -228,9 +228,8 @@ class AdamWPlan:
     addresses, sizes, types and layouts are read again at every step, so it follows
     tensors whose storage was exchanged (``.data = ...``) for one of the same type and
     size, and refuses others.  A gradient that was its parameter's ``grad`` has to stay
-    that (``zero_grad(set_to_none=False)``).  Parameters that require gradients count a step as a
-    change in place, so that autograd refuses a backward pass that saved them
-    before."""
+    that (``zero_grad(set_to_none=False)``).  A step counts as a change in place of all
+    that it writes, so that autograd refuses a backward pass that saved it before."""
 
     def __init__(self, params, grads, states, masters=None):
         params, grads = list(params), list(grads)
@@ -242,10 +241,10 @@ class AdamWPlan:
         self._device = params[0].get_device() if params else -1
         if params and not params[0].is_cuda:
             raise TypeError("params must be device tensors")
-        self._recorded = [p for p in params if p.requires_grad]
         self._of_autograd = [(p, g) for p, g in zip(params, grads) if p.is_leaf and p.grad is g]
         self._kinds = self._checked()
-        self._all = tuple(t for t in (*params, *grads, *(masters or ()), *(t for s in states for t in s)) if t is not None)
+        self._written = tuple(t for t in (*params, *(masters or ()), *(t for s in states for t in s)) if t is not None)
+        self._all = (*self._written, *grads)
         groups = {}
         for k, (_, *kind) in enumerate(self._kinds):
             groups.setdefault(tuple(kind), []).append(k)
@@ -299,7 +298,7 @@ class AdamWPlan:
             if p.grad is not g:
                 raise ValueError("a parameter's grad is no longer the tensor that the plan was given (set to None and made "
                                  "anew?): keep it, or make a plan of the new ones")
-        seen = _tensor_notes()(self._all)
+        seen = _native().note(self._all)
         if seen == self._seen:
             return
         if self._seen is not None and self._checked() != self._kinds:
@@ -316,12 +315,11 @@ class AdamWPlan:
         """Refuses tensors that are written twice in a step, or read as a gradient
         while they are written (but for a parameter that is its own gradient, each
         element of which is read and written by one thread)."""
-        written = [*self.params, *(self.masters or ()), *(x for s in self.states for x in s)]
         read = [g for p, g in zip(self.params, self.grads) if g.data_ptr() != p.data_ptr() or g.dtype != p.dtype]
         spans = []
-        for ts, write in ((written, True), (read, False)):
+        for ts, write in ((self._written, True), (read, False)):
             for t in ts:
-                if t is not None and t.numel():
+                if t.numel():
                     spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), write))
         spans.sort()
         last = {True: 0, False: 0}  # where what was written (read) so far ends
@@ -345,8 +343,7 @@ class AdamWPlan:
                 how.step, how.lr, how.eps, how.weight_decay, how.grad_scale = step, lr, eps, weight_decay, scale
                 how.beta1, how.beta2 = betas
                 _check(lib.spsyrk_adamw(table, len(table), _byref(how), _raw_stream(self._device)))
-        if self._recorded:
-            torch.autograd.graph.increment_version(self._recorded)
+        _tensors.changed(self._written)
 
 
 def adamw_plan(params, grads, states, masters=None):

@@ -70,7 +70,7 @@ def test_the_binding_says_what_is_not_built(monkeypatch):
     import sys
 
     from paper_2608_09713_amd import training
-    monkeypatch.setattr(training, "_note", None)
+    monkeypatch.setattr(training, "_tensors", None)
     monkeypatch.setitem(sys.modules, "paper_2608_09713_amd._tensors", None)
     monkeypatch.delattr(sp, "_tensors", raising=False)
     with pytest.raises(ImportError, match="build"):
@@ -79,7 +79,7 @@ def test_the_binding_says_what_is_not_built(monkeypatch):
 
 def test_notes_are_of_tensors():
     from paper_2608_09713_amd import training
-    note = training._tensor_notes()
+    note = training._native().note
     t = torch.zeros(6)
     assert note((t, t[1:])) == note((t, t[1:])) != note((t, t[2:]))
     assert note(()) == b"" and len(note((t,))) * 2 == len(note((t, t)))
@@ -170,3 +170,31 @@ def test_a_gradient_that_autograd_replaced_is_refused():
     other = sp.adamw_plan(params, [torch.ones(6) for _ in params], [sp.adam_state(p) for p in params])
     params[0].grad = None
     other._follow()
+
+
+def test_a_step_counts_as_a_change_of_all_that_it_writes(monkeypatch):
+    from paper_2608_09713_amd import training
+
+    class Library:
+        @staticmethod
+        def spsyrk_adamw(*_):
+            return 0
+
+    monkeypatch.setattr(sp, "_lib", Library)
+    monkeypatch.setattr(training, "_raw_stream", lambda device: 0)
+    w = host(torch.ones(8, dtype=torch.bfloat16))
+    master, g = torch.ones(8), torch.ones(8, dtype=torch.bfloat16)
+    state = sp.adam_state(w)
+    with torch.inference_mode():
+        frozen = torch.ones(8)  # (has no count of its changes)
+    plan = sp.adamw_plan([w, host(frozen)], [g, frozen.clone()], [state, sp.adam_state(frozen)], [master, None])
+    x = torch.ones(8, requires_grad=True)
+    saved = [(x * t).sum() for t in (w, master, state.m, state.v)]
+    kept = (x * g).sum()
+    w.requires_grad_()  # (after the plan was made)
+    own = (w * w).sum()
+    plan.step(1e-3, 1)
+    for loss in (*saved, own):
+        with pytest.raises(RuntimeError, match="inplace"):
+            loss.backward()
+    kept.backward()
