@@ -8,8 +8,8 @@ Leading dimensions count as rows where they can be walked with one stride.
 Work is enqueued on the current stream of the tensors' device and nothing waits
 for it.  Autograd does not record these calls: every gradient is a call of its
 own.  ``embed``, ``layer_norm`` and ``distill`` refuse inputs that require a
-gradient while gradients are recorded, as it would be lost; call them under
-``torch.no_grad()`` or on detached tensors.
+gradient while gradients are recorded, as it would be lost (and ones with a
+forward-mode tangent); call them under ``torch.no_grad()`` or on detached tensors.
 """
 from __future__ import annotations
 
@@ -18,6 +18,7 @@ import functools
 import threading
 
 import torch
+import torch.autograd.forward_ad as _forward_ad
 
 import paper_2608_09713_amd as _sp
 
@@ -48,11 +49,17 @@ def _rows(t, name):
 
 
 def _unrecorded(gradient, *tensors):
-    """Refuses inputs whose gradient autograd would be expected to pass on."""
+    """Refuses inputs whose gradient, or forward-mode tangent, autograd would be expected to pass on."""
     for t in tensors:
         if t is not None and t.requires_grad and torch.is_grad_enabled():
             raise RuntimeError("autograd does not record this call, and an input requires a gradient: call it under "
                                f"torch.no_grad() or on detached tensors, and take the gradient from {gradient}")
+    # (the level first: unpacking costs as much as the rest of a call's checks)
+    if _forward_ad._current_level >= 0:
+        for t in tensors:
+            if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+                raise RuntimeError("forward-mode derivatives do not pass through this call, and an input has a tangent: "
+                                   "call it on detached tensors")
 
 
 def _like(t):
