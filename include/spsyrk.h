@@ -459,8 +459,9 @@ spsyrk_status spsyrk_distill_grad(const spsyrk_dense* S, const spsyrk_entries* t
  * X: m x d, W: v x d, of one type, d >= 1, v >= 1.  targets: m x v, rectangular
  * rows of one entry and no values; a row whose target lies outside [0, v) is
  * padding and has loss 0.  The logits are formed in 32 bits, piece by piece,
- * and not kept.  Logits that are NaN or infinite make their row's loss NaN or
- * infinite.  loss: m floats; lse: m floats, or NULL.  d of 2^22 or more,
+ * and not kept.  A logit of NaN or inf makes its row's loss NaN or infinite, one of
+ * -inf only its own target's.  The loss of a row that is nearly sure keeps its digits
+ * (it is formed without the target's 1).  loss: m floats; lse: m floats, or NULL.  d of 2^22 or more,
  * v of 2^28 or more: SPSYRK_ERR_SHAPE.  Workspace: 8 bytes for every 64 columns of
  * each of up to 64 rows; of more rows about 256 MB at most, and copies of X and W if their
  * rows are not on 16-byte boundaries or not a multiple of 128 bytes long.

@@ -11,17 +11,19 @@
 // 3.4, 3.5 and 3.8 and G 0.38 (5.6 TB/s).
 // The logits are not kept.  A tile of the product (a piece of the vocabulary by
 // some rows) leaves each row's largest logit and the sum of the exponentials
-// below it; the rows' pieces are joined by a second launch.  The gradient takes
-// some rows at a time and keeps their exponentials, each relative to its tile's
-// largest, in the inputs' type: a rounding of at most half a step of each
-// probability, where a rounded logit would cost several.  `fold` makes G of
-// them in place, the target's entry from its 32-bit logit (its difference to 1
-// would lose all digits of a row that is nearly sure).  The products that follow
-// take W, G and x turned as they lie, with no copies but of x's rows that count.
+// below it; the rows' pieces are joined by a second launch.  The target's logit
+// takes no part in them but is kept apart: of a row that is nearly sure the others'
+// sum e^(z - z[t]) is the loss, all of whose digits a sum with the target's 1 would
+// take.  The gradient takes some rows at a time and keeps their exponentials, each
+// relative to its tile's largest, in the inputs' type: a rounding of at most half a
+// step of each probability, where a rounded logit would cost several.  `fold` makes
+// G of them in place, the target's entry, w (e^-loss - 1), from the 32-bit loss.  The
+// products that follow take W, G and x turned as they lie, with no copies but of x's
+// rows that count.
 //
 // Exponentials are powers of two of differences times log2(e), so that logits
 // up to the floats' ends keep theirs.  A tile's base is at least the lowest
-// float, so that logits of -inf add nothing.
+// float, so that logits of -inf (and a target's place) add nothing.
 #include <algorithm>
 #include <cmath>
 
@@ -51,7 +53,8 @@ __device__ inline float row_weight(const Targets& t, const float* weight, int64_
     return c < 0 || c >= V ? 0.f : weight ? weight[row] : 1.f;
 }
 
-// what a tile leaves of a row: its largest logit, and the sum of exp(logit - largest)
+// what a tile leaves of a row: the largest logit of those that are not the target's,
+// and their sum of exp(logit - largest)
 struct Piece {
     float top, sum;
 };
@@ -100,7 +103,11 @@ __global__ __launch_bounds__(WM* WN* kWave) void logits_kernel(Operand W, Operan
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) h = at_target == i * 16 + r ? acc[i][j][r] : h;
+                for (int r = 0; r < 4; ++r)
+                    if (at_target == i * 16 + r) {
+                        h = acc[i][j][r];
+                        acc[i][j][r] = -__builtin_huge_valf();
+                    }
             if (at_target >= 0 && at_target < FM * 16 && (at_target & 15) < 4) hit[n] = h;
         }
 #pragma unroll
@@ -263,7 +270,10 @@ __global__ __launch_bounds__(kBlock) void logits_few(const T* __restrict__ w, in
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             v[j][r] = m + r < V ? v[j][r] * scale : -__builtin_huge_valf();
-            if (m + r == target && m + r < V) hit[n] = v[j][r];
+            if (m + r == target && m + r < V) {
+                hit[n] = v[j][r];
+                v[j][r] = -__builtin_huge_valf();
+            }
             mx = fmaxf(mx, v[j][r]);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
@@ -294,7 +304,9 @@ __global__ __launch_bounds__(kBlock) void logits_few(const T* __restrict__ w, in
     pieces[n * tm + blockIdx.x] = {mx, s};
 }
 
-// A row's pieces joined: loss and lse (may be null).
+__device__ inline float log_of(float v) { return __builtin_amdgcn_logf(v) * kLn2; }
+
+// A row's pieces joined with the target's logit: loss and lse (may be null).
 __global__ __launch_bounds__(kBlock) void join_pieces(const Piece* __restrict__ pieces, int64_t tm, int64_t rows,
                                                       const float* __restrict__ hit, Targets t, int64_t V,
                                                       float* __restrict__ loss, float* __restrict__ lse) {
@@ -312,11 +324,25 @@ __global__ __launch_bounds__(kBlock) void join_pieces(const Piece* __restrict__ 
         const float mx = wave_max(top);
         s = wave_total(s * exp_of(top - mx));
         if (lane_id() != 0) continue;
-        // (the difference of the two largest terms first: a small loss keeps its digits)
-        const float l = __builtin_amdgcn_logf(s) * kLn2;
         const int64_t target = target_of(t, n);
-        loss[n] = target < 0 || target >= V ? 0.f : mx - hit[n] + l;
-        if (lse) lse[n] = mx + l;
+        if (target < 0 || target >= V) {
+            loss[n] = 0.f;
+            if (lse) lse[n] = mx + log_of(s);
+            continue;
+        }
+        // log(1 + e^d s), by the larger of the two terms
+        const float h = hit[n], d = mx - h;
+        float l, all;
+        if (d <= 0.f) {
+            l = log1pf(s * exp_of(d)) + (h - h);  // (of an infinite h NaN)
+            all = h + l;
+        } else {
+            const float more = log_of(s + exp_of(-d));
+            l = d + more;
+            all = mx + more;
+        }
+        loss[n] = l;
+        if (lse) lse[n] = all;
     }
 }
 
