@@ -463,8 +463,9 @@ spsyrk_status spsyrk_distill_grad(const spsyrk_dense* S, const spsyrk_entries* t
  * -inf only its own target's.  The loss of a row that is nearly sure keeps its digits
  * (it is formed without the target's 1).  loss: m floats; lse: m floats, or NULL.  d of 2^22 or more,
  * v of 2^28 or more: SPSYRK_ERR_SHAPE.  Workspace: 8 bytes for every 64 columns of
- * each of up to 64 rows; of more rows about 256 MB at most, and copies of X and W if their
- * rows are not on 16-byte boundaries or not a multiple of 128 bytes long.
+ * each of up to 64 rows; of more rows about 256 MB at most, or 16 v bytes where that is
+ * more (v above 2^24), and copies of X and W if their rows are not on 16-byte boundaries
+ * or not a multiple of 128 bytes long.
  */
 spsyrk_status spsyrk_linear_cross_entropy(const spsyrk_dense* X, const spsyrk_dense* W, const spsyrk_entries* targets,
                                           float scale, const spsyrk_allocator* al, void* hip_stream, float* loss,

@@ -776,9 +776,10 @@ __global__ __launch_bounds__(kJoinBlock) void join_sums(Sums sums, Spread go, in
 }
 
 // Lanes of a wavefront for up to 64 packs, else a workgroup's threads, one pack
-// each (two of four columns past 1024): the gradient's thread holds four inputs
-// and the next row's, three parameters and two sums for each of its columns, and
-// has no registers for more.  Rows of more than 8192 columns are read again (np 0).
+// each (two of four columns past 1024): the gradient's thread holds four inputs,
+// three parameters and up to three sums for each of its columns, and has no
+// registers for more.  Rows of more than 8192 columns are read again (np 0), by the
+// forward pass too, which goes by the gradient's shapes.
 inline RowShape block_shape(int64_t d, int dt) {
     const int64_t packs = packs_of(d, dt);
     if (packs <= kWave) {

@@ -696,7 +696,7 @@ size_t cross_entropy(const DenseRows& X, const DenseRows& W, const Targets& t, f
         return 0;
     }
     const Operand x = operand_rows<T>(X, c, s), w = operand_rows<T>(W, c, s);
-    // rows at a time: 256 MB of pieces at most
+    // rows at a time: 256 MB of pieces at most, but 256 rows at least (16 V bytes of them)
     const int64_t chunk =
         std::max<int64_t>(kLarge.m, std::min(X.m, (int64_t(1) << 25) / ceil_div(W.m, kSmall.m) / kLarge.m * kLarge.m));
     const int64_t most = std::min(X.m, chunk);

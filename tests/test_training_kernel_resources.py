@@ -37,3 +37,12 @@ def test_adamw_budgets():
     assert len([k for k in ks if "adamw_wide" in k]) == len([k for k in ks if "adamw_narrow" in k]) == 9
     for name, r in ks.items():
         assert r["ScratchSize"] == 0 and r["Occupancy"] >= (8 if "adamw_wide" in name else 4), (name, r)
+
+
+def test_products_keep_two_wavefronts_a_simd():
+    # (by registers and by LDS: one workgroup of eight wavefronts or two of four on a compute unit)
+    products = {k: v for k, v in _report("crossentropy.hip").items() if "logits_kernel" in k or "product_kernel" in k}
+    for name, r in products.items():
+        assert r["Occupancy"] >= 2 and r["VGPRs"] <= 256, (name, r)
+        assert r["LDS"] * (1 if "Li8ELi4ELi2ELi4E" in name else 2) <= 160 * 1024, (name, r)
+    assert sum("Li8ELi4ELi2ELi4E" in k for k in products) == 12
