@@ -10,6 +10,9 @@ an input whose gradient would be lost.
 from __future__ import annotations
 
 import ctypes
+import itertools
+import operator
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -242,32 +245,41 @@ class AdamWPlan:
         if params and not params[0].is_cuda:
             raise TypeError("params must be device tensors")
         self._of_autograd = [(p, g) for p, g in zip(params, grads) if p.is_leaf and p.grad is g]
-        self._kinds = self._checked()
-        self._written = tuple(t for t in (*params, *(masters or ()), *(t for s in states for t in s)) if t is not None)
-        self._all = (*self._written, *grads)
+        columns = [params, masters or [], *([s[c] for s in states] for c in range(4)), grads]
+        # (param, master, m, v, m_scale, v_scale, grad: those that there are)
+        self._columns = [c for c, column in enumerate(columns) if any(t is not None for t in column)]
+        self._all = tuple(t for c in self._columns for t in columns[c])
+        self._written = self._all[:len(self._all) - len(grads)]
+        notes = _native().note(self._all)
+        self._kinds = self._checked(notes)
         groups = {}
-        for k, (_, *kind) in enumerate(self._kinds):
-            groups.setdefault(tuple(kind), []).append(k)
+        for k, kind in enumerate(self._kinds):
+            groups.setdefault(kind[1:], []).append(k)
         # (one call for each kind of tensor)
-        self._calls = []
-        for (pt, gt, bits, wide), index in groups.items():
-            how = _sp._AdamStep(_DTYPE[pt], _DTYPE[gt], bits)
-            columns = [[params[k] for k in index], [grads[k] for k in index], [masters[k] for k in index] if wide else None]
-            columns += [[states[k][c] for k in index] for c in range(4 if bits == 8 else 2)]
-            table = (_sp._AdamTensor * len(index))()
-            for row, k in zip(table, index):
-                row.n = params[k].numel()
-            self._calls.append((how, table, columns))
-        self._seen = None
-        self._follow()
+        self._calls = [(_sp._AdamStep(_DTYPE[pt], _DTYPE[gt], bits), (_sp._AdamTensor * len(index))(), index)
+                       for (pt, gt, bits, _), index in groups.items()]
+        self._fill(notes)
 
-    def _checked(self):
+    def _checked(self, notes):
         """(size, parameter's type, gradient's type, state's bits, with a master copy) of every tensor."""
+        words = memoryview(notes).cast("q").tolist()
+        here = (1 << 16) + (self._device & 0xffff)  # contiguous, on the device
+        if {made >> 32 for made in words[2::3]} - {-1, here} or not all(map(operator.ge, words[0::3], map(bool, words[1::3]))):
+            for t in self._all:
+                if t is not None:
+                    if t.get_device() != self._device:
+                        raise ValueError("all tensors must be on one device")
+                    if not t.is_contiguous():
+                        raise ValueError("all tensors must be contiguous")
+                    if t.numel() and not t.data_ptr():
+                        raise ValueError("a tensor of the plan has no storage")
         kinds = []
         for k, (p, g, s) in enumerate(zip(self.params, self.grads, self.states)):
             w = None if self.masters is None else self.masters[k]
             if p.dtype not in _DTYPE:
                 raise TypeError(f"params must be float32, float16 or bfloat16, not {p.dtype}")
+            if g is None:
+                raise TypeError("every parameter must have a gradient, not None")
             if g.dtype not in (torch.float32, p.dtype):
                 raise TypeError(f"grads must be float32 or the parameter's type, not {g.dtype}")
             n = p.numel()
@@ -278,16 +290,7 @@ class AdamWPlan:
                     raise TypeError("float32 parameters have no master copy")
                 if w.dtype != torch.float32 or w.numel() != n:
                     raise TypeError("a master copy must be float32, of its parameter's size")
-            bits = _state_bits(s, n)
-            for t in (p, g, w, *s):
-                if t is not None:
-                    if t.get_device() != self._device:
-                        raise ValueError("all tensors must be on one device")
-                    if not t.is_contiguous():
-                        raise ValueError("all tensors must be contiguous")
-                    if n and not t.data_ptr():
-                        raise ValueError("a tensor of the plan has no storage")
-            kinds.append((n, p.dtype, g.dtype, bits, w is not None))
+            kinds.append((n, p.dtype, g.dtype, _state_bits(s, n), w is not None))
         return kinds
 
     def _follow(self):
@@ -298,32 +301,38 @@ class AdamWPlan:
             if p.grad is not g:
                 raise ValueError("a parameter's grad is no longer the tensor that the plan was given (set to None and made "
                                  "anew?): keep it, or make a plan of the new ones")
-        seen = _native().note(self._all)
-        if seen == self._seen:
+        notes = _tensors.note(self._all)
+        if notes == self._seen:
             return
-        if self._seen is not None and self._checked() != self._kinds:
+        if self._checked(notes) != self._kinds:
             raise ValueError("a tensor of the plan has changed its type or size")
-        self._distinct()
-        for _, table, columns in self._calls:
-            for name, column in zip(("param", "grad", "master", "m", "v", "m_scale", "v_scale"), columns):
-                if column is not None:
-                    for row, t in zip(table, column):
-                        setattr(row, name, _ptr(t))
-        self._seen = seen
+        self._fill(notes)
 
-    def _distinct(self):
+    def _fill(self, notes):
+        words, n = memoryview(notes).cast("q").tolist(), len(self.params)
+        at, size = words[0::3], words[1::3]
+        self._distinct(at, size)
+        columns = [[0] * n] * 7
+        for i, c in enumerate(self._columns):
+            columns[c] = at[i * n:i * n + n]
+        param, master, m, v, m_scale, v_scale, grad = columns
+        rows = list(zip((k[0] for k in self._kinds), param, grad, master, m, v, m_scale, v_scale))
+        for _, table, index in self._calls:
+            struct.pack_into(f"{8 * len(index)}q", table, 0, *itertools.chain.from_iterable(rows[k] for k in index))
+        self._seen = notes
+
+    def _distinct(self, at, size):
         """Refuses tensors that are written twice in a step, or read as a gradient
         while they are written (but for a parameter that is its own gradient, each
         element of which is read and written by one thread)."""
-        read = [g for p, g in zip(self.params, self.grads) if g.data_ptr() != p.data_ptr() or g.dtype != p.dtype]
-        spans = []
-        for ts, write in ((self._written, True), (read, False)):
-            for t in ts:
-                if t.numel():
-                    spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), write))
-        spans.sort()
+        ends = list(map(operator.add, at, size))
+        spans = sorted(zip(at, ends))
+        if not any(map(operator.gt, (end for _, end in spans), (start for start, _ in spans[1:]))):
+            return  # (no two lie across each other)
+        n, written = len(self.params), len(self._written)
+        own = {written + k for k in range(n) if at[k] == at[written + k] and self.grads[k].dtype == self.params[k].dtype}
         last = {True: 0, False: 0}  # where what was written (read) so far ends
-        for start, end, write in spans:
+        for start, end, write in sorted((at[k], ends[k], k < written) for k in range(len(at)) if size[k] and k not in own):
             if start < last[True] or (write and start < last[False]):
                 raise ValueError("tensors that a step writes must not overlap, nor be the gradients of others (the same "
                                  "one twice?)")

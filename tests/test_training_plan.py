@@ -82,8 +82,8 @@ def test_notes_are_of_tensors():
     note = training._native().note
     t = torch.zeros(6)
     assert note((t, t[1:])) == note((t, t[1:])) != note((t, t[2:]))
-    assert note(()) == b"" and len(note((t,))) * 2 == len(note((t, t)))
-    for bad in ([t], (t, None), (3,)):
+    assert note(()) == b"" and len(note((t,))) * 2 == len(note((t, None))) and note((None,)) != note((t,))
+    for bad in ([t], None, (3,)):
         with pytest.raises(TypeError):
             note(bad)
 
@@ -198,3 +198,36 @@ def test_a_step_counts_as_a_change_of_all_that_it_writes(monkeypatch):
         with pytest.raises(RuntimeError, match="inplace"):
             loss.backward()
     kept.backward()
+
+
+def test_what_a_plan_refuses_when_it_is_made():
+    p, s = host(torch.zeros(6, 6)), sp.adam_state(torch.zeros(6, 6))
+    g = torch.ones(6, 6)
+    with pytest.raises(ValueError, match="contiguous"):
+        sp.adamw_plan([p], [g.t()], [s])
+    with pytest.raises(ValueError, match="contiguous"):
+        sp.adamw_plan([p], [g], [sp.AdamState(s.m, s.v.t())])
+    with pytest.raises(ValueError, match="storage"):
+        sp.adamw_plan([p], [torch.ones((6, 6), device="meta")], [s])
+    empty = g.clone()
+    empty.untyped_storage().resize_(0)
+    with pytest.raises(ValueError, match="storage"):
+        sp.adamw_plan([p], [empty], [s])
+    with pytest.raises(TypeError):
+        sp.adamw_plan([p], [None], [s])
+    with pytest.raises(TypeError):
+        sp.adamw_plan([p], [g.double()], [s])
+    with pytest.raises(ValueError, match="size"):
+        sp.adamw_plan([p], [g[:5]], [s])
+    with pytest.raises(TypeError, match="master"):
+        sp.adamw_plan([p], [g], [s], [g.clone()])
+    plan = sp.adamw_plan([], [], [])
+    assert plan._calls == [] and plan.step(1e-3, 1) is None
+    # storage given back and taken again, as by programs that keep parameters elsewhere between steps
+    plan = sp.adamw_plan([p], [g], [s])
+    g.untyped_storage().resize_(0)
+    with pytest.raises(ValueError, match="storage"):
+        plan._follow()
+    g.untyped_storage().resize_(36 * 4)
+    plan._follow()
+    assert plan._calls[0][1][0].grad == g.data_ptr()
