@@ -7,8 +7,8 @@
 // for few rows by the bytes of W (1 x 32000 x 2048 bf16: 31 us in a call, 22 of them
 // the reading of 131 MB).  8192 x 131072 x 4096 bf16: 6.33 ms, 1390 TFLOP/s of the
 // 1484 that a plain library product reaches here; the chip's clock falls to 1.9 GHz
-// under either.  The gradient of 4096 such rows: 11.0 ms, of which the products take
-// 3.4, 3.5 and 3.8 and G 0.38 (5.6 TB/s).
+// under either.  The gradient of 4096 such rows: 10.8 to 11.3 ms, of which the
+// products take 3.4, 3.5 and 3.8 and G 0.38 (5.6 TB/s).
 // The logits are not kept.  A tile of the product (a piece of the vocabulary by
 // some rows) leaves each row's largest logit and the sum of the exponentials
 // below it; the rows' pieces are joined by a second launch.  The target's logit
@@ -177,9 +177,9 @@ __global__ __launch_bounds__(WM* WN* kWave) void logits_kernel(Operand W, Operan
 // ---- the same for few rows: one reading of W, from memory into the registers of
 // the matrix instructions.  A workgroup takes kFewColumns rows of W, its wavefronts
 // a quarter of k each; rows of any alignment, past their ends zeros.  Bound by W's
-// bytes (32000 x 2048 bf16, one row: 22 us, 5.9 TB/s; four steps of W under way
-// instead of eight no better, 32.4 us a call and 31.9; with loads that pass the caches
-// by 35.7).
+// bytes (32000 x 2048 bf16, one row: 22 us, 5.9 TB/s; of W eight steps under way, 27.2
+// us a call, four 27.7 and two 28.0; with loads that pass the caches by 35.7, of 31.9
+// then).
 
 constexpr int kFewColumns = 64, kFewRows = 64;  // a piece's columns; rows at most
 
@@ -313,6 +313,10 @@ __global__ __launch_bounds__(kBlock) void join_pieces(const Piece* __restrict__ 
     for (int64_t n = int64_t(blockIdx.x) * kWavesPerBlock + threadIdx.x / kWave; n < rows;
          n += int64_t(gridDim.x) * kWavesPerBlock) {
         const Piece* p = pieces + n * tm;
+        // (under way beside the pieces: after them they would be waited for one by one)
+        const int64_t target = target_of(t, n);
+        const bool named = target >= 0 && target < V;
+        const float h = named ? hit[n] : 0.f;
         float top = -3.402823466e38f, s = 0.f;
 #pragma unroll 8
         for (int64_t i = lane_id(); i < tm; i += kWave) {
@@ -324,14 +328,13 @@ __global__ __launch_bounds__(kBlock) void join_pieces(const Piece* __restrict__ 
         const float mx = wave_max(top);
         s = wave_total(s * exp_of(top - mx));
         if (lane_id() != 0) continue;
-        const int64_t target = target_of(t, n);
-        if (target < 0 || target >= V) {
+        if (!named) {
             loss[n] = 0.f;
             if (lse) lse[n] = mx + log_of(s);
             continue;
         }
         // log(1 + e^d s), by the larger of the two terms
-        const float h = hit[n], d = mx - h;
+        const float d = mx - h;
         float l, all;
         if (d <= 0.f) {
             l = log1pf(s * exp_of(d)) + (h - h);  // (of an infinite h NaN)
@@ -546,14 +549,16 @@ __global__ __launch_bounds__(kBlock) void join_parts(Product o, int64_t parts, i
 }
 
 // Tiles of m by n.  16-bit products go by 256 x 256 and eight wavefronts where such
-// tiles fill three quarters of the chip (8192 x 131072 x 4096 bf16: 6.70 ms, by the
-// others 8.53), else by 128 x 128 and four.  Where k can be split, its parts count
+// tiles fill three quarters of the chip (8192 x 131072 x 4096 bf16: 6.25 ms, by the
+// others 7.89), else by 128 x 128 and four.  Where k can be split, its parts count
 // as tiles (2047 x 1001 x 50021 f16: 197 us with eight parts, 237 by small tiles),
 // unless large tiles would be padded by a quarter more.  32-bit products, whose
 // fragments feed the matrix cores four times as long, go by small tiles, which leave
-// less of the last round idle (1001 x 50021 x 250: 257 us, 298 by large ones), or
-// by 128 x 64 where the busiest compute unit has less to do by those (217 x 36096 x
-// 1472: 229 us, 272 by 128 x 128; 25 x 44003 x 257 with its gradient: 123 and 169).
+// less of the last round idle (1001 x 50021 x 250: 244 us, 288 by large ones; 300 x
+// 100000 x 2048: 0.98 ms and 1.90; but 2048 x 32768 x 1024, whole rounds of either:
+// 1.00 and 0.97), or by 128 x 64 where the busiest compute unit has less to do by
+// those (217 x 36096 x 1472: 235 us, 274 by 128 x 128; 25 x 44003 x 257 with its
+// gradient: 112 and 155).
 struct Tile {
     int m, n;
 };
@@ -664,9 +669,10 @@ inline Operand turned(const Operand& o, int64_t columns) { return {o.p, o.ld, co
 
 // Whether the loss of some rows goes by one reading of W (kernel above): up to 16;
 // up to 64 where W would have to be packed for the tiles, or makes too few of them
-// (32 rows of 2000 x 2048 bf16: 16 us, tiles 22; 24 of 50021 x 1001 f16: 53 and 67;
-// but 64 of 131072 x 4096 bf16: 303 and 222, 32 of 32000 x 2048: 32.4 and 30.6; in
-// 32 bits 24 of 50021 x 1024: 69 and 71, 64: 117 and 73).
+// (32 rows of 2000 x 2048 bf16: 17 us, tiles 23; 24 of 50021 x 1001 f16: 53 and 67,
+// though 64 of them 77 and 68; but 64 of 131072 x 4096 bf16: 303 and 223, 32 of
+// 32000 x 2048: 32.4 and 31.3; in 32 bits 24 of 50021 x 1024: 70 and 72, 64: 116 and
+// 74).
 inline bool few_rows(const DenseRows& X, const DenseRows& W) {
     if (X.m <= (X.dt == kDtF32 ? 32 : 16)) return true;
     return X.m <= kFewRows && (!as_they_are(W) || 4 * ceil_div(W.m, kSmall.m) < 3 * kCus);
