@@ -30,10 +30,10 @@ namespace {
 constexpr int kAt = 4;  // elements of a pack: 16 bytes of 32-bit floats
 // Packs of a thread, a workgroup's width apart, and threads of a workgroup.  States
 // of 32 bits: the widest chunks are read and written fastest (160 M elements of
-// bf16 with copies: 980 us by 128 threads, 902 by 256, 888 by 1024; two packs a
-// thread 967).  Of 8 bits, where a wavefront's arithmetic counts, two packs by
-// 256 threads (64 M, with the values: one pack 290 us, by 1024 threads 296, these 280,
-// and 259 with one comparison for values next to a border).
+// bf16 with copies: 965 us by 128 threads, 896 by 256, 888 by 1024; two packs a
+// thread 988).  Of 8 bits, where a wavefront's arithmetic counts, two packs by
+// 256 threads (64 M, with the values: 260 us, by 1024 threads 296; one pack, which took
+// 10 us more before values next to a border had one comparison, 256).
 template <bool NARROW>
 constexpr int kPacks = NARROW ? 2 : 1;
 template <bool NARROW>

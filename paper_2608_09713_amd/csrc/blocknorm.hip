@@ -397,9 +397,10 @@ __device__ inline void add_rows(float (&v)[NP][N], float* lds, int threads, int 
 }
 
 // Four wavefronts a SIMD, two workgroups of 512 threads on a compute unit, even
-// where sums are spilled for it (16384 x 4096, 64 groups: 160 us, 209 without the
-// limit; 262144 x 128, 4096 groups: 75 and 87), but for rows of a wavefront's lanes
-// whose groups are not split (262144 x 128, a gate for each: 86, with it 92).
+// where sums are spilled for it (16384 x 4096, 64 groups: 162 us, 212 without the
+// limit; 262144 x 128, 4096 groups: 75 and 92, 512 groups: 83 and 82), but for rows of
+// a wavefront's lanes whose groups are not split (262144 x 128, a gate for each: 88,
+// with it 93).
 template <typename T, int N, int L, int MOST, int NP, bool ANY, int GATE>
 __global__ __launch_bounds__(MOST) __attribute__((amdgpu_waves_per_eu(L && GATE != kSplit ? 2 : 4))) void
 after_block_grad(GradArgs<T> a) {
@@ -704,9 +705,9 @@ __global__ __launch_bounds__(kBlock) void after_block_sums_long(GradArgs<T> a, c
 // The parts added up.  A workgroup takes some columns of dpre, of dpost (and of the
 // gate, if that is one row) or of a row of the gate, many parts of them side by
 // side: each in its order, then those sums pairwise.  16 columns instead of 64 where
-// few would leave most of the chip idle (512 parts of 1001 columns: 4 us and 6, of
-// 8192: 15 and 5); kGateColumns of a gate's row that has few parts (16384 x 4096, 64
-// rows of the gate, 8 parts each: 209 us in all, 224 by 64 columns).
+// few would leave most of the chip idle (512 parts of 1001 columns: 4.4 us and 4.9; of
+// 4096: 9.6 and 5.8); kGateColumns of a gate's row that has few parts (16384 x 4096, 64
+// rows of the gate, 8 parts each: 161 us in all, 178 by 64 columns).
 constexpr int kJoinBlock = 1024, kGateColumns = 256;
 inline __host__ __device__ int gate_columns(int64_t parts, int columns) { return parts < 16 ? kGateColumns : columns; }
 
@@ -779,7 +780,9 @@ __global__ __launch_bounds__(kJoinBlock) void join_sums(Sums sums, Spread go, in
 // each (two of four columns past 1024): the gradient's thread holds four inputs,
 // three parameters and up to three sums for each of its columns, and has no
 // registers for more.  Rows of more than 8192 columns are read again (np 0), by the
-// forward pass too, which goes by the gradient's shapes.
+// forward pass too, which goes by the gradient's shapes (4096 x 16384 bf16, one gate:
+// forward 128 us, 4.2 TB/s of what has to move, and gradient 341, 2.4; as many elements
+// in rows of 8192: 96, 5.6 TB/s, and 176, 4.6).
 inline RowShape block_shape(int64_t d, int dt) {
     const int64_t packs = packs_of(d, dt);
     if (packs <= kWave) {
@@ -816,8 +819,8 @@ inline void by_block_shape(const RowShape& s, F f) {
 
 // Rows that a workgroup of the gradient has under way, and workgroups: 16
 // wavefronts on a compute unit, as few workgroups as that takes, since each leaves
-// sums of d floats (8191 x 1001: 31 us, with half as many workgroups 37, with twice
-// as many 41; 8192 x 4096: 88, 107 and 100).
+// sums of d floats (8191 x 1001: 29 us, with half as many workgroups 36, with twice
+// as many 36; 8192 x 4096: 80, 103 and 87; but 262144 x 128: 83, 74 and 78).
 inline int grad_rows(const RowShape& s) {
     return s.lanes ? kGradBlock / s.lanes : s.threads && s.threads <= kGradBlock ? kGradBlock / s.threads : 1;
 }
@@ -830,8 +833,8 @@ Spread spread_of(int64_t m, int64_t groups, const RowShape& s) {
     const int64_t room = !s.np ? kLongParts : s.threads > kGradBlock ? kCus : 2 * kCus;
     // Groups of fewer rows than a workgroup takes side by side go whole to a row's
     // threads each, if they are so many that the workgroups would take longer by
-    // turns (262144 x 128: of 16 rows 86 us, split 124; of 2 rows 79 and 725; of 32
-    // rows, which fill a workgroup, 79 split and 92 whole).
+    // turns (262144 x 128: of 16 rows 101 us, split 130; of 2 rows 81 and 728; of 32
+    // rows, which fill a workgroup, 81 split and 105 whole).
     if (rows > 1 && m > 0 && go.per < rows && go.per * room < 2 * groups) {
         go.whole = true;
         go.slots = std::min(room, ceil_div(groups, rows));
