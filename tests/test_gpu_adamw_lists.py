@@ -50,3 +50,19 @@ def test_copies_of_some_parameters(bits, order):
 def test_an_empty_tensor_in_front(bits, copy):
     same_as_alone([(0, torch.bfloat16, copy), (500, torch.bfloat16, copy), (0, torch.bfloat16, copy), (33, torch.bfloat16, copy)],
                   bits)
+
+
+def test_a_change_at_the_same_address_is_refused_before_anything_is_stepped():
+    w, g = torch.ones((64, 64), device=DEV), torch.ones((64, 64), device=DEV)
+    state = sp.adam_state(w)
+    plan = sp.adamw_plan([w], [g], [state])
+    whole = w.data
+    for other in (whole[:32], whole.t(), whole.view(torch.int32)):
+        w.data = other
+        for _ in range(2):
+            with pytest.raises((ValueError, TypeError)):
+                plan.step(LR, 1)
+    assert (whole == 1).all() and not state.m.any()
+    w.data = whole
+    plan.step(LR, 1, weight_decay=0.0)
+    assert (1 - whole - LR).abs().max() <= 2.0 ** -23  # (a first step of one rate, and a rounding near 1)
